@@ -116,11 +116,41 @@ typedef struct fdh_block {
   int32_t kind;         /* fdh_param_kind */
 } fdh_block;
 
+/* Queries and keys of a Llama-family model between their projection and
+ * attention.  norm: RMSNorm of every query and key head over its head_dim
+ * elements (epsilon norm_eps) before the rotation, with one gain vector for the
+ * queries and one for the keys of a layer; they are parameters of the layer
+ * ("h0.qnorm.g", "h0.knorm.g", behind its wqkv).  n_axes: position axes of the
+ * rotation (time, height, width, ...).  Pair i of a head (elements i and
+ * i + head_dim/2) turns by rope_base^(-2i/head_dim) times the token's position
+ * along the pair's axis; sections[a] pairs belong to axis a (their sum is
+ * head_dim / 2), axis after axis or, interleaved, pairs a, a + n_axes, ... to
+ * axis a >= 1 and the others to axis 0.  n_axes 0 is one axis (sections unread). */
+#define FDH_MAX_AXES 4
+typedef struct fdh_qk_config {
+  int32_t norm;                     /* 0 or 1 */
+  int32_t n_axes;                   /* 0 .. FDH_MAX_AXES */
+  int32_t sections[FDH_MAX_AXES];
+  int32_t interleaved;              /* 0 or 1 */
+  int32_t reserved;                 /* 0 */
+} fdh_qk_config;
+
+/* The gains of one layer's query and key norm (device pointers). */
+typedef struct fdh_qk_gains {
+  const void *q, *k;        /* [head_dim] of the context's dtype */
+  const float *v_q, *v_k;   /* [head_dim] directions; NULL: the same gain at both points */
+  double eps;               /* the points are q + eps v_q and q - eps v_q; positive, finite */
+} fdh_qk_gains;
+
 typedef struct fdh_ctx fdh_ctx;
 
 /* Create a context for one model on the current HIP device; hip_stream is a
  * hipStream_t (NULL = default stream).  *out receives the context. */
 fdh_status fdh_create(const fdh_model_config* cfg, void* hip_stream, fdh_ctx** out);
+/* fdh_create with a per-head norm of queries and keys and position axes (Llama
+ * family, head_dim <= 256: FDH_ERR_UNSUPPORTED otherwise; FDH_ERR_INVALID_ARG for
+ * sections that do not divide the pairs).  qk NULL or all zero is fdh_create. */
+fdh_status fdh_create_qk(const fdh_model_config* cfg, const fdh_qk_config* qk, void* hip_stream, fdh_ctx** out);
 void fdh_destroy(fdh_ctx* ctx);
 int32_t fdh_api_version(void);
 
@@ -207,6 +237,49 @@ fdh_status fdh_bind(fdh_ctx* ctx, const void* params_dev, const int32_t* tokens_
  * QUAD_DIAG contexts take nbatch = 0. */
 fdh_status fdh_bind_dataset(fdh_ctx* ctx, const void* params_dev, const fdh_batch* batches, int32_t nbatch,
                             double eps, int32_t reduction, int64_t* n_targets);
+
+/* fdh_bind_dataset with the rotation's positions (Llama family, head_dim <= 256).
+ * positions: host array of nbatch device pointers, positions[i] int32
+ * [axes, B, S] of batch i (axes = max(1, n_axes)), any int32 values, or NULL for
+ * 0 .. S - 1 on every axis (text); a NULL array is fdh_bind_dataset.  The pointers
+ * are kept, not copied.  The attention mask stays the causal one of the token
+ * order. */
+fdh_status fdh_bind_dataset_positions(fdh_ctx* ctx, const void* params_dev, const fdh_batch* batches,
+                                      const int32_t* const* positions, int32_t nbatch, double eps, int32_t reduction,
+                                      int64_t* n_targets);
+
+/* The q/k front of a layer on caller-owned device memory, as the HVP runs it:
+ * every tensor is a pair, _m the mean and _d the half difference of its values
+ * at two points.  x: the q/k/v projection's output, B*S rows of
+ * (n_heads + 2 n_kv_heads) head_dim elements of the context's dtype (query heads,
+ * key heads, value heads), ldx elements apart; y: the same with query and key heads
+ * normed (contexts with norm: gains required, otherwise NULL) and turned, value
+ * heads copied.  y may be x (both pointers and the stride the same: the value heads
+ * stay as they are); no other overlap.  positions_dev: int32 [axes, B, S] or NULL
+ * (0 .. S - 1 in every row).  Pointers 16-byte aligned, strides in multiples of 16
+ * bytes; positions and gains of any element alignment.  Any B*S from 0 (nothing is
+ * done) to below 2^31; needs no workspace.  Each output is rounded once from fp32
+ * arithmetic with fp64 sums; a head that holds a NaN or an infinity is normed to NaN.
+ * Only enqueued on the context stream (no wait, no allocation: may be captured in
+ * a graph); a layer's call for one token is the call with B = S = 1. */
+fdh_status fdh_qk_forward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_t* positions_dev, int32_t B, int32_t S,
+                          const void* x_m, const void* x_d, int64_t ldx, void* y_m, void* y_d, int64_t ldy);
+
+/* Its backward: dx (context dtype, as x) from dy (float32, as y); the value heads are
+ * rounded to the dtype.  With norm, x is the forward's input and dgq, dgk (float32
+ * [head_dim]) receive, or with accumulate != 0 are added, the gains' entries of Hv:
+ * the half difference of their gradients, summed over tokens and heads, over eps
+ * (fp64 sums in a fixed order: the same bits in every call); without norm x may be
+ * NULL and dgq, dgk are NULL.  scratch: device memory, 16-byte aligned, of at least
+ * fdh_qk_scratch_bytes (0 without norm), in use until the call's work is done: calls
+ * that may overlap on the device need scratch of their own.  No output overlaps an
+ * input.  B*S = 0 sets dgq and dgk to zero (or leaves them).  Only enqueued, as
+ * fdh_qk_forward. */
+fdh_status fdh_qk_backward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_t* positions_dev, int32_t B, int32_t S,
+                           const void* x_m, const void* x_d, int64_t ldx, const float* dy_m, const float* dy_d,
+                           int64_t lddy, void* dx_m, void* dx_d, int64_t lddx, float* dgq, float* dgk,
+                           int32_t accumulate, void* scratch, size_t scratch_bytes);
+fdh_status fdh_qk_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes);
 
 /* hv = H v of the bound operator (fdh_bind or fdh_bind_dataset): one FD-HVP
  * per batch, accumulated into hv in batch order; fdh_last_losses then returns

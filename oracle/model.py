@@ -15,6 +15,10 @@ Llama family   token embedding; blocks
                x += Wd . (silu(Wg h') * (Wu h')), h' = RMS2 x;
                grouped-query attention (head i uses KV head i // (H / Hkv)),
                rotate-half RoPE; final RMSNorm; untied LM head; no biases.
+               With qk_norm every query and key head goes through an RMSNorm
+               over its dh elements before the rotation (one gain vector for
+               the queries, one for the keys of a layer); with rope_sections
+               pair i of a head turns by the position along its own axis.
 
 LayerNorm eps and RMSNorm eps are taken from the config (1e-5), LayerNorm
 variance is the biased one.  The loss is the mean over the B*(S-1) next-token
@@ -25,7 +29,8 @@ layer partition of the block-diagonal test in section 6):
 
 GPT-2:  wte[V,d] wpe[S_max,d] | per layer: ln1.g ln1.b wqkv[3d,d] bqkv[3d]
         wo[d,d] bo[d] ln2.g ln2.b w1[F,d] b1[F] w2[d,F] b2[d] | lnf.g lnf.b
-Llama:  embed[V,d] | per layer: norm1.g wqkv[(H+2Hkv)dh,d] wo[d,H dh]
+Llama:  embed[V,d] | per layer: norm1.g wqkv[(H+2Hkv)dh,d]
+        (with qk_norm: qnorm.g[dh] knorm.g[dh]) wo[d,H dh]
         norm2.g wgu[2F,d] (gate rows, then up rows) wd[d,F] | normf.g head[V,d]
 """
 from __future__ import annotations
@@ -54,6 +59,9 @@ class ModelConfig:
     norm_eps: float = 1e-5
     rope_base: float = 10000.0
     bf16: bool = False
+    qk_norm: bool = False          # Llama: RMSNorm of every query and key head before the rotation
+    rope_sections: tuple = ()      # rotated pairs per position axis; empty: one axis
+    rope_interleaved: bool = False
 
     def __post_init__(self):
         if self.n_kv_heads == 0:
@@ -116,6 +124,9 @@ def layout(cfg: ModelConfig) -> list[Entry]:
             p = f"h{l}."
             add(p + "norm1.g", (d,), GAIN, l)
             add(p + "wqkv", ((H + 2 * Hkv) * dh, d), MATRIX, l)
+            if cfg.qk_norm:
+                add(p + "qnorm.g", (dh,), GAIN, l)
+                add(p + "knorm.g", (dh,), GAIN, l)
             add(p + "wo", (d, H * dh), MATRIX, l)
             add(p + "norm2.g", (d,), GAIN, l)
             add(p + "wgu", (2 * F, d), MATRIX, l)
@@ -199,6 +210,33 @@ def rope_tables(S, dh, base):
     return np.cos(ang), np.sin(ang)
 
 
+def axis_of_pairs(cfg: ModelConfig) -> np.ndarray:
+    """Position axis of each rotated pair: the sections one after the other or,
+    interleaved over n axes, every n-th pair from pair a on for axis a >= 1 (as
+    many as its section) and all other pairs for axis 0."""
+    half = cfg.head_dim // 2
+    n = len(cfg.rope_sections)
+    if n < 2:
+        return np.zeros(half, dtype=np.int64)
+    assert sum(cfg.rope_sections) == half
+    if not cfg.rope_interleaved:
+        return np.repeat(np.arange(n), cfg.rope_sections)
+    axis = np.zeros(half, dtype=np.int64)
+    for a in range(1, n):
+        axis[a::n][:cfg.rope_sections[a]] = a
+    assert all((axis == a).sum() == s for a, s in enumerate(cfg.rope_sections))
+    return axis
+
+
+def rope_tables_at(cfg: ModelConfig, positions):
+    """cos and sin [B, 1, S, dh/2] for positions [axes, B, S]."""
+    half = cfg.head_dim // 2
+    inv = cfg.rope_base ** (-np.arange(half, dtype=np.float64) * 2.0 / cfg.head_dim)
+    pos = np.moveaxis(np.asarray(positions, dtype=np.float64)[axis_of_pairs(cfg)], 0, -1)
+    ang = (pos * inv)[:, None]
+    return np.cos(ang), np.sin(ang)
+
+
 def rope_apply(x, cos, sin, inverse=False):
     """Rotate-half RoPE on x[..., S, dh]; ``inverse`` applies the transpose."""
     half = x.shape[-1] // 2
@@ -245,7 +283,7 @@ IGNORE = -100   # label of positions that carry no target (padding, prompt)
 
 
 def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
-                  want_grad: bool = True, labels=None):
+                  want_grad: bool = True, labels=None, positions=None):
     """Mean next-token cross-entropy L(theta) and its gradient (float64).
 
     ``theta`` is the flat parameter vector (any float dtype; used in float64),
@@ -255,6 +293,8 @@ def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
     padding positions carry the label -100) it is labels[:, t + 1], and
     positions whose label is -100 are left out of the mean.  The mean is over
     the remaining targets (zero loss and gradient when there are none).
+    ``positions`` (Llama family, int [axes, B, S]) are the rotation's positions;
+    without them every axis has 0 .. S - 1.
     Returns (L, grad) with grad float64 of length P.
     """
     theta = np.asarray(theta, dtype=np.float64)
@@ -270,7 +310,7 @@ def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
         x = W["wte"][tok] + W["wpe"][:S][None, :, :]
     else:
         x = W["embed"][tok].copy()
-        cos, sin = rope_tables(S, dh, cfg.rope_base)
+        cos, sin = rope_tables(S, dh, cfg.rope_base) if positions is None else rope_tables_at(cfg, positions)
     caches = []
     for l in range(cfg.n_layers):
         p = f"h{l}."
@@ -285,6 +325,9 @@ def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
         q = qkv[..., :H * dh].reshape(B, S, H, dh).transpose(0, 2, 1, 3)
         k = qkv[..., H * dh:(H + Hkv) * dh].reshape(B, S, Hkv, dh).transpose(0, 2, 1, 3)
         v = qkv[..., (H + Hkv) * dh:].reshape(B, S, Hkv, dh).transpose(0, 2, 1, 3)
+        if cfg.qk_norm:
+            q, c["qn"] = rmsnorm_fwd(q, W[p + "qnorm.g"], eps)
+            k, c["kn"] = rmsnorm_fwd(k, W[p + "knorm.g"], eps)
         if not gpt2:
             q = rope_apply(q, cos, sin)
             k = rope_apply(k, cos, sin)
@@ -394,6 +437,9 @@ def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
         if not gpt2:
             dq = rope_apply(dq, cos, sin, inverse=True)
             dk = rope_apply(dk, cos, sin, inverse=True)
+        if cfg.qk_norm:
+            dq, g[p + "qnorm.g"] = rmsnorm_bwd(dq, W[p + "qnorm.g"], c["qn"])
+            dk, g[p + "knorm.g"] = rmsnorm_bwd(dk, W[p + "knorm.g"], c["kn"])
         dqkv = np.concatenate([
             dq.transpose(0, 2, 1, 3).reshape(B, S, H * dh),
             dk.transpose(0, 2, 1, 3).reshape(B, S, Hkv * dh),
@@ -420,8 +466,8 @@ def loss_and_grad(cfg: ModelConfig, theta: np.ndarray, tokens: np.ndarray,
     return loss, grad
 
 
-def loss(cfg: ModelConfig, theta, tokens, labels=None) -> float:
-    return loss_and_grad(cfg, theta, tokens, want_grad=False, labels=labels)[0]
+def loss(cfg: ModelConfig, theta, tokens, labels=None, positions=None) -> float:
+    return loss_and_grad(cfg, theta, tokens, want_grad=False, labels=labels, positions=positions)[0]
 
 
 def num_targets(tokens, labels=None) -> int:

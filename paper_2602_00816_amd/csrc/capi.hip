@@ -53,6 +53,26 @@ const char* validate(const fdh_model_config* cfg) {
   return nullptr;
 }
 
+fdh_status validate_qk(const fdh_model_config* cfg, const fdh_qk_config* qk) {
+  if (qk->norm < 0 || qk->norm > 1 || qk->interleaved < 0 || qk->interleaved > 1 || qk->n_axes < 0 ||
+      qk->n_axes > FDH_MAX_AXES || qk->reserved != 0)
+    return FDH_ERR_INVALID_ARG;
+  if (!qk->norm && !qk->n_axes) return FDH_OK;
+  if (cfg->family != FDH_FAMILY_LLAMA) return FDH_ERR_UNSUPPORTED;
+  const int half = cfg->d_model / cfg->n_heads / 2;
+  if (2 * half > fdh::QK_MAX_DH) return FDH_ERR_UNSUPPORTED;
+  if (!qk->n_axes) return FDH_OK;
+  int64_t sum = 0;
+  for (int a = 0; a < qk->n_axes; ++a) {
+    const int64_t s = qk->sections[a];
+    if (s < 0 || s > half) return FDH_ERR_INVALID_ARG;
+    // the last pair of axis a when interleaved
+    if (qk->interleaved && a > 0 && s > 0 && a + qk->n_axes * (s - 1) >= half) return FDH_ERR_INVALID_ARG;
+    sum += s;
+  }
+  return sum == half ? FDH_OK : FDH_ERR_INVALID_ARG;
+}
+
 }  // namespace
 
 extern "C" {
@@ -60,13 +80,21 @@ extern "C" {
 int32_t fdh_api_version(void) { return FDH_API_VERSION; }
 
 fdh_status fdh_create(const fdh_model_config* cfg, void* hip_stream, fdh_ctx** out) {
+  return fdh_create_qk(cfg, nullptr, hip_stream, out);
+}
+
+fdh_status fdh_create_qk(const fdh_model_config* cfg, const fdh_qk_config* qk, void* hip_stream, fdh_ctx** out) {
   if (!out) return FDH_ERR_INVALID_ARG;
   *out = nullptr;
   if (validate(cfg)) return FDH_ERR_INVALID_ARG;
+  const fdh_qk_config plain{};
+  if (!qk) qk = &plain;
+  const fdh_status q = validate_qk(cfg, qk);
+  if (q != FDH_OK) return q;
   fdh_ctx* c = new (std::nothrow) fdh_ctx;
   if (!c) return FDH_ERR_INVALID_ARG;
   try {
-    c->eng = new fdh::Engine(*cfg, (hipStream_t)hip_stream);
+    c->eng = new fdh::Engine(*cfg, *qk, (hipStream_t)hip_stream);
   } catch (...) {
     delete c;
     return FDH_ERR_INVALID_ARG;
@@ -177,16 +205,46 @@ fdh_status fdh_bind(fdh_ctx* ctx, const void* params_dev, const int32_t* tokens_
 
 fdh_status fdh_bind_dataset(fdh_ctx* ctx, const void* params_dev, const fdh_batch* batches, int32_t nbatch, double eps,
                             int32_t reduction, int64_t* n_targets) {
+  return fdh_bind_dataset_positions(ctx, params_dev, batches, nullptr, nbatch, eps, reduction, n_targets);
+}
+
+fdh_status fdh_bind_dataset_positions(fdh_ctx* ctx, const void* params_dev, const fdh_batch* batches,
+                                      const int32_t* const* positions, int32_t nbatch, double eps, int32_t reduction,
+                                      int64_t* n_targets) {
   return run(ctx, [&](fdh::Engine& e) -> int {
     if (nbatch < 0 || (nbatch > 0 && !batches)) { e.err = "bad batch list"; return FDH_ERR_INVALID_ARG; }
     std::vector<fdh::BatchRef> bt((size_t)nbatch);
     for (int i = 0; i < nbatch; ++i) {
       bt[i].tok = batches[i].tokens;
       bt[i].lab = batches[i].labels;
+      bt[i].pos = positions ? positions[i] : nullptr;
       bt[i].B = batches[i].B;
       bt[i].S = batches[i].S;
     }
     return e.bind_batches(params_dev, bt.data(), nbatch, eps, reduction, n_targets);
+  });
+}
+
+fdh_status fdh_qk_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes) {
+  if (!ctx || !ctx->eng || !bytes || B < 0 || S < 0) return FDH_ERR_INVALID_ARG;
+  const fdh::Engine& e = *ctx->eng;
+  if (!e.llama || e.dh > fdh::QK_MAX_DH || (int64_t)B * S > INT32_MAX) return FDH_ERR_UNSUPPORTED;
+  *bytes = e.qk_norm ? fdh::qk_scratch_bytes((int64_t)B * S, e.Hq, e.Hk, e.dh) : 0;
+  return FDH_OK;
+}
+
+fdh_status fdh_qk_forward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_t* positions_dev, int32_t B, int32_t S,
+                          const void* x_m, const void* x_d, int64_t ldx, void* y_m, void* y_d, int64_t ldy) {
+  return run(ctx, [&](fdh::Engine& e) { return e.qk_forward(gains, positions_dev, B, S, x_m, x_d, ldx, y_m, y_d, ldy); });
+}
+
+fdh_status fdh_qk_backward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_t* positions_dev, int32_t B, int32_t S,
+                           const void* x_m, const void* x_d, int64_t ldx, const float* dy_m, const float* dy_d,
+                           int64_t lddy, void* dx_m, void* dx_d, int64_t lddx, float* dgq, float* dgk,
+                           int32_t accumulate, void* scratch, size_t scratch_bytes) {
+  return run(ctx, [&](fdh::Engine& e) {
+    return e.qk_backward(gains, positions_dev, B, S, x_m, x_d, ldx, dy_m, dy_d, lddy, dx_m, dx_d, lddx, dgq, dgk,
+                         accumulate != 0, scratch, scratch_bytes);
   });
 }
 

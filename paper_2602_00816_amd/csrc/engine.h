@@ -17,7 +17,7 @@ struct ParamRef {
 };
 
 struct LayerRefs {
-  ParamRef n1g, n1b, wqkv, bqkv, wo, bo, n2g, n2b, w1, b1, w2, b2;
+  ParamRef n1g, n1b, wqkv, bqkv, qng, kng, wo, bo, n2g, n2b, w1, b1, w2, b2;
 };
 
 struct Entry {
@@ -29,6 +29,7 @@ struct Entry {
 struct BatchRef {  // one token batch of a bound dataset (device pointers, caller-owned)
   const int32_t* tok = nullptr;
   const int32_t* lab = nullptr;  // nullptr: next-token targets
+  const int32_t* pos = nullptr;  // [axes][B][S] rotation positions; nullptr: 0 .. S - 1 on every axis
   int B = 0, S = 0;
 };
 
@@ -66,7 +67,8 @@ int ritz_diagnostics(const double* alpha, const double* beta, int s, double tol,
 // the buffers in use.
 struct WsLayout {
   struct LayerSpans {
-    Span x_in_m, x_in_d, a_m, a_d, qkv_m, qkv_d, P_m, P_d, st, o_m, o_d, xmid_m, xmid_d, b_m, b_d, u_m, u_d, z_m, z_d;
+    // (qr: the q/k/v projection before a per-head norm)
+    Span x_in_m, x_in_d, a_m, a_d, qr_m, qr_d, qkv_m, qkv_d, P_m, P_d, st, o_m, o_d, xmid_m, xmid_d, b_m, b_d, u_m, u_d, z_m, z_d;
   };
   std::vector<LayerSpans> ls;
   Span xL_m, xL_d, f_m, f_d, lo, sc_m, sc_d, log_m, log_d, dlog_m, dlog_d, rowloss, losses;
@@ -92,10 +94,14 @@ struct WsLayout {
 
 class Engine : public WsLayout {
  public:
-  explicit Engine(const fdh_model_config& cfg, hipStream_t stream);
+  // qk: per-head norm and position axes of a Llama model (already validated)
+  Engine(const fdh_model_config& cfg, const fdh_qk_config& qk, hipStream_t stream);
 
   // configuration
   fdh_model_config cfg;
+  bool qk_norm = false;
+  int n_axes = 1;
+  QkRotary rot{};   // angles of the position rotation (Llama, head_dim <= QK_MAX_DH)
   hipStream_t stream;
   bool gpt2 = false, llama = false, quad = false, bf16 = false;
   int L = 0, d = 0, Hq = 0, Hk = 0, dh = 0, F = 0, V = 0, Smax = 0, qkvd = 0;
@@ -148,6 +154,13 @@ class Engine : public WsLayout {
   int block_diagonal(const float* v, double* out);
   int cg_solve(const float* b, double lam, int max_iters, double rel_tol, float* x, double* res, int* steps);
   int set_basis_offload(int device_rows, void* host, size_t bytes);
+  // the q/k front of a layer on caller-owned pairs (fdh_qk_forward, fdh_qk_backward)
+  int qk_check(const fdh_qk_gains* g, int B, int S, QkArgs* a);
+  int qk_forward(const fdh_qk_gains* g, const int32_t* pos, int B, int S, const void* x_m, const void* x_d, int64_t ldx,
+                 void* y_m, void* y_d, int64_t ldy);
+  int qk_backward(const fdh_qk_gains* g, const int32_t* pos, int B, int S, const void* x_m, const void* x_d, int64_t ldx,
+                  const float* dy_m, const float* dy_d, int64_t lddy, void* dx_m, void* dx_d, int64_t lddx, float* dgq,
+                  float* dgk, bool acc, void* scratch, size_t scratch_bytes);
   std::vector<int64_t> layer_ranges() const;
 
  private:
@@ -158,8 +171,7 @@ class Engine : public WsLayout {
   int check_batch(const int32_t* tok, int B, int S);
   int finish_checked(const float* hv);
   template <typename T>
-  int hvp_t(const T* th, const float* v, double eps, const int32_t* tok, const int32_t* lab, int B, int S, double inv_n,
-            bool acc, float* hv);
+  int hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, double inv_n, bool acc, float* hv);
   template <typename B> int lanczos_t(int m, uint64_t seed, const fdh_lanczos_opts& o, double* alpha, double* beta, int* steps);
   template <typename T> void* wsp(const Span& s) const { return (void*)(ws + s.off); }
 

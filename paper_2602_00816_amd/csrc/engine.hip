@@ -57,7 +57,7 @@ constexpr int MAX_TOKENS = 16384;   // of one batch (a plan's largest B and S ma
 
 }  // namespace
 
-Engine::Engine(const fdh_model_config& c, hipStream_t s) : cfg(c), stream(s) {
+Engine::Engine(const fdh_model_config& c, const fdh_qk_config& qk, hipStream_t s) : cfg(c), stream(s) {
   quad = cfg.family == FDH_FAMILY_QUAD_DIAG;
   gpt2 = cfg.family == FDH_FAMILY_GPT2;
   llama = cfg.family == FDH_FAMILY_LLAMA;
@@ -76,6 +76,16 @@ Engine::Engine(const fdh_model_config& c, hipStream_t s) : cfg(c), stream(s) {
   V = cfg.vocab;
   Smax = cfg.max_seq;
   qkvd = (Hq + 2 * Hk) * dh;
+  qk_norm = qk.norm != 0;
+  n_axes = std::max(1, qk.n_axes);
+  if (llama && dh <= QK_MAX_DH) {
+    for (int i = 0; i < dh / 2; ++i)
+      rot.freq[i] = std::pow((double)c.rope_base, -2.0 * i / dh) / 6.283185307179586476925;
+    // axis of each pair: section after section or, interleaved, pairs a,
+    // a + n, ... for axis a >= 1 and the others for axis 0
+    for (int a = 1, i = qk.sections[0]; a < n_axes; ++a)
+      for (int j = 0; j < qk.sections[a]; ++j, ++i) rot.axis[qk.interleaved ? a + n_axes * j : i] = (uint8_t)a;
+  }
   int64_t off = 0;
   auto add = [&](const std::string& name, int64_t rows, int64_t cols, int layer, int kind) {
     ParamRef r;
@@ -116,6 +126,10 @@ Engine::Engine(const fdh_model_config& c, hipStream_t s) : cfg(c), stream(s) {
       LayerRefs& R = layers[l];
       R.n1g = add(p + "norm1.g", d, 1, l, FDH_PARAM_GAIN);
       R.wqkv = add(p + "wqkv", qkvd, d, l, FDH_PARAM_MATRIX);
+      if (qk_norm) {
+        R.qng = add(p + "qnorm.g", dh, 1, l, FDH_PARAM_GAIN);
+        R.kng = add(p + "knorm.g", dh, 1, l, FDH_PARAM_GAIN);
+      }
       R.wo = add(p + "wo", d, Hq * dh, l, FDH_PARAM_MATRIX);
       R.n2g = add(p + "norm2.g", d, 1, l, FDH_PARAM_GAIN);
       R.w1 = add(p + "wgu", 2 * F, d, l, FDH_PARAM_MATRIX);
@@ -260,6 +274,7 @@ size_t Engine::plan(int B, int S, int m, const fdh_lanczos_opts* o, WsLayout* ou
     // the activations a layer's backward reads (everything but its input pair)
     auto take_acts = [&](LayerSpans& s) {
       take(s.a_m, td * ob); take(s.a_d, td * ob);
+      take(s.qr_m, qk_norm ? tq * ob : 0); take(s.qr_d, qk_norm ? tq * ob : 0);
       take(s.qkv_m, tq * ob); take(s.qkv_d, tq * ob);
       take(s.P_m, pp * ob); take(s.P_d, pp * ob);
       take(s.st, fused ? rows * 16 : 0);
@@ -303,6 +318,7 @@ size_t Engine::plan(int B, int S, int m, const fdh_lanczos_opts* o, WsLayout* ou
       const size_t rows_n = std::min<size_t>(T_, 2048), rows_b = std::min<size_t>(T_, 1024);
       size_t by = 3 * rows_n * d * 8;
       if (gpt2) by = std::max(by, std::max((size_t)bias_rows(rows_b, F) * F, (size_t)bias_rows(rows_b, qkvd) * qkvd) * 8);
+      if (qk_norm) by = std::max(by, qk_scratch_bytes((int64_t)T_, Hq, Hk, dh));
       take(W.gpart, by);
     }
     take(W.do_m, ta * ob); take(W.do_d, ta * ob);
@@ -393,7 +409,7 @@ uint64_t Engine::layout_digest() const {
   };
   auto sp = [&](const Span& x) { mix(x.off); mix(x.bytes); };
   for (const LayerSpans& s : ls)
-    for (const Span* x : {&s.x_in_m, &s.x_in_d, &s.a_m, &s.a_d, &s.qkv_m, &s.qkv_d, &s.P_m, &s.P_d, &s.st, &s.o_m,
+    for (const Span* x : {&s.x_in_m, &s.x_in_d, &s.a_m, &s.a_d, &s.qr_m, &s.qr_d, &s.qkv_m, &s.qkv_d, &s.P_m, &s.P_d, &s.st, &s.o_m,
                           &s.o_d, &s.xmid_m, &s.xmid_d, &s.b_m, &s.b_d, &s.u_m, &s.u_d, &s.z_m, &s.z_d})
       sp(*x);
   for (const Span* x : {&xL_m, &xL_d, &f_m, &f_d, &lo, &sc_m, &sc_d, &log_m, &log_d, &dlog_m, &dlog_d, &rowloss,
@@ -560,8 +576,9 @@ static int run_gemm_pair(Engine& e, GemmArgs& g0, GemmArgs& g1) {
 // acc the batch's Hv is added to hv (and its losses to the loss pair), which
 // is how several batches form the token-weighted dataset average (Algorithm 1).
 template <typename T>
-int Engine::hvp_t(const T* th, const float* v, double eps, const int32_t* tok, const int32_t* lab, int B, int S,
-                  double inv_n, bool acc, float* hv) {
+int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, double inv_n, bool acc, float* hv) {
+  const int32_t *tok = bt.tok, *lab = bt.lab;
+  const int B = bt.B, S = bt.S;
   hipStream_t st = stream;
   const int T_ = B * S;
   const float feps = (float)eps;
@@ -593,7 +610,24 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const int32_t* tok, c
   lo_for_v = nullptr;
   int* nf = (int*)(ws + nfflag.off);  // [0] v non-finite, [1] Hv non-finite, [2] token out of range
   if (!lo_ready) CK(launch_scale_cast<T>(lo, v, eps, P, st, nf));
-  if (llama) CK(launch_rope_table((double*)(ws + rope.off), S, dh, (double)cfg.rope_base, st));
+  // per-head norm or given positions: one pass over q and k with the angles
+  // formed there; otherwise the rotation by 0 .. S - 1 from a table
+  const bool qk_pass = llama && (qk_norm || bt.pos);
+  auto qk_args = [&](const LayerRefs& R) {
+    QkArgs a{};
+    a.T = T_; a.S = S; a.Hq = Hq; a.Hk = Hk; a.dh = dh;
+    a.pos = bt.pos;
+    a.ldx = a.ldy = a.lddy = qkvd;
+    if (qk_norm) {
+      a.gq = th + R.qng.off; a.gk = th + R.kng.off;
+      a.vq = v + R.qng.off; a.vk = v + R.kng.off;
+    }
+    a.eps = eps; a.neps = (double)neps;
+    a.part = (double*)(ws + gpart.off);
+    a.rot = rot;
+    return a;
+  };
+  if (llama && !qk_pass) CK(launch_rope_table((double*)(ws + rope.off), S, dh, (double)cfg.rope_base, st));
 
   // ---- linear helpers ----
   // Y = X W^T (+ bias) (+ residual R, fp32 output only) at both points; out:
@@ -743,8 +777,14 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const int32_t* tok, c
     CK(launch_norm_fwd<T>(PairT<T>{OP(s.a_m), OP(s.a_d)}, xm, xd, T_, d, ln, th + R.n1g.off, v + R.n1g.off,
                           ln ? th + R.n1b.off : nullptr, ln ? v + R.n1b.off : nullptr, eps, neps, st));
     // qkv projection
-    RC(lin_fwd(OP(s.a_m), OP(s.a_d), d, R.wqkv, R.bqkv, OP(s.qkv_m), OP(s.qkv_d), nullptr, nullptr, qkvd, OUT_OP));
-    if (llama)
+    const Span &pm = qk_norm ? s.qr_m : s.qkv_m, &pd = qk_norm ? s.qr_d : s.qkv_d;
+    RC(lin_fwd(OP(s.a_m), OP(s.a_d), d, R.wqkv, R.bqkv, OP(pm), OP(pd), nullptr, nullptr, qkvd, OUT_OP));
+    if (qk_pass) {
+      QkArgs a = qk_args(R);
+      a.x_m = OP(pm); a.x_d = OP(pd);
+      a.y_m = OP(s.qkv_m); a.y_d = OP(s.qkv_d);
+      CK(launch_qk_fwd<T>(a, st));
+    } else if (llama)
       CK(launch_rope_inplace<T>(PairT<T>{OP(s.qkv_m), OP(s.qkv_d)}, T_, S, Hq, Hk, dh, (const double*)(ws + rope.off), st));
     if (fused) {
       if constexpr (std::is_same<T, bf16_t>::value) {
@@ -1009,6 +1049,12 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const int32_t* tok, c
         qom = (T*)gm;
         qod = (T*)gd;
       }
+    } else if (qk_pass) {
+      QkArgs a = qk_args(R);
+      a.x_m = OP(s.qr_m); a.x_d = OP(s.qr_d);
+      a.dy_m = gm; a.dy_d = gd;
+      a.y_m = qom; a.y_d = qod;
+      CK(launch_qk_bwd<T>(a, qk_norm ? hv + R.qng.off : nullptr, qk_norm ? hv + R.kng.off : nullptr, acc, st));
     } else {
       CK(launch_qkv_bwd_post<T>(PairT<T>{qom, qod}, gm, gd, T_, S, Hq, Hk, dh, (const double*)(ws + rope.off), st));
     }
@@ -1066,8 +1112,12 @@ int Engine::hvp(const void* params, const float* v, double eps, const int32_t* t
   if (rc != FDH_OK) return rc;
   const double inv_n = 1.0 / ((double)B * (S - 1));
   CK(launch_fill_f32((float*)(ws + nfflag.off), 4, 0.f, stream));
-  rc = bf16 ? hvp_t<bf16_t>((const bf16_t*)params, v, eps, tok, nullptr, B, S, inv_n, false, hv)
-            : hvp_t<float>((const float*)params, v, eps, tok, nullptr, B, S, inv_n, false, hv);
+  BatchRef b;
+  b.tok = tok;
+  b.B = B;
+  b.S = S;
+  rc = bf16 ? hvp_t<bf16_t>((const bf16_t*)params, v, eps, b, inv_n, false, hv)
+            : hvp_t<float>((const float*)params, v, eps, b, inv_n, false, hv);
   if (rc != FDH_OK) return rc;
   return finish_checked(hv);
 }
@@ -1098,8 +1148,8 @@ int Engine::hvp_batches(const void* params, const float* v, double eps, const Ba
   }
   for (int i = 0; i < nb; ++i) {
     const BatchRef& b = bt[i];
-    const int rc = bf16 ? hvp_t<bf16_t>((const bf16_t*)params, v, eps, b.tok, b.lab, b.B, b.S, inv_n, i > 0, hv)
-                        : hvp_t<float>((const float*)params, v, eps, b.tok, b.lab, b.B, b.S, inv_n, i > 0, hv);
+    const int rc = bf16 ? hvp_t<bf16_t>((const bf16_t*)params, v, eps, b, inv_n, i > 0, hv)
+                        : hvp_t<float>((const float*)params, v, eps, b, inv_n, i > 0, hv);
     if (rc != FDH_OK) return rc;
   }
   return FDH_OK;
@@ -1124,6 +1174,10 @@ int Engine::bind_batches(const void* params, const BatchRef* bt, int nb, double 
   for (int i = 0; i < nb; ++i) {
     const int rc = check_batch(bt[i].tok, bt[i].B, bt[i].S);
     if (rc != FDH_OK) return rc;
+    if (bt[i].pos && (!llama || dh > QK_MAX_DH)) {
+      err = "positions need the Llama family and head_dim <= 256";
+      return FDH_ERR_UNSUPPORTED;
+    }
   }
   {
     // count the kept targets, the invalid labels and the invalid tokens on
@@ -1171,6 +1225,138 @@ int Engine::last_losses(double* lp, double* lm) {
   CK(hipStreamSynchronize(stream));
   if (lp) *lp = h[0];
   if (lm) *lm = h[1];
+  return FDH_OK;
+}
+
+// ---------------------------------------------------------------------------
+// the q/k front of a layer on caller-owned pairs
+// ---------------------------------------------------------------------------
+namespace {
+
+// rows of `width` bytes, `ld` bytes apart
+struct Region {
+  const char* p;
+  int64_t rows, ld, width;
+};
+Region flat(const void* p, int64_t bytes) { return {(const char*)p, 1, bytes, bytes}; }
+
+// whether a byte of one may lie in the other: regions of the same row stride are
+// told apart by their columns (two slices of one wide buffer do not overlap)
+bool overlap(const Region& a, const Region& b) {
+  if (!a.p || !b.p || a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0) return false;
+  const Region &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
+  const int64_t gap = hi.p - lo.p;
+  if (gap >= (lo.rows - 1) * lo.ld + lo.width) return false;
+  if (lo.ld != hi.ld) return true;
+  const int64_t c = gap % lo.ld;
+  return !(c >= lo.width && lo.ld - c >= hi.width);
+}
+
+bool any_overlap(const Region* w, int nw, const Region* r, int nr) {
+  for (int i = 0; i < nw; ++i) {
+    for (int j = i + 1; j < nw; ++j)
+      if (overlap(w[i], w[j])) return true;
+    for (int j = 0; j < nr; ++j)
+      if (overlap(w[i], r[j])) return true;
+  }
+  return false;
+}
+
+// a [rows][ld] operand of `size`-byte elements: 16-byte accesses and row offsets in 64 bits
+bool bad_rows(const void* p, int64_t ld, int64_t cols, int size) {
+  return !p || (uintptr_t)p % 16 || ld < cols || ld > ((int64_t)1 << 31) || ld * size % 16;
+}
+
+}  // namespace
+
+// the shape and gains of a call, shared by both directions
+int Engine::qk_check(const fdh_qk_gains* g, int B, int S, QkArgs* a) {
+  if (!llama) { err = "needs a Llama-family context"; return FDH_ERR_UNSUPPORTED; }
+  if (dh > QK_MAX_DH) { err = "head_dim must be <= 256"; return FDH_ERR_UNSUPPORTED; }
+  if (B < 0 || S < 0) { err = "B and S must not be negative"; return FDH_ERR_INVALID_ARG; }
+  if ((int64_t)B * S > INT32_MAX) { err = "B*S must be < 2^31"; return FDH_ERR_UNSUPPORTED; }
+  if (qk_norm) {
+    if (!g || !g->q || !g->k) { err = "this context norms its heads: gains are required"; return FDH_ERR_INVALID_ARG; }
+    if (!(g->eps > 0.0) || !std::isfinite(g->eps)) { err = "eps must be positive and finite"; return FDH_ERR_INVALID_ARG; }
+    a->gq = g->q; a->gk = g->k;
+    a->vq = g->v_q; a->vk = g->v_k;
+    a->eps = g->eps;
+  } else if (g) {
+    err = "this context does not norm its heads: gains must be null";
+    return FDH_ERR_INVALID_ARG;
+  }
+  a->T = B * S; a->S = S; a->Hq = Hq; a->Hk = Hk; a->dh = dh;
+  a->neps = (double)cfg.norm_eps;
+  a->rot = rot;
+  return FDH_OK;
+}
+
+int Engine::qk_forward(const fdh_qk_gains* g, const int32_t* pos, int B, int S, const void* x_m, const void* x_d, int64_t ldx,
+                       void* y_m, void* y_d, int64_t ldy) {
+  QkArgs a{};
+  const int rc = qk_check(g, B, S, &a);
+  if (rc != FDH_OK) return rc;
+  if (a.T == 0) return FDH_OK;
+  const int ob = bf16 ? 2 : 4;
+  if (bad_rows(x_m, ldx, qkvd, ob) || bad_rows(x_d, ldx, qkvd, ob) || bad_rows(y_m, ldy, qkvd, ob) || bad_rows(y_d, ldy, qkvd, ob)) {
+    err = "x and y: 16-byte aligned rows, at least (n_heads + 2 n_kv_heads) head_dim elements apart";
+    return FDH_ERR_INVALID_ARG;
+  }
+  const int64_t T_ = a.T, wd = (int64_t)qkvd * ob, gb = (int64_t)dh * ob, vb = (int64_t)dh * 4;
+  const bool same = x_m == y_m && x_d == y_d && ldx == ldy;
+  const Region xm{(const char*)x_m, T_, ldx * ob, wd}, xd{(const char*)x_d, T_, ldx * ob, wd};
+  const Region w[2] = {{(const char*)y_m, T_, ldy * ob, wd}, {(const char*)y_d, T_, ldy * ob, wd}};
+  const Region none = flat(nullptr, 0);
+  const Region r[7] = {same ? none : xm, same ? none : xd, flat(pos, 4 * n_axes * T_), flat(a.gq, gb), flat(a.gk, gb),
+                       flat(a.vq, vb), flat(a.vk, vb)};
+  if (any_overlap(w, 2, r, 7)) { err = "y overlaps an input (only y = x with the same row stride may) or itself"; return FDH_ERR_INVALID_ARG; }
+  a.pos = pos;
+  a.x_m = x_m; a.x_d = x_d; a.ldx = ldx;
+  a.y_m = y_m; a.y_d = y_d; a.ldy = ldy;
+  if (bf16) CK(launch_qk_fwd<bf16_t>(a, stream));
+  else CK(launch_qk_fwd<float>(a, stream));
+  return FDH_OK;
+}
+
+int Engine::qk_backward(const fdh_qk_gains* g, const int32_t* pos, int B, int S, const void* x_m, const void* x_d,
+                        int64_t ldx, const float* dy_m, const float* dy_d, int64_t lddy, void* dx_m, void* dx_d,
+                        int64_t lddx, float* dgq, float* dgk, bool acc, void* scratch, size_t scratch_bytes) {
+  QkArgs a{};
+  const int rc = qk_check(g, B, S, &a);
+  if (rc != FDH_OK) return rc;
+  const int ob = bf16 ? 2 : 4;
+  const int64_t T_ = a.T, wd = (int64_t)qkvd * ob, gb = (int64_t)dh * ob, vb = (int64_t)dh * 4;
+  size_t need = 0;
+  if (qk_norm) {
+    need = qk_scratch_bytes(T_, Hq, Hk, dh);
+    if (!dgq || !dgk) { err = "null gain gradient"; return FDH_ERR_INVALID_ARG; }
+    if (need && (!scratch || scratch_bytes < need)) { err = "scratch smaller than fdh_qk_scratch_bytes"; return FDH_ERR_WORKSPACE; }
+    if (need && (uintptr_t)scratch % 16) { err = "scratch must be 16-byte aligned"; return FDH_ERR_WORKSPACE; }
+  } else if (dgq || dgk) {
+    err = "this context does not norm its heads: gain gradients must be null";
+    return FDH_ERR_INVALID_ARG;
+  }
+  if (T_ > 0 && (bad_rows(dy_m, lddy, qkvd, 4) || bad_rows(dy_d, lddy, qkvd, 4) || bad_rows(dx_m, lddx, qkvd, ob) ||
+                 bad_rows(dx_d, lddx, qkvd, ob) || (qk_norm && (bad_rows(x_m, ldx, qkvd, ob) || bad_rows(x_d, ldx, qkvd, ob))))) {
+    err = "x, dy and dx: 16-byte aligned rows, at least (n_heads + 2 n_kv_heads) head_dim elements apart";
+    return FDH_ERR_INVALID_ARG;
+  }
+  const Region none = flat(nullptr, 0);
+  const Region w[5] = {{(const char*)dx_m, T_, lddx * ob, wd}, {(const char*)dx_d, T_, lddx * ob, wd}, flat(dgq, vb),
+                       flat(dgk, vb), need ? flat(scratch, (int64_t)need) : none};
+  const Region r[9] = {qk_norm ? Region{(const char*)x_m, T_, ldx * ob, wd} : none,
+                       qk_norm ? Region{(const char*)x_d, T_, ldx * ob, wd} : none,
+                       {(const char*)dy_m, T_, lddy * 4, (int64_t)qkvd * 4},
+                       {(const char*)dy_d, T_, lddy * 4, (int64_t)qkvd * 4},
+                       flat(pos, 4 * n_axes * T_), flat(a.gq, gb), flat(a.gk, gb), flat(a.vq, vb), flat(a.vk, vb)};
+  if (any_overlap(w, 5, r, 9)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }
+  a.pos = pos;
+  a.x_m = x_m; a.x_d = x_d; a.ldx = ldx;
+  a.dy_m = dy_m; a.dy_d = dy_d; a.lddy = lddy;
+  a.y_m = dx_m; a.y_d = dx_d; a.ldy = lddx;
+  a.part = (double*)scratch;
+  if (bf16) CK(launch_qk_bwd<bf16_t>(a, dgq, dgk, acc, stream));
+  else CK(launch_qk_bwd<float>(a, dgq, dgk, acc, stream));
   return FDH_OK;
 }
 

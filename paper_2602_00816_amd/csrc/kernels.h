@@ -175,6 +175,47 @@ hipError_t launch_qkv_bwd_post(PairT<T> out, float* gm, float* gd, int T_, int S
 // rope table: cs[s*dh + 2i] = cos(s * base^(-2i/dh)), cs[s*dh + 2i + 1] = sin(...)
 hipError_t launch_rope_table(double* cs, int S, int dh, double base, hipStream_t s);
 
+// ---- qk.hip: per-head norm and position rotation of the q and k columns ----------
+constexpr int QK_MAX_DH = 256;
+// most workgroups per segment (queries, keys) that leave a row of gain sums in the backward
+constexpr int QK_BWD_BLOCKS = 1024;
+// pair i of a head (elements i, i + dh/2) turns by 2 pi freq[i] pos[axis[i]]
+struct QkRotary {
+  double freq[QK_MAX_DH / 2];    // turns per position: base^(-2i/dh) / (2 pi)
+  uint8_t axis[QK_MAX_DH / 2];
+};
+struct QkArgs {
+  int T, S, Hq, Hk, dh;          // tokens; without pos token t has position t % S
+  const int32_t* pos;            // [axes][T] or null
+  const void *x_m, *x_d;         // [T][ldx] q, k, v columns, operand type (backward without gains: unused)
+  int64_t ldx;
+  void *y_m, *y_d;               // [T][ldy] output (backward: dx), operand type
+  int64_t ldy;
+  const float *dy_m, *dy_d;      // backward: [T][lddy] output gradient
+  int64_t lddy;
+  const void *gq, *gk;           // gains [dh], operand type; null: no norm
+  const float *vq, *vk;          // their directions (null: the same gains at both points)
+  double eps, neps;
+  double* part;                  // backward with gains: qk_scratch_bytes
+  double inv_n;                  // set by the launchers
+  QkRotary rot;
+};
+// how a launch is split: per segment units of 64 / G heads per token, units per
+// wavefront, workgroups; then the workgroups that move the value columns
+struct QkSplit {
+  int chunks[2], per[2], blocks[2], vblocks;
+};
+// bytes of part for up to T_ tokens
+size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh);
+// y = rotated (normed) q and k columns of x, v columns copied unless y is x
+// (in place: the same pointers and row strides)
+template <typename T>
+hipError_t launch_qk_fwd(QkArgs a, hipStream_t s);
+// dx from dy (all columns) and, with gains, dgq/dgk (+)= 1/eps times the half
+// difference of the gain gradients (float32 [dh])
+template <typename T>
+hipError_t launch_qk_bwd(QkArgs a, float* dgq, float* dgk, bool acc, hipStream_t s);
+
 // causal softmax at both points: rows of S scores (fp32 pairs, already scaled) -> P (operand type)
 template <typename T>
 hipError_t launch_attn_softmax(PairT<T> P, const float* Sm, const float* Sd, int nrows_total, int S, hipStream_t s);

@@ -40,6 +40,15 @@ class ModelConfig(C.Structure):
                 ("quad_n", C.c_int64)]
 
 
+class QkConfig(C.Structure):
+    _fields_ = [("norm", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 4), ("interleaved", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class QkGains(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v_q", C.c_void_p), ("v_k", C.c_void_p), ("eps", C.c_double)]
+
+
 class LanczosOpts(C.Structure):
     _fields_ = [("reorth", C.c_int32), ("window", C.c_int32), ("basis_dtype", C.c_int32),
                 ("breakdown_tol", C.c_float)]
@@ -70,6 +79,7 @@ def lib():
     sig = {
         "fdh_api_version": (i32, []),
         "fdh_create": (i32, [C.POINTER(ModelConfig), vp, C.POINTER(vp)]),
+        "fdh_create_qk": (i32, [C.POINTER(ModelConfig), C.POINTER(QkConfig), vp, C.POINTER(vp)]),
         "fdh_destroy": (None, [vp]),
         "fdh_num_params": (i64, [vp]),
         "fdh_num_blocks": (i32, [vp]),
@@ -85,6 +95,11 @@ def lib():
         "fdh_last_losses": (i32, [vp, pd, pd]),
         "fdh_bind": (i32, [vp, vp, vp, i32, i32, f64]),
         "fdh_bind_dataset": (i32, [vp, vp, C.POINTER(Batch), i32, f64, i32, C.POINTER(i64)]),
+        "fdh_bind_dataset_positions": (i32, [vp, vp, C.POINTER(Batch), C.POINTER(vp), i32, f64, i32, C.POINTER(i64)]),
+        "fdh_qk_scratch_bytes": (i32, [vp, i32, i32, C.POINTER(C.c_size_t)]),
+        "fdh_qk_forward": (i32, [vp, C.POINTER(QkGains), vp, i32, i32, vp, vp, i64, vp, vp, i64]),
+        "fdh_qk_backward": (i32, [vp, C.POINTER(QkGains), vp, i32, i32, vp, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp,
+                                  i32, vp, C.c_size_t]),
         "fdh_hvp_bound": (i32, [vp, vp, vp]),
         "fdh_set_basis_offload": (i32, [vp, i32, vp, C.c_size_t]),
         "fdh_lanczos": (i32, [vp, i32, u64, C.POINTER(LanczosOpts), pd, pd, pi]),
@@ -171,18 +186,33 @@ class Entry:
 
 
 class Model:
-    """One fdh_ctx: a model (or the quadratic test operator) on the current GPU."""
+    """One fdh_ctx: a model (or the quadratic test operator) on the current GPU.
+
+    Llama family: qk_norm norms every query and key head before the rotation;
+    rope_sections (rotated pairs per position axis, together head_dim / 2)
+    rotates over several axes, rope_interleaved deals the axes' pairs in turn.
+    stream: a hipStream_t (torch's ``stream.cuda_stream``); None is the default
+    stream."""
 
     def __init__(self, family: str, n_layers=0, d_model=0, n_heads=1, n_kv_heads=0, d_ff=0, vocab=0,
-                 max_seq=0, dtype="f32", norm_eps=1e-5, rope_base=10000.0, quad_n=0, stream=None):
+                 max_seq=0, dtype="f32", norm_eps=1e-5, rope_base=10000.0, quad_n=0, stream=None, qk_norm=False,
+                 rope_sections=None, rope_interleaved=False):
         self._L = lib()
         self.cfg = ModelConfig(FAMILY[family], n_layers, d_model, n_heads, n_kv_heads or n_heads, d_ff, vocab,
                                max_seq, DTYPE[dtype], norm_eps, rope_base, 0, quad_n)
         self.family, self.dtype = family, dtype
         h = C.c_void_p()
-        st = self._L.fdh_create(C.byref(self.cfg), stream if stream is not None else C.c_void_p(0), C.byref(h))
+        sec = [] if rope_sections is None else [int(s) for s in rope_sections]
+        if len(sec) > 4:
+            raise ValueError("rope_sections: at most 4 axes")
+        qk = QkConfig(int(bool(qk_norm)), len(sec), (C.c_int32 * 4)(*sec), int(bool(rope_interleaved)), 0)
+        st = self._L.fdh_create_qk(C.byref(self.cfg), C.byref(qk), stream if stream is not None else C.c_void_p(0),
+                                   C.byref(h))
         if st != OK:
             raise FdhError(st, "fdh_create rejected the configuration")
+        self.qk_norm, self.n_axes = bool(qk_norm), max(1, len(sec))
+        self._stream = int(getattr(stream, "value", stream) or 0)
+        self._qk_dtype = "float32" if dtype == "f32" else "bfloat16"
         self._h = h
         self._ws = None
         self._keep = []        # tensors the bound operator points to
@@ -191,7 +221,9 @@ class Model:
     @classmethod
     def from_workload(cls, w: dict, stream=None):
         return cls(w["family"], w["n_layers"], w["d_model"], w["n_heads"], w["n_kv_heads"], w["d_ff"],
-                   w["vocab"], w["max_seq"], w["dtype"], rope_base=w["rope_base"], stream=stream)
+                   w["vocab"], w["max_seq"], w["dtype"], rope_base=w["rope_base"], stream=stream,
+                   qk_norm=w.get("qk_norm", False), rope_sections=w.get("rope_sections"),
+                   rope_interleaved=w.get("rope_interleaved", False))
 
     def close(self):
         if getattr(self, "_h", None):
@@ -321,11 +353,12 @@ class Model:
         self._keep = [params, tokens]
         self._check(self._L.fdh_bind(self._h, _ptr(params), _ptr(tokens), B, S, float(eps)), "fdh_bind")
 
-    def bind_dataset(self, params, batches, eps: float, reduction: str = "mean") -> int:
+    def bind_dataset(self, params, batches, eps: float, reduction: str = "mean", positions=None) -> int:
         """Bind the token-weighted dataset operator over ``batches``: a list of
         int32 [B, S] token tensors or (tokens, labels) pairs on the device
-        (labels aligned with the tokens, -100 = no target).  Returns the number
-        of kept targets."""
+        (labels aligned with the tokens, -100 = no target).  positions (Llama
+        family): one int32 [axes, B, S] tensor or None (0 .. S - 1 on every
+        axis) per batch.  Returns the number of kept targets."""
         import torch
         self._check_params(params)
         items = [b if isinstance(b, tuple) else (b, None) for b in batches]
@@ -335,12 +368,143 @@ class Model:
                     raise ValueError("tokens and labels must be contiguous int32 [B, S] tensors on the device")
             if lab is not None and lab.shape != tok.shape:
                 raise ValueError("labels must have the shape of their tokens")
+        pos = [None] * len(items) if positions is None else list(positions)
+        if len(pos) != len(items):
+            raise ValueError("positions must have one entry per batch")
+        for p, (tok, _) in zip(pos, items):
+            if p is not None and (p.dtype != torch.int32 or not p.is_cuda or not p.is_contiguous()
+                                  or tuple(p.shape) != (self.n_axes, *tok.shape)):
+                raise ValueError(f"positions must be contiguous int32 [{self.n_axes}, B, S] tensors on the device")
+        parr = (C.c_void_p * len(items))(*[_ptr(p) for p in pos])
         arr = (Batch * len(items))(*[Batch(_ptr(t), _ptr(l), t.shape[0], t.shape[1]) for t, l in items])
         n = C.c_int64()
-        self._keep = [params] + [x for it in items for x in it if x is not None]
-        self._check(self._L.fdh_bind_dataset(self._h, _ptr(params), arr, len(items), float(eps), REDUCTION[reduction],
-                                             C.byref(n)), "fdh_bind_dataset")
+        self._keep = [params] + [x for it in items for x in it if x is not None] + [p for p in pos if p is not None]
+        if positions is None:
+            st = self._L.fdh_bind_dataset(self._h, _ptr(params), arr, len(items), float(eps), REDUCTION[reduction],
+                                          C.byref(n))
+        else:
+            st = self._L.fdh_bind_dataset_positions(self._h, _ptr(params), arr, parr, len(items), float(eps),
+                                                    REDUCTION[reduction], C.byref(n))
+        self._check(st, "fdh_bind_dataset")
         return int(n.value)
+
+    # ---- the q/k front of a layer ----
+    def _qk_pair(self, pair, what, dtype, T=None):
+        """Pointers and row stride of a pair of [T, (n_heads + 2 n_kv_heads) head_dim] tensors."""
+        m, d = pair
+        ncol = (self.cfg.n_heads + 2 * self.cfg.n_kv_heads) * (self.cfg.d_model // self.cfg.n_heads)
+        for t in (m, d):
+            if t.dim() != 2 or t.shape[1] != ncol or (T is not None and t.shape[0] != T):
+                raise ValueError(f"{what} must be two [tokens, {ncol}] tensors")
+            if str(t.dtype) != "torch." + dtype:
+                raise ValueError(f"{what} must have dtype {dtype}")
+            if t.stride(1) != 1:
+                raise ValueError(f"{what}: the elements of a row must be contiguous")
+        ld = ncol if m.shape[0] <= 1 else m.stride(0)
+        if d.shape[0] != m.shape[0] or (m.shape[0] > 1 and d.stride(0) != ld):
+            raise ValueError(f"{what}: both tensors must have the same rows and row stride")
+        self._qk_device(m, d)
+        return m.data_ptr(), d.data_ptr(), ld
+
+    def _qk_device(self, *tensors):
+        import torch
+        dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+        for t in tensors:
+            if t is not None and (not t.is_cuda or t.device.index != dev):
+                raise ValueError("tensors must lie on the current device")
+
+    def _qk_args(self, T, seq, gains, eps, positions):
+        """(gains, positions pointer, B, S) of a call; refuses a current stream that is not the context's."""
+        import torch
+        if seq < 1 or T % seq:
+            raise ValueError("seq must be positive and divide the number of tokens")
+        if T and torch.cuda.current_stream().cuda_stream != self._stream:
+            raise ValueError("the current stream is not the model's: build the model with stream=<the current stream>")
+        g = None
+        if gains is not None:
+            dh = self.cfg.d_model // self.cfg.n_heads
+            q, k, vq, vk = gains
+            for t, what, dt in ((q, "gains", self._qk_dtype), (k, "gains", self._qk_dtype), (vq, "gain directions", "float32"),
+                                (vk, "gain directions", "float32")):
+                if t is None and what != "gains":
+                    continue
+                if t is None or str(t.dtype) != "torch." + dt or t.numel() != dh or not t.is_contiguous():
+                    raise ValueError(f"{what} must be contiguous {dt} tensors of {dh} elements")
+            self._qk_device(q, k, vq, vk)
+            g = C.byref(QkGains(_ptr(q), _ptr(k), _ptr(vq), _ptr(vk), float(eps)))
+        if positions is not None:
+            if str(positions.dtype) != "torch.int32" or positions.numel() != self.n_axes * T or not positions.is_contiguous():
+                raise ValueError(f"positions must be a contiguous int32 tensor of {self.n_axes} x tokens elements")
+            self._qk_device(positions)
+        return g, _ptr(positions), T // seq, seq
+
+    def qk_scratch(self, B: int, S: int):
+        """A device buffer for qk_backward on B x S tokens (None where it needs none)."""
+        import torch
+        n = C.c_size_t()
+        self._check(self._L.fdh_qk_scratch_bytes(self._h, B, S, C.byref(n)), "fdh_qk_scratch_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device="cuda") if n.value else None
+
+    def qk_forward(self, x, seq: int, gains=None, eps: float = 1.0, positions=None, out=None):
+        """Per-head norm (with qk_norm) and rotation of the query and key columns of
+        the pair x = (mean, half difference), each [tokens, (n_heads + 2 n_kv_heads)
+        head_dim] of the model's dtype in rows of any stride; value columns are
+        copied.  tokens = B * seq.  gains = (q, k, v_q, v_k): the gains and their
+        directions (or None), taken at q +- eps v_q.  positions: int32 [axes,
+        tokens], None for 0 .. seq - 1.  out: a pair to write (x itself for in
+        place).  Enqueued on the model's stream, which must be the current one."""
+        import torch
+        xm, xd, ldx = self._qk_pair(x, "x", self._qk_dtype)
+        T = x[0].shape[0]
+        g, pos, B, S = self._qk_args(T, seq, gains, eps, positions)
+        if out is None:
+            out = tuple(torch.empty(x[0].shape, dtype=x[0].dtype, device=x[0].device) for _ in range(2))
+        ym, yd, ldy = self._qk_pair(out, "out", self._qk_dtype, T)
+        st = self._L.fdh_qk_forward(self._h, g, pos, B, S, xm, xd, ldx, ym, yd, ldy)
+        if st < 0:
+            self._check(st, "fdh_qk_forward")
+        return out
+
+    def qk_backward(self, dy, seq: int, x=None, gains=None, eps: float = 1.0, positions=None, out=None, gain_grads=None,
+                    accumulate: bool = False, scratch=None):
+        """Backward of qk_forward: dx (a pair of the model's dtype) from the float32
+        pair dy.  With qk_norm also x (the forward's input) and gains, and the
+        result is (dx, (dq, dk)) with the gains' entries of Hv, float32
+        [head_dim] (added to gain_grads with accumulate).  scratch: qk_scratch(B,
+        seq), made here if None; calls that may overlap on the device need one
+        each."""
+        import torch
+        gm, gd, lddy = self._qk_pair(dy, "dy", "float32")
+        T = dy[0].shape[0]
+        g, pos, B, S = self._qk_args(T, seq, gains, eps, positions)
+        if out is None:
+            dt = getattr(torch, self._qk_dtype)
+            out = tuple(torch.empty(dy[0].shape, dtype=dt, device=dy[0].device) for _ in range(2))
+        om, od, lddx = self._qk_pair(out, "out", self._qk_dtype, T)
+        xm = xd = ldx = 0
+        dg = (None, None)
+        if self.qk_norm:
+            if x is None:
+                raise ValueError("a model with qk_norm needs x")
+            xm, xd, ldx = self._qk_pair(x, "x", self._qk_dtype, T)
+            dh = self.cfg.d_model // self.cfg.n_heads
+            if gain_grads is None:
+                if accumulate:
+                    raise ValueError("accumulate needs gain_grads")
+                gain_grads = tuple(torch.empty(dh, device=dy[0].device) for _ in range(2))
+            dg = gain_grads
+            for t in dg:
+                if str(t.dtype) != "torch.float32" or t.numel() != dh or not t.is_contiguous():
+                    raise ValueError(f"gain_grads must be contiguous float32 tensors of {dh} elements")
+            if scratch is None:
+                scratch = self.qk_scratch(B, S)
+            self._qk_device(*dg, scratch)
+        nb = 0 if scratch is None else scratch.numel() * scratch.element_size()
+        st = self._L.fdh_qk_backward(self._h, g, pos, B, S, xm, xd, ldx, gm, gd, lddy, om, od, lddx, _ptr(dg[0]), _ptr(dg[1]),
+                                     int(accumulate), _ptr(scratch), nb)
+        if st < 0:
+            self._check(st, "fdh_qk_backward")
+        return (out, gain_grads) if self.qk_norm else out
 
     def hvp_bound(self, v, out=None):
         """H v of the bound operator (float32 [P]); enqueued on the context stream."""

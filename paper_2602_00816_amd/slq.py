@@ -2,6 +2,7 @@
 
     python -m paper_2602_00816_amd.slq --workload llama-1.3b-bf16 [--probes N] [--m M]
                                        [--eps E] [--block-diagonal] [--out FILE.json]
+                                       [--qk-norm] [--rope-sections T,H,W] [--rope-interleaved] [--grid H,W]
 
 Runs the SLQ estimate of section 4 with the workload's own settings (probe
 count, Lanczos length, reorthogonalisation mode and window, basis precision,
@@ -19,6 +20,11 @@ also forms, for a Gaussian unit direction v, the layer-block-diagonal product
 (v restricted to each layer's block, the proxy of section 6, Exp I) and
 reports its relative error and cosine against the full Hv per layer.  --out
 writes everything as JSON.
+
+A Llama workload can be given a per-head norm of queries and keys (--qk-norm) and a
+rotation over several position axes (--rope-sections: rotated pairs per axis, time
+first).  With --grid H,W the tokens of a row stand for frames of H x W patches and
+rotate at their (time, row, column); without it they are text, at 0 .. S - 1 on every axis.
 """
 from __future__ import annotations
 
@@ -50,6 +56,23 @@ def density_bins(nodes, weights, steps, nbins=40):
     return edges, mass
 
 
+def grid_positions(axes, B, S, h, w):
+    """int32 [axes, B, S]: token s of a row at (frame, row, column) of frames of h x w
+    patches (the first axes of these)."""
+    s = np.arange(S)
+    p = np.stack([s // (h * w), s // w % h, s % w][:axes]).astype(np.int32)
+    return np.ascontiguousarray(np.broadcast_to(p[:, None], (axes, B, S)))
+
+
+def _numbers(least, most, low):
+    def parse(text):
+        v = [int(x) for x in text.split(",")]
+        if not least <= len(v) <= most or min(v) < low:
+            raise argparse.ArgumentTypeError(f"takes {least} to {most} numbers from {low} up")
+        return v
+    return parse
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--workload", default="llama-1.3b-bf16", choices=sorted(WORKLOADS))
@@ -58,13 +81,26 @@ def main(argv=None):
     ap.add_argument("--eps", type=float, default=-1.0, help="finite-difference step (-1: the workload's first)")
     ap.add_argument("--seed", type=int, default=SEED_PROBE, help="probe seed")
     ap.add_argument("--block-diagonal", action="store_true", help="also the layer-block-diagonal proxy (Exp I)")
+    ap.add_argument("--qk-norm", action="store_true", help="norm every query and key head before the rotation (Llama)")
+    ap.add_argument("--rope-sections", type=_numbers(1, 3, 0), help="rotated pairs per position axis (Llama): time, height, width")
+    ap.add_argument("--rope-interleaved", action="store_true", help="deal the axes' pairs in turn")
+    ap.add_argument("--grid", type=_numbers(2, 2, 1), help="H,W: frames of H x W patches give the positions")
     ap.add_argument("--out", default="", help="write the results as JSON")
     args = ap.parse_args(argv)
+
+    w = dict(WORKLOADS[args.workload])
+    if (args.qk_norm or args.rope_sections or args.rope_interleaved or args.grid) and w["family"] != "llama":
+        ap.error("--qk-norm, --rope-sections, --rope-interleaved and --grid need a Llama workload")
+    if (args.grid or args.rope_interleaved) and not args.rope_sections:
+        ap.error("--grid and --rope-interleaved need --rope-sections")
+    half = w["d_model"] // w["n_heads"] // 2
+    if args.rope_sections and sum(args.rope_sections) != half:
+        ap.error(f"--rope-sections must add up to {half} pairs")
+    w.update(qk_norm=args.qk_norm, rope_sections=args.rope_sections, rope_interleaved=args.rope_interleaved)
 
     import torch
     from paper_2602_00816_amd import fdhvp as fd
 
-    w = WORKLOADS[args.workload]
     probes = w["probes"] if args.probes < 0 else args.probes
     m = w["m"] if args.m < 0 else args.m
     eps = w["eps"][0] if args.eps < 0 else args.eps
@@ -79,7 +115,11 @@ def main(argv=None):
     ws = mod.set_workspace(B, S, m, o)
     params = mod.init_params(SEED_PARAMS)
     tok = mod.make_tokens(B, S, SEED_TOKENS, w["token_dist"])
-    mod.bind(params, tok, eps)
+    if args.grid:
+        pos = torch.from_numpy(grid_positions(len(args.rope_sections), B, S, *args.grid)).cuda()
+        mod.bind_dataset(params, [tok], eps, positions=[pos])
+    else:
+        mod.bind(params, tok, eps)
     torch.cuda.synchronize()
     say(f"{args.workload}: P = {mod.num_params}, {B}x{S} tokens, eps {eps:g}, {probes} probes x m = {m}, "
         f"reorth {w['reorth']}{' ' + str(w['window']) if w['reorth'] == 'window' else ''}, {w['basis']} basis, "
@@ -103,7 +143,9 @@ def main(argv=None):
     say("density (bin centre, mass): " + ", ".join(f"({0.5 * (edges[i] + edges[i + 1]):.3e}, {mass[i]:.3e})"
                                                    for i in range(len(mass)) if mass[i] > 0))
     out = dict(workload=args.workload, params=mod.num_params, batch=B, seq=S, eps=eps, probes=probes, m=m,
-               reorth=w["reorth"], window=w["window"], basis=w["basis"], seconds=t, lanczos_steps=n_hvp,
+               reorth=w["reorth"], window=w["window"], basis=w["basis"], qk_norm=args.qk_norm,
+               rope_sections=args.rope_sections, rope_interleaved=args.rope_interleaved, grid=args.grid,
+               seconds=t, lanczos_steps=n_hvp,
                iters_per_min=60.0 * n_hvp / t, trace_estimate=trace, status=st, per_probe=per_probe,
                nodes=[nodes[p, :steps[p]].tolist() for p in range(probes)],
                weights=[weights[p, :steps[p]].tolist() for p in range(probes)],

@@ -1,0 +1,225 @@
+"""HVPs of Llama models with a per-head norm of queries and keys and with given
+positions against the oracle: relative L2 <= 5e-3 in fp32 (every parameter block on
+its own) and <= 5e-2 in bf16, as the other parity tests; all attention paths,
+recomputation, datasets, Lanczos, and what must not change."""
+import numpy as np
+import pytest
+
+import synth
+from oracle import hvp as OH
+from oracle import lanczos as OL
+from oracle import model as M
+from tests.gpu_util import need_gpu, rel_l2, say, upload_params
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-3
+SMALL = dict(family="llama", n_layers=2, d_model=96, n_heads=6, n_kv_heads=2, d_ff=200, vocab=264, max_seq=40, rope_base=10000.0)
+W64 = dict(family="llama", n_layers=2, d_model=256, n_heads=4, n_kv_heads=2, d_ff=256, vocab=264, max_seq=256, rope_base=10000.0)
+W128 = dict(family="llama", n_layers=2, d_model=256, n_heads=2, n_kv_heads=1, d_ff=256, vocab=264, max_seq=256, rope_base=10000.0)
+
+
+def _cfg(w):
+    return M.ModelConfig(w["family"], w["n_layers"], w["d_model"], w["n_heads"], w["d_ff"], w["vocab"], w["max_seq"],
+                         n_kv_heads=w["n_kv_heads"], rope_base=w["rope_base"], bf16=w["dtype"] == "bf16",
+                         qk_norm=w.get("qk_norm", False), rope_sections=tuple(w.get("rope_sections") or ()),
+                         rope_interleaved=w.get("rope_interleaved", False))
+
+
+def _theta(cfg, std=0.05):
+    theta = synth.init_params(M.init_ranges(cfg), M.num_params(cfg), 1, std=std, bf16=cfg.bf16)
+    for e in M.layout(cfg):
+        if e.kind == M.GAIN:     # gains away from one, so that their curvature counts
+            g = theta[e.offset:e.offset + e.numel] + (0.2 * synth.normal(17, 1, e.offset, e.numel)).astype(np.float32)
+            theta[e.offset:e.offset + e.numel] = synth.bf16_round(g) if cfg.bf16 else g
+    return theta
+
+
+def _positions(axes, B, S, seed=3, far=200):
+    """Image-like positions: rows and columns of patches from a start of each batch row's own."""
+    rng = np.random.default_rng(seed)
+    s = rng.integers(0, far, (B, 1))
+    i = np.arange(S)
+    grid = [i // 16, i // 4 % 4, i % 4, i][:axes] if axes > 1 else [i]
+    return np.stack([s + g for g in grid]).astype(np.int32)
+
+
+def _run(torch, fd, w, theta, batches, v, unfused=False, recompute=False, B=None, S=None):
+    mod = fd.Model.from_workload(w)
+    if unfused:
+        mod.unfused_attention(True)
+    mod.set_recompute(recompute)
+    mod.set_workspace(B or max(t.shape[0] for t, _, _ in batches), S or max(t.shape[1] for t, _, _ in batches))
+    th = upload_params(torch, theta, w["dtype"])
+    dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    items = [(dev(t), dev(l)) if l is not None else dev(t) for t, l, _ in batches]
+    mod.bind_dataset(th, items, EPS, positions=[dev(p) for _, _, p in batches])
+    hv = mod.hvp_bound(torch.from_numpy(v.astype(np.float32)).cuda()).cpu().numpy()
+    return hv, mod.last_losses(), mod, th
+
+
+@pytest.mark.parametrize("shape,dtype,B,S,unfused", [
+    (SMALL, "f32", 2, 40, False), (SMALL, "bf16", 2, 40, False), (W64, "bf16", 1, 128, False), (W64, "bf16", 1, 128, True),
+    (W128, "bf16", 2, 72, False), (W128, "bf16", 2, 72, True), (W128, "bf16", 1, 256, False)])
+@pytest.mark.parametrize("norm,sections,inter,given", [(True, None, False, False), (True, "3", True, True),
+                                                       (False, "3", False, True), (False, None, False, True)])
+def test_hvp_matches_oracle(shape, dtype, B, S, norm, sections, inter, given, unfused):
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    half = shape["d_model"] // shape["n_heads"] // 2
+    sec = (half - 2 * (half // 3), half // 3, half // 3) if sections else None
+    w = dict(shape, dtype=dtype, qk_norm=norm, rope_sections=sec, rope_interleaved=inter)
+    cfg = _cfg(w)
+    theta = _theta(cfg)
+    tok = synth.tokens(2, B, S, w["vocab"], "zipf")
+    pos = _positions(len(sec) if sec else 1, B, S) if given else None
+    v = synth.gaussian_direction(4, theta.size).astype(np.float32)
+    got, losses, _, _ = _run(torch, fd, w, theta, [(tok, None, pos)], v, unfused)
+    want = OH.lm_hvp(cfg, theta, v.astype(np.float64), EPS, tok, positions=pos)
+    tol = 5e-3 if dtype == "f32" else 5e-2
+    err = rel_l2(got, want)
+    say(f"heads {w['n_heads']}/{w['n_kv_heads']}x{2 * half} {dtype} {B}x{S} norm={norm} axes={sec} inter={inter} "
+        f"given={given} unfused={unfused}: rel_l2 {err:.3e}")
+    assert err <= tol
+    for e in M.layout(cfg):
+        wb = want[e.offset:e.offset + e.numel]
+        eb = rel_l2(got[e.offset:e.offset + e.numel], wb) if np.linalg.norm(wb) > 1e-6 * np.linalg.norm(want) else 0.0
+        if "norm.g" in e.name and e.layer >= 0:
+            say(f"  {e.name}: {eb:.3e}")
+        if dtype == "f32":
+            assert eb <= tol, e.name
+    for s, l in zip((1, -1), losses):
+        ref = M.loss(cfg, theta.astype(np.float64) + s * EPS * v, tok, positions=pos)
+        assert abs(l - ref) <= (1e-6 if dtype == "f32" else 1e-2) * abs(ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dataset_recompute_and_lanczos(dtype):
+    """Batches of several lengths, with and without positions and labels; recomputation
+    gives the same bits; Lanczos runs on the bound operator."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    w = dict(SMALL, dtype=dtype, qk_norm=True, rope_sections=(4, 2, 2))
+    cfg = _cfg(w)
+    theta = _theta(cfg)
+    V = w["vocab"]
+    t1, t2, t3 = (synth.tokens(30 + i, B, S, V, "zipf") for i, (B, S) in enumerate([(2, 40), (1, 24), (3, 16)]))
+    l1 = t1.copy()
+    l1[0, :9] = M.IGNORE
+    batches = [(t1, l1, _positions(3, 2, 40)), (t2, None, None), (t3, None, _positions(3, 3, 16, 5))]
+    v = synth.gaussian_direction(4, theta.size).astype(np.float32)
+    got, _, mod, th = _run(torch, fd, w, theta, batches, v)
+    again = mod.hvp_bound(torch.from_numpy(v).cuda()).cpu().numpy()
+    assert np.array_equal(got, again)
+    rc, _, _, _ = _run(torch, fd, w, theta, batches, v, recompute=True)
+    assert np.array_equal(got, rc)
+    want = OH.lm_hvp_dataset(cfg, theta, v.astype(np.float64), EPS, batches)
+    err = rel_l2(got, want)
+    say(f"dataset with positions {dtype}: rel_l2 {err:.3e}")
+    assert err <= (5e-3 if dtype == "f32" else 5e-2)
+    if dtype == "f32":
+        for e in M.layout(cfg):
+            if e.kind == M.GAIN:
+                assert rel_l2(got[e.offset:e.offset + e.numel], want[e.offset:e.offset + e.numel]) <= 5e-3, e.name
+        mm = 6
+        o = fd.opts("full", 0, "f32")
+        mod.set_workspace(3, 40, mm, o)
+        a, b, s, _ = mod.lanczos(mm, 3, o)
+        q1 = synth.rademacher_probe(3, theta.size).astype(np.float64)
+        ao, bo, _ = OL.lanczos(lambda x: OH.lm_hvp_dataset(cfg, theta, x, EPS, batches), q1, mm, OL.FULL)
+        lg, lo = (np.sort(np.linalg.eigvalsh(OL.tridiag(p, q))) for p, q in ((a, b), (ao, bo)))
+        assert s == mm and abs(lg[-1] - lo[-1]) <= 1e-3 * np.abs(lo).max() and abs(lg[0] - lo[0]) <= 1e-3 * np.abs(lo).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_text_is_what_it_was(dtype):
+    """Axes without positions give the bits of the plain model; given positions
+    0 .. S - 1 give the same product up to the angles' precision (fp32 factors
+    against fp64 ones, and what the operand type's rounding makes of that)."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    w = dict(SMALL, dtype=dtype)
+    cfg = _cfg(w)
+    theta = _theta(cfg)
+    tok = synth.tokens(2, 2, 40, w["vocab"], "zipf")
+    v = synth.gaussian_direction(4, theta.size).astype(np.float32)
+    plain, lp, _, _ = _run(torch, fd, w, theta, [(tok, None, None)], v)
+    axes, la, _, _ = _run(torch, fd, dict(w, rope_sections=(3, 3, 2), rope_interleaved=True), theta, [(tok, None, None)], v)
+    assert np.array_equal(plain, axes) and lp == la
+    pos = np.broadcast_to(np.arange(40, dtype=np.int32), (1, 2, 40))
+    given, _, _, _ = _run(torch, fd, w, theta, [(tok, None, pos)], v)
+    err = rel_l2(given, plain)
+    say(f"positions 0..S-1 against none {dtype}: {err:.3e}")
+    assert err <= (1e-5 if dtype == "f32" else 2e-2)
+
+
+def test_front_as_the_layer_runs_it():
+    """Projection, norm and rotation, scores and back: the two calls around plain
+    products give the directional derivative that autograd gives in float64."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    from tests import qk_ref as R
+    hq, hk, dh, S = 4, 2, 32, 24
+    m = fd.Model("llama", 0, hq * dh, hq, hk, 8, 8, 64, "f32", qk_norm=True, rope_sections=(6, 5, 5))
+    g = torch.Generator().manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    h, W, dW = rnd(S, 64), 0.2 * rnd((hq + 2 * hk) * dh, 64), rnd((hq + 2 * hk) * dh, 64)
+    gq, gk, vq, vk = 1 + 0.2 * rnd(dh), 1 + 0.2 * rnd(dh), rnd(dh), rnd(dh)
+    pos = torch.randint(0, 40, (3, S), generator=g, dtype=torch.int32)
+    ang = R.angles(dh, 1e4, S, S, pos, (6, 5, 5))
+    eps = 1e-3
+
+    def loss(Wp, q, k):
+        y = R.front(h.double() @ Wp.T, hq, hk, dh, ang, (q, k)).view(S, hq + 2 * hk, dh).transpose(0, 1)
+        s = y[:hq] @ y[hq:hq + hk].repeat_interleave(hq // hk, 0).transpose(1, 2) / dh ** 0.5
+        return (torch.tanh(s) ** 2).sum() / 2
+
+    grads = []
+    for sg in (1, -1):
+        leaves = [(a.double() + sg * eps * b.double()).requires_grad_(True) for a, b in ((W, dW), (gq, vq), (gk, vk))]
+        grads.append(torch.autograd.grad(loss(*leaves), leaves))
+    want = [(a - b) / (2 * eps) for a, b in zip(*grads)]
+    # the same with the library between products in float64 on pairs
+    up = lambda t: t.float().cuda().contiguous()
+    x = (up(h @ W.T), up(eps * (h.double() @ dW.double().T)))
+    gains = tuple(up(t) for t in (gq, gk, vq, vk))
+    y = m.qk_forward(x, S, gains=gains, eps=eps, positions=pos.cuda())
+    dys = []
+    for sg in (1, -1):
+        p = (y[0].double() + sg * y[1].double()).cpu().requires_grad_(True)
+        z = p.view(S, hq + 2 * hk, dh).transpose(0, 1)
+        s = z[:hq] @ z[hq:hq + hk].repeat_interleave(hq // hk, 0).transpose(1, 2) / dh ** 0.5
+        dys.append(torch.autograd.grad((torch.tanh(s) ** 2).sum() / 2, p)[0])
+    dy = tuple(up(t) for t in R.as_pair(*dys))
+    dx, dg = m.qk_backward(dy, S, x=x, gains=gains, eps=eps, positions=pos.cuda())
+    hvW = dx[1].double().cpu().T @ h.double() / eps
+    for got, w, what in zip((hvW, dg[0].double().cpu(), dg[1].double().cpu()), want, ("projection", "query gain", "key gain")):
+        err = float((got - w).norm() / w.norm())
+        say(f"{what}: {err:.3e}")
+        assert err <= 1e-4      # fp32 pairs: some ten steps of 2^-24 over an eps of 1e-3
+
+
+def test_slq_command_with_norm_and_axes(monkeypatch, tmp_path):
+    """The command on a small Llama workload: its Ritz values and trace estimate
+    against the oracle's Lanczos run."""
+    need_gpu()
+    from paper_2602_00816_amd import slq
+    w = dict(SMALL, dtype="f32", batch=2, seq=40, token_dist="zipf", probes=1, m=8, reorth="full", window=0, basis="f32", eps=[EPS])
+    monkeypatch.setitem(slq.WORKLOADS, "small-llama", w)
+    got = slq.main(["--workload", "small-llama", "--qk-norm", "--rope-sections", "4,2,2", "--rope-interleaved", "--grid", "3,4",
+                    "--out", str(tmp_path / "slq.json")])
+    cfg = _cfg(dict(w, qk_norm=True, rope_sections=(4, 2, 2), rope_interleaved=True))
+    P = M.num_params(cfg)
+    assert got["params"] == P and got["rope_sections"] == [4, 2, 2] and got["grid"] == [3, 4] and got["qk_norm"]
+    theta = synth.init_params(M.init_ranges(cfg), P, slq.SEED_PARAMS, std=0.02)
+    tok = synth.tokens(slq.SEED_TOKENS, 2, 40, w["vocab"], "zipf")
+    s = np.arange(40)
+    pos = np.broadcast_to(np.stack([s // 12, s // 4 % 3, s % 4])[:, None], (3, 2, 40))
+    q1 = synth.rademacher_probe(slq.SEED_PROBE, P).astype(np.float64)
+    ao, bo, _ = OL.lanczos(lambda x: OH.lm_hvp(cfg, theta, x, EPS, tok, positions=pos), q1, w["m"], OL.FULL)
+    lo, _ = OL.ritz(ao, bo)
+    nodes = np.array(got["nodes"][0])
+    scale = np.abs(lo).max()
+    say(f"Ritz [{nodes.min():.6e}, {nodes.max():.6e}], oracle [{lo.min():.6e}, {lo.max():.6e}]")
+    assert nodes.size == w["m"] and abs(nodes.max() - lo.max()) <= 1e-3 * scale and abs(nodes.min() - lo.min()) <= 1e-3 * scale
+    assert abs(got["trace_estimate"] - P * ao[0]) <= 1e-4 * abs(P * ao[0]) + 1e-6 * scale * P
