@@ -177,8 +177,6 @@ hipError_t launch_rope_table(double* cs, int S, int dh, double base, hipStream_t
 
 // ---- qk.hip: per-head norm and position rotation of the q and k columns ----------
 constexpr int QK_MAX_DH = 256;
-// most workgroups per segment (queries, keys) that leave a row of gain sums in the backward
-constexpr int QK_BWD_BLOCKS = 1024;
 // pair i of a head (elements i, i + dh/2) turns by 2 pi freq[i] pos[axis[i]]
 struct QkRotary {
   double freq[QK_MAX_DH / 2];    // turns per position: base^(-2i/dh) / (2 pi)
@@ -197,13 +195,13 @@ struct QkArgs {
   const float *vq, *vk;          // their directions (null: the same gains at both points)
   double eps, neps;
   double* part;                  // backward with gains: qk_scratch_bytes
-  double inv_n;                  // set by the launchers
+  double inv_n;                  // set by the launchers, as is
+  bool gvec;                     // gains and directions 16-byte aligned
   QkRotary rot;
 };
-// how a launch is split: per segment units of 64 / G heads per token, units per
-// wavefront, workgroups; then the workgroups that move the value columns
+// how a launch is split: pieces of a row (queries, keys, values), tokens per step, workgroups
 struct QkSplit {
-  int chunks[2], per[2], blocks[2], vblocks;
+  int chunks[3], step, blocks;
 };
 // bytes of part for up to T_ tokens
 size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh);

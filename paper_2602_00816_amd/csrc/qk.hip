@@ -14,10 +14,11 @@
 // R turns pair i (elements i and i + n/2) by base^(-2i/n) times the token's
 // position along the axis of pair i; without a norm y = R x and dx = R^T dy.
 //
-// The sums over a head and all that is formed from them once per head are fp64
-// (no overflow or underflow; rho in place of r.d keeps the elements' arithmetic in
-// the normal range, too, up to |x| of 1e37), the elements fp32, each output rounded
-// once to its type.  A head that holds a NaN or an infinity gives NaN in
+// The sums behind r and all that is formed from them once per head are fp64, with
+// S+- = mean(x.m^2 + x.d^2) +- 2 mean(x.m x.d) + e (no overflow or underflow; rho in
+// place of r.d keeps the elements' arithmetic in the normal range, too, up to |x| of
+// 1e37); the elements, and c, whose terms are bounded by du, are fp32; the gains' sums
+// are fp64; each output is rounded once to its type.  A head that holds a NaN or an infinity gives NaN in
 // all its elements, other heads are not touched by it.
 //
 // Memory-bound: 8 bytes per bf16 element forward, 16 backward, against some 25 and 50
@@ -30,38 +31,63 @@ namespace fdh {
 
 namespace {
 
-constexpr int NT = 256, NWAVE = NT / 64;
+// threads per workgroup, most wavefronts of a launch (see "Work split")
+constexpr int FWD_NT = 256, FWD_WAVES = 32768;
+constexpr int BWD_NT = 512, BWD_WAVES = 4096;
 
 // ---- vectors of V elements ------------------------------------------------------
+// as they lie in memory (4 V or 2 V bytes), so that loads can be held in flight
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T, int V>
-__device__ inline void load(float (&x)[V], const T* p) {
-  if constexpr (sizeof(T) == 4) {
+struct Raw {
+  static constexpr int N = V * sizeof(T) / 4;
+  uint32_t w[N];
+};
+// STREAM: nontemporal accesses
+template <typename T, int V, bool STREAM = false>
+__device__ inline void load(Raw<T, V>& r, const T* p) {
+  constexpr int N = Raw<T, V>::N;
+  if constexpr (N % 4 == 0) {
 #pragma unroll
-    for (int e = 0; e < V; e += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(p + e);
-      x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
+    for (int i = 0; i < N; i += 4) {
+      const u32x4* q = reinterpret_cast<const u32x4*>(p + i * 4 / sizeof(T));
+      const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+      r.w[i] = v[0]; r.w[i + 1] = v[1]; r.w[i + 2] = v[2]; r.w[i + 3] = v[3];
     }
   } else {
-#pragma unroll
-    for (int e = 0; e < V; e += 4) {
-      const uint2 v = *reinterpret_cast<const uint2*>(p + e);
-      x[e] = bf16_to_f32((bf16_t)(v.x & 0xFFFF));
-      x[e + 1] = bf16_to_f32((bf16_t)(v.x >> 16));
-      x[e + 2] = bf16_to_f32((bf16_t)(v.y & 0xFFFF));
-      x[e + 3] = bf16_to_f32((bf16_t)(v.y >> 16));
-    }
+    const u32x2* q = reinterpret_cast<const u32x2*>(p);
+    const u32x2 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+    r.w[0] = v[0]; r.w[1] = v[1];
   }
 }
 template <typename T, int V>
-__device__ inline void store(T* p, const float (&x)[V]) {
-  if constexpr (sizeof(T) == 4) {
+__device__ inline float get(const Raw<T, V>& r, int e) {
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, r.w[e]);
+  else return __builtin_bit_cast(float, e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+}
+template <typename T, int V, bool STREAM = false>
+__device__ inline void store(T* p, const float* x) {
+  Raw<T, V> r;
+  constexpr int N = Raw<T, V>::N;
 #pragma unroll
-    for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 4) r.w[i] = __builtin_bit_cast(uint32_t, x[i]);
+    else r.w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
+  }
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 v = {r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]};
+      u32x4* q = reinterpret_cast<u32x4*>(p + i * 4 / sizeof(T));
+      if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+      else *q = v;
+    }
   } else {
-#pragma unroll
-    for (int e = 0; e < V; e += 4)
-      *reinterpret_cast<uint2*>(p + e) = make_uint2((uint32_t)f32_to_bf16(x[e]) | ((uint32_t)f32_to_bf16(x[e + 1]) << 16),
-                                                    (uint32_t)f32_to_bf16(x[e + 2]) | ((uint32_t)f32_to_bf16(x[e + 3]) << 16));
+    const u32x2 v = {r.w[0], r.w[1]};
+    u32x2* q = reinterpret_cast<u32x2*>(p);
+    if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+    else *q = v;
   }
 }
 
@@ -86,6 +112,20 @@ __device__ inline double group_sum(double x) {
   return x;
 }
 
+template <int CTRL>
+__device__ inline float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, false));
+}
+template <int G>
+__device__ inline float group_sum(float x) {
+  if constexpr (G >= 2) x += dpp<0xB1>(x);
+  if constexpr (G >= 4) x += dpp<0x4E>(x);
+  if constexpr (G >= 8) x += dpp<0x141>(x);
+  if constexpr (G >= 16) x += dpp<0x140>(x);
+  if constexpr (G >= 32) x += __shfl_xor(x, 16, 64);
+  return x;
+}
+
 // ---- per-head statistics ------------------------------------------------------------
 // 1 / sqrt(x) and 1 / x: the hardware's approximation and one Newton step (relative error below 2^-44)
 __device__ inline double rsqrt_nr(double x) {
@@ -96,12 +136,13 @@ __device__ inline double rcp_nr(double x) {
   const double y = __builtin_amdgcn_rcp(x);
   return fma(fma(-x, y, 1.0), y, y);
 }
-// r.m and rho = r.d / r.m of the head from sum (m + d)^2, sum (m - d)^2, sum m d
+// r.m and rho = r.d / r.m of the head from sum (m^2 + d^2) and sum m d
 struct Rms { double m, rho; };
-__device__ inline Rms rms_pair(double sp, double sm, double md, double inv_n, double neps) {
-  const double rp = rsqrt_nr(fma(sp, inv_n, neps)), rm = rsqrt_nr(fma(sm, inv_n, neps));
-  const double s = rp + rm, p = rp * rm * rcp_nr(s);
-  return {0.5 * s, -4.0 * md * inv_n * p * p};
+__device__ inline Rms rms_pair(double sq, double md, double inv_n, double neps) {
+  const double b = 2.0 * md, p = sq + b, q = sq - b;   // sums of (m + d)^2, (m - d)^2
+  const double rp = rsqrt_nr(fma(p < 0.0 ? 0.0 : p, inv_n, neps)), rm = rsqrt_nr(fma(q < 0.0 ? 0.0 : q, inv_n, neps));
+  const double s = rp + rm, x = rp * rm * rcp_nr(s);
+  return {0.5 * s, -2.0 * b * inv_n * x * x};
 }
 
 // ---- angles --------------------------------------------------------------------
@@ -134,313 +175,282 @@ __device__ inline void cos_sin(int pos, double f, float& c, float& s) {
   s = k >= 2 ? -b : b;
 }
 
+// A token's angles: lane l of the wavefront forms pairs l and l + 64, every lane
+// then takes those of its own V pairs from LDS (cs: the wavefront's own part, whose
+// accesses keep their order).  Eight heads of a wavefront share the 45 or so fp64
+// operations of an angle; formed by every lane for its own pairs, they took a third of
+// the forward's time.
 template <int V>
-__device__ inline void token_angles(const QkArgs& a, int t, int i0, bool on, float (&c)[V], float (&s)[V]) {
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    c[e] = 1.f;
-    s[e] = 0.f;
+__device__ inline void token_angles(const QkArgs& a, int t, int i0, float2* cs, float (&c)[V], float (&s)[V]) {
+  const int ts = a.pos ? 0 : t % a.S;
+  for (int i = threadIdx.x & 63; i < a.dh / 2; i += 64) {
+    const int pos = a.pos ? a.pos[(int64_t)a.rot.axis[i] * a.T + t] : ts;
+    float x, y;
+    cos_sin(pos, a.rot.freq[i], x, y);
+    cs[i] = make_float2(x, y);
   }
-  if (!on) return;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const int pos = a.pos ? a.pos[(int64_t)a.rot.axis[i0 + e] * a.T + t] : t % a.S;
-    cos_sin(pos, a.rot.freq[i0 + e], c[e], s[e]);
+    const float2 x = cs[i0 + e];
+    c[e] = x.x;
+    s[e] = x.y;
   }
 }
 
-// gains of the lane's elements (first and second half of the head)
+// gains of the lane's elements (first and second half of the head), as a pair
 template <typename T, int V>
-__device__ inline void load_gains(const T* g, const float* v, double eps, int i0, int half, bool on, float (&gm)[2 * V],
-                                  float (&gd)[2 * V]) {
+__device__ inline void lane_gains(const QkArgs& a, int seg, int i0, float (&gm)[2 * V], float (&gd)[2 * V]) {
+  const T* g = (const T*)(seg ? a.gk : a.gq);
+  const float* v = seg ? a.vk : a.vq;
+  const int half = a.dh / 2;
 #pragma unroll
-  for (int e = 0; e < 2 * V; ++e) {
-    const int j = i0 + (e < V ? e : half + e - V);
-    gm[e] = on ? ldf(g, j) : 0.f;
-    gd[e] = on && v ? (float)(eps * (double)v[j]) : 0.f;
+  for (int h = 0; h < 2; ++h) {
+    const int j = i0 + (h ? half : 0);
+    if (a.gvec) {
+      Raw<T, V> r;
+      load<T, V>(r, g + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) gm[h * V + e] = get<T, V>(r, e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) gm[h * V + e] = ldf(g, j + e);
+    }
+    if (!v) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) gd[h * V + e] = 0.f;
+    } else if (a.gvec) {
+      Raw<float, V> r;
+      load<float, V>(r, v + j);
+#pragma unroll
+      for (int e = 0; e < V; ++e) gd[h * V + e] = (float)(a.eps * (double)get<float, V>(r, e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) gd[h * V + e] = (float)(a.eps * (double)v[j + e]);
+    }
   }
 }
 
-// Work split: a wavefront takes 64 / G heads of one token at a time (a unit), G
-// lanes per head, lane g of a head its pairs g V .. g V + V - 1, so that a lane
-// turns pairs it holds itself.  G is the power of two from half / V up; lanes past
-// the head hold zeros.  The units of the query heads, then those of the key heads
-// are dealt to wavefronts in runs of `per` (cosines and gains are kept along a
-// run); the last workgroups move the value columns.
-struct Unit {
-  int seg, t, c, left;
+// Work split: a wavefront takes 64 / G heads of one token at a time, G lanes per
+// head, lane g of a head its pairs g V .. g V + V - 1, so that a lane turns pairs that
+// it holds itself.  G is the power of two from half / V up; lanes past the head and
+// past the last head work on elements of another lane, outside the sums, and store nothing.  A token's row is `chunks` such pieces (query heads, key heads, value heads);
+// a wavefront keeps one piece of the row, its gains and its gain sums, and goes from
+// token to token in steps of `step` tokens, so that the wavefronts of the grid
+// read and write memory in its order.
+struct Piece {
+  int seg, i0, col;   // 0 queries, 1 keys, 2 values; the lane's first pair in its head, its first column
+  bool on, ok;        // a lane of the head; of a head that the piece has
 };
-template <int G>
-__device__ inline bool first_unit(const QkArgs& a, const QkSplit& w, Unit& u) {
-  u.seg = (int)blockIdx.x >= w.blocks[0] ? 1 : 0;
-  const int b = blockIdx.x - (u.seg ? w.blocks[0] : 0);
-  const int64_t first = ((int64_t)b * NWAVE + (threadIdx.x >> 6)) * w.per[u.seg];
-  const int64_t units = (int64_t)a.T * w.chunks[u.seg];
-  u.left = (int)max((int64_t)0, min((int64_t)w.per[u.seg], units - first));
-  u.t = u.left ? (int)(first / w.chunks[u.seg]) : 0;
-  u.c = u.left ? (int)(first % w.chunks[u.seg]) : 0;
-  return u.left > 0;
-}
-
-// value columns: V = 8 elements per step
-template <typename T, typename TI>
-__device__ inline void move_values(const QkArgs& a, const TI* im, const TI* id, int64_t ldi, T* om, T* od, int64_t ldo,
-                                   int block, int nblocks) {
-  const int c0 = (a.Hq + a.Hk) * a.dh, n8 = a.Hk * a.dh / 8;
-  const int64_t n = (int64_t)a.T * n8;
-  for (int64_t i = (int64_t)block * NT + threadIdx.x; i < n; i += (int64_t)nblocks * NT) {
-    const int64_t t = i / n8;
-    const int c = c0 + 8 * (int)(i % n8);
-    float x[8], y[8];
-    load<TI, 8>(x, im + t * ldi + c);
-    load<TI, 8>(y, id + t * ldi + c);
-    store<T, 8>(om + t * ldo + c, x);
-    store<T, 8>(od + t * ldo + c, y);
-  }
+template <int V, int G>
+__device__ inline Piece piece(const QkArgs& a, const QkSplit& w, int c) {
+  const int lane = threadIdx.x & 63, i0 = (lane & (G - 1)) * V;
+  Piece p;
+  p.seg = c < w.chunks[0] ? 0 : c < w.chunks[0] + w.chunks[1] ? 1 : 2;
+  const int c0 = p.seg == 0 ? 0 : p.seg == 1 ? w.chunks[0] : w.chunks[0] + w.chunks[1];
+  const int h0 = p.seg == 0 ? 0 : p.seg == 1 ? a.Hq : a.Hq + a.Hk;
+  const int head = (c - c0) * (64 / G) + lane / G, H = p.seg ? a.Hk : a.Hq;
+  p.on = i0 < a.dh / 2;
+  p.ok = p.on && head < H;
+  p.i0 = p.on ? i0 : 0;
+  p.col = (h0 + min(head, H - 1)) * a.dh + p.i0;
+  return p;
 }
 
 template <typename T, int V, int G, bool NORM>
-__global__ __launch_bounds__(NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
+__global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
+  __shared__ float2 cs[FWD_NT / 64][QK_MAX_DH / 2];
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
-  const int nqk = w.blocks[0] + w.blocks[1];
-  if ((int)blockIdx.x >= nqk) {
-    move_values<T, T>(a, xm, xd, a.ldx, ym, yd, a.ldy, blockIdx.x - nqk, w.vblocks);
-    return;
-  }
-  Unit u;
-  if (!first_unit<G>(a, w, u)) return;
-  const int lane = threadIdx.x & 63, half = a.dh / 2;
-  const int i0 = (lane & (G - 1)) * V;
-  const bool on = i0 < half;
-  const int H = u.seg ? a.Hk : a.Hq, col0 = u.seg ? a.Hq * a.dh : 0;
-  float gm[2 * V], gd[2 * V], c[V], s[V];
-  if constexpr (NORM) load_gains<T, V>((const T*)(u.seg ? a.gk : a.gq), u.seg ? a.vk : a.vq, a.eps, i0, half, on, gm, gd);
-  token_angles<V>(a, u.t, i0, on, c, s);
-  while (true) {
-    const int head = u.c * (64 / G) + lane / G;
-    const bool ok = on && head < H;
-    float m[2 * V], d[2 * V];
-    {
-      float l[V], h[V];
-      const int64_t o = (int64_t)u.t * a.ldx + col0 + head * a.dh + i0;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (FWD_NT / 64) + (threadIdx.x >> 6)));
+  const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
+  if (wave / C >= w.step) return;
+  const Piece p = piece<V, G>(a, w, wave % C);
+  const int half = a.dh / 2;
+  float gm[2 * V], gd[2 * V];
+  if constexpr (NORM)
+    if (p.seg < 2) lane_gains<T, V>(a, p.seg, p.i0, gm, gd);
+  for (int64_t t = wave / C; t < a.T; t += w.step) {
+    Raw<T, V> in[4];   // mean and half difference, first and second half of the head
+    const int64_t o = t * a.ldx + p.col;
 #pragma unroll
-      for (int e = 0; e < V; ++e) l[e] = h[e] = 0.f;
-      if (ok) {
-        load<T, V>(l, xm + o);
-        load<T, V>(h, xm + o + half);
+    for (int k = 0; k < 4; ++k) {
+      load<T, V>(in[k], (k & 2 ? xd : xm) + o + (k & 1 ? half : 0));
+    }
+    float m[2 * V], d[2 * V], c[V], s[V];
+    if (p.seg < 2) token_angles<V>(a, (int)t, p.i0, cs[threadIdx.x >> 6], c, s);
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) {
+      m[e] = get<T, V>(in[e / V], e % V);
+      d[e] = get<T, V>(in[2 + e / V], e % V);
+    }
+    if (p.seg < 2) {
+      if constexpr (NORM) {
+        double sq = 0.0, md = 0.0;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          const double x = m[e], y = d[e];
+          sq = fma(x, x, fma(y, y, sq));
+          md = fma(x, y, md);
+        }
+        const Rms r = rms_pair(group_sum<G>(p.on ? sq : 0.0), group_sum<G>(p.on ? md : 0.0), a.inv_n, a.neps);
+        const float rm = (float)r.m, rho = (float)r.rho;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          const float um = (m[e] + d[e] * rho) * rm, ud = (m[e] * rho + d[e]) * rm;
+          m[e] = um * gm[e] + ud * gd[e];
+          d[e] = um * gd[e] + ud * gm[e];
+        }
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        m[e] = l[e];
-        m[V + e] = h[e];
-        l[e] = h[e] = 0.f;
-      }
-      if (ok) {
-        load<T, V>(l, xd + o);
-        load<T, V>(h, xd + o + half);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        d[e] = l[e];
-        d[V + e] = h[e];
+        const float ml = m[e], mh = m[V + e], dl = d[e], dh = d[V + e];
+        m[e] = ml * c[e] - mh * s[e];
+        m[V + e] = mh * c[e] + ml * s[e];
+        d[e] = dl * c[e] - dh * s[e];
+        d[V + e] = dh * c[e] + dl * s[e];
       }
     }
-    if constexpr (NORM) {
-      double sp = 0.0, sm = 0.0, md = 0.0;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) {
-        const double p = (double)m[e] + (double)d[e], q = (double)m[e] - (double)d[e];
-        sp = fma(p, p, sp);
-        sm = fma(q, q, sm);
-        md = fma((double)m[e], (double)d[e], md);
-      }
-      const Rms r = rms_pair(group_sum<G>(sp), group_sum<G>(sm), group_sum<G>(md), a.inv_n, a.neps);
-      const float rm = (float)r.m, rho = (float)r.rho;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) {
-        const float um = (m[e] + d[e] * rho) * rm, ud = (m[e] * rho + d[e]) * rm;
-        m[e] = um * gm[e] + ud * gd[e];
-        d[e] = um * gd[e] + ud * gm[e];
-      }
-    }
-    if (ok) {
-      const int64_t o = (int64_t)u.t * a.ldy + col0 + head * a.dh + i0;
-      float l[V], h[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        l[e] = m[e] * c[e] - m[V + e] * s[e];
-        h[e] = m[V + e] * c[e] + m[e] * s[e];
-      }
-      store<T, V>(ym + o, l);
-      store<T, V>(ym + o + half, h);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        l[e] = d[e] * c[e] - d[V + e] * s[e];
-        h[e] = d[V + e] * c[e] + d[e] * s[e];
-      }
-      store<T, V>(yd + o, l);
-      store<T, V>(yd + o + half, h);
-    }
-    if (--u.left == 0) break;
-    if (++u.c == w.chunks[u.seg]) {
-      u.c = 0;
-      ++u.t;
-      token_angles<V>(a, u.t, i0, on, c, s);
+    if (p.ok) {
+      const int64_t q = t * a.ldy + p.col;
+      store<T, V>(ym + q, m);
+      store<T, V>(ym + q + half, m + V);
+      store<T, V>(yd + q, d);
+      store<T, V>(yd + q + half, d + V);
     }
   }
 }
 
-// Backward.  Every workgroup leaves its sum of the gain gradient's half
-// difference (fp64, fixed order) as row blockIdx.x of part.
+// Backward.  Every workgroup leaves its sums of the gain gradients' half differences
+// (fp64, fixed order) as rows 2 blockIdx.x (queries) and 2 blockIdx.x + 1 (keys) of part.
 template <typename T, int V, int G, bool NORM>
-__global__ __launch_bounds__(NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
+__global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
+  constexpr int NW = BWD_NT / 64;
+  __shared__ float2 cs[NW][QK_MAX_DH / 2];
+  __shared__ double sh[NORM ? NW : 1][NORM ? 2 * V * G : 1];
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
-  const int nqk = w.blocks[0] + w.blocks[1];
-  if ((int)blockIdx.x >= nqk) {
-    move_values<T, float>(a, a.dy_m, a.dy_d, a.lddy, ym, yd, a.ldy, blockIdx.x - nqk, w.vblocks);
-    return;
-  }
-  __shared__ double sh[NORM ? NWAVE * 2 * V * G : 1];
-  Unit u;
-  const bool any = first_unit<G>(a, w, u);
-  if (!NORM && !any) return;
-  const int lane = threadIdx.x & 63, half = a.dh / 2;
-  const int i0 = (lane & (G - 1)) * V;
-  const bool on = i0 < half;
-  const int H = u.seg ? a.Hk : a.Hq, col0 = u.seg ? a.Hq * a.dh : 0;
-  float gm[2 * V], gd[2 * V], c[V], s[V];
+  const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * NW + wv));
+  const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
+  const int tokens = wave / C < w.step ? a.T : 0;   // (the last workgroup may hold wavefronts without work)
+  const Piece p = piece<V, G>(a, w, wave % C);
+  const int half = a.dh / 2;
+  float gm[2 * V], gd[2 * V];
   double acc[2 * V];
   if constexpr (NORM) {
-    load_gains<T, V>((const T*)(u.seg ? a.gk : a.gq), u.seg ? a.vk : a.vq, a.eps, i0, half, on, gm, gd);
+    if (p.seg < 2) lane_gains<T, V>(a, p.seg, p.i0, gm, gd);
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) acc[e] = 0.0;
   }
-  if (any) token_angles<V>(a, u.t, i0, on, c, s);
-  while (u.left > 0) {
-    const int head = u.c * (64 / G) + lane / G;
-    const bool ok = on && head < H;
-    float zm[2 * V], zd[2 * V], m[2 * V], d[2 * V];
-    {
-      const int64_t o = (int64_t)u.t * a.lddy + col0 + head * a.dh + i0;
-      float l[V], h[V];
+  for (int64_t t = wave / C; t < tokens; t += w.step) {
+    Raw<float, V> dy[4];
+    Raw<T, V> in[4];
 #pragma unroll
-      for (int ch = 0; ch < 2; ++ch) {
-        const float* g = ch ? a.dy_d : a.dy_m;
-        float* z = ch ? zd : zm;
+    for (int k = 0; k < 4; ++k) {
+      const int j = p.col + (k & 1 ? half : 0);
+      load<float, V, true>(dy[k], (k & 2 ? a.dy_d : a.dy_m) + t * a.lddy + j);
+      if constexpr (NORM)
+        if (p.seg < 2) load<T, V, true>(in[k], (k & 2 ? xd : xm) + t * a.ldx + j);
+    }
+    float zm[2 * V], zd[2 * V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) l[e] = h[e] = 0.f;
-        if (ok) {
-          load<float, V>(l, g + o);
-          load<float, V>(h, g + o + half);
+    for (int e = 0; e < 2 * V; ++e) {
+      zm[e] = get<float, V>(dy[e / V], e % V);
+      zd[e] = get<float, V>(dy[2 + e / V], e % V);
+    }
+    if (p.seg < 2) {
+      float c[V], s[V];
+      token_angles<V>(a, (int)t, p.i0, cs[wv], c, s);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float ml = zm[e], mh = zm[V + e], dl = zd[e], dh = zd[V + e];
+        zm[e] = ml * c[e] + mh * s[e];
+        zm[V + e] = mh * c[e] - ml * s[e];
+        zd[e] = dl * c[e] + dh * s[e];
+        zd[V + e] = dh * c[e] - dl * s[e];
+      }
+      if constexpr (NORM) {
+        float m[2 * V], d[2 * V];
+        double sq = 0.0, md = 0.0;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          m[e] = get<T, V>(in[e / V], e % V);
+          d[e] = get<T, V>(in[2 + e / V], e % V);
+          const double x = m[e], y = d[e];
+          sq = fma(x, x, fma(y, y, sq));
+          md = fma(x, y, md);
         }
+        const Rms r = rms_pair(group_sum<G>(p.on ? sq : 0.0), group_sum<G>(p.on ? md : 0.0), a.inv_n, a.neps);
+        const float rm = (float)r.m, rho = (float)r.rho;
+        float cm = 0.f, cd = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          z[e] = l[e] * c[e] + h[e] * s[e];
-          z[V + e] = h[e] * c[e] - l[e] * s[e];
+        for (int e = 0; e < 2 * V; ++e) {
+          const float um = (m[e] + d[e] * rho) * rm, ud = (m[e] * rho + d[e]) * rm;
+          m[e] = um;
+          d[e] = ud;
+          acc[e] += (double)(zm[e] * ud + zd[e] * um);
+          const float dum = zm[e] * gm[e] + zd[e] * gd[e], dud = zm[e] * gd[e] + zd[e] * gm[e];
+          zm[e] = dum;
+          zd[e] = dud;
+          cm += um * dum + ud * dud;
+          cd += um * dud + ud * dum;
+        }
+        cm = group_sum<G>(p.on ? cm : 0.f) * (float)a.inv_n;
+        cd = group_sum<G>(p.on ? cd : 0.f) * (float)a.inv_n;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          const float tm = zm[e] - (m[e] * cm + d[e] * cd), td = zd[e] - (m[e] * cd + d[e] * cm);
+          zm[e] = (tm + td * rho) * rm;
+          zd[e] = (tm * rho + td) * rm;
         }
       }
     }
-    if constexpr (NORM) {
-      const int64_t o = (int64_t)u.t * a.ldx + col0 + head * a.dh + i0;
-      float l[V], h[V];
-#pragma unroll
-      for (int ch = 0; ch < 2; ++ch) {
-        const T* x = ch ? xd : xm;
-        float* q = ch ? d : m;
-#pragma unroll
-        for (int e = 0; e < V; ++e) l[e] = h[e] = 0.f;
-        if (ok) {
-          load<T, V>(l, x + o);
-          load<T, V>(h, x + o + half);
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          q[e] = l[e];
-          q[V + e] = h[e];
-        }
-      }
-      double sp = 0.0, sm = 0.0, md = 0.0;
-      double xum = 0.0, xud = 0.0;   // of x o du
-      float dum[2 * V], dud[2 * V];
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) {
-        dum[e] = zm[e] * gm[e] + zd[e] * gd[e];
-        dud[e] = zm[e] * gd[e] + zd[e] * gm[e];
-        const double x = m[e], y = d[e], p = x + y, q = x - y;
-        sp = fma(p, p, sp);
-        sm = fma(q, q, sm);
-        md = fma(x, y, md);
-        xum = fma(x, (double)dum[e], fma(y, (double)dud[e], xum));
-        xud = fma(x, (double)dud[e], fma(y, (double)dum[e], xud));
-      }
-      const Rms r = rms_pair(group_sum<G>(sp), group_sum<G>(sm), group_sum<G>(md), a.inv_n, a.neps);
-      const double rn = r.m * a.inv_n, wm = group_sum<G>(xum) * rn, wd = group_sum<G>(xud) * rn;
-      const float rm = (float)r.m, rho = (float)r.rho;
-      const float cm = (float)fma(wd, r.rho, wm), cd = (float)fma(wm, r.rho, wd);
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) {
-        const float um = (m[e] + d[e] * rho) * rm, ud = (m[e] * rho + d[e]) * rm;
-        acc[e] += (double)(zm[e] * ud + zd[e] * um);
-        const float tm = dum[e] - (um * cm + ud * cd), td = dud[e] - (um * cd + ud * cm);
-        zm[e] = (tm + td * rho) * rm;
-        zd[e] = (tm * rho + td) * rm;
-      }
-    }
-    if (ok) {
-      const int64_t o = (int64_t)u.t * a.ldy + col0 + head * a.dh + i0;
-      float l[V], h[V];
-#pragma unroll
-      for (int ch = 0; ch < 2; ++ch) {
-        const float* z = ch ? zd : zm;
-        T* y = ch ? yd : ym;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          l[e] = z[e];
-          h[e] = z[V + e];
-        }
-        store<T, V>(y + o, l);
-        store<T, V>(y + o + half, h);
-      }
-    }
-    if (--u.left == 0) break;
-    if (++u.c == w.chunks[u.seg]) {
-      u.c = 0;
-      ++u.t;
-      token_angles<V>(a, u.t, i0, on, c, s);
+    if (p.ok) {
+      const int64_t q = t * a.ldy + p.col;
+      store<T, V, true>(ym + q, zm);
+      store<T, V, true>(ym + q + half, zm + V);
+      store<T, V, true>(yd + q, zd);
+      store<T, V, true>(yd + q + half, zd + V);
     }
   }
   if constexpr (NORM) {
-    // over the wavefront's head groups, then over the wavefronts
+    // over the wavefront's heads, then over the wavefronts of each segment
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) {
+      if (!p.ok) acc[e] = 0.0;
 #pragma unroll
       for (int o = G; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
-      if (lane < G) sh[((threadIdx.x >> 6) * 2 * V + e) * G + lane] = acc[e];
+      if (lane < G) sh[wv][e * G + lane] = acc[e];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < 2 * V * G; j += NT) {
-      double t = 0.0;
+    for (int k = threadIdx.x; k < 2 * 2 * V * G; k += BWD_NT) {
+      const int seg = k / (2 * V * G), j = k % (2 * V * G);
+      double x = 0.0;
 #pragma unroll
-      for (int v = 0; v < NWAVE; ++v) t += sh[v * 2 * V * G + j];
+      for (int v = 0; v < NW; ++v) {
+        const int c = (int)((blockIdx.x * NW + v) % C);
+        const int sv = c < w.chunks[0] ? 0 : c < w.chunks[0] + w.chunks[1] ? 1 : 2;
+        if (sv == seg) x += sh[v][j];
+      }
       // entry j: element e = j / G of lane j % G
       const int e = j / G, i = (j % G) * V;
-      if (i < half) a.part[(int64_t)blockIdx.x * a.dh + i + (e < V ? e : half + e - V)] = t;
+      if (i < half) a.part[(int64_t)(2 * blockIdx.x + seg) * a.dh + i + (e < V ? e : half + e - V)] = x;
     }
   }
 }
 
-// out[seg][j] (+)= scale * sum of the segment's rows of part: 16 columns and 64
-// row groups per workgroup, added in a fixed order
-__global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, QkSplit w, int dh, double scale, float* dgq,
+// out[seg][j] (+)= scale * sum over the workgroups' rows of the segment: 16 columns
+// and 64 row groups per workgroup, added in a fixed order
+__global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, int rows, int dh, double scale, float* dgq,
                                                        float* dgk, bool acc) {
   __shared__ double sh[16][16];
   const int seg = blockIdx.y, cl = threadIdx.x & 15, j = blockIdx.x * 16 + cl;
-  const int r0 = seg ? w.blocks[0] : 0, r1 = r0 + w.blocks[seg];
   double t = 0.0;
   if (j < dh)
-    for (int r = r0 + (threadIdx.x >> 4); r < r1; r += 64) t += part[(int64_t)r * dh + j];
+    for (int r = threadIdx.x >> 4; r < rows; r += 64) t += part[(int64_t)(2 * r + seg) * dh + j];
   t += __shfl_xor(t, 16, 64);
   t += __shfl_xor(t, 32, 64);
   if ((threadIdx.x & 63) < 16) sh[threadIdx.x >> 6][cl] = t;
@@ -454,76 +464,98 @@ __global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, QkSpl
   *out = acc ? (float)((double)*out + t) : (float)t;
 }
 
+// Pairs per lane: 8 (16-byte accesses) in the bf16 forward where a head divides into
+// them, 4 otherwise.  8192 tokens of 48 heads of 128, norm: 76 us against 78 with 4;
+// 16384, rotation alone: 147 against 152.  In the backward 8 leaves two wavefronts per
+// SIMD (204 registers): 155 us against 145.
+template <typename T, bool BWD>
+int lane_pairs(int dh) { return !BWD && sizeof(T) == 2 && dh % 16 == 0 ? 8 : 4; }
 // lanes per head
-int group_lanes(int dh) {
+int group_lanes(int dh, int v) {
   int g = 1;
-  while (4 * g < dh / 2) g *= 2;
+  while (v * g < dh / 2) g *= 2;
   return g;
 }
+int pieces(int heads, int dh, int v) { return (int)ceil_div(heads, 64 / group_lanes(dh, v)); }
 
-QkSplit split(const QkArgs& a, bool bwd, bool values) {
+QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
   QkSplit w{};
-  const int hpw = 64 / group_lanes(a.dh);
-  for (int k = 0; k < 2; ++k) {
-    w.chunks[k] = (int)ceil_div(k ? a.Hk : a.Hq, hpw);
-    const int64_t units = (int64_t)a.T * w.chunks[k];
-    const int64_t waves = (int64_t)NWAVE * (bwd ? QK_BWD_BLOCKS : 4096);
-    w.per[k] = (int)std::max<int64_t>(1, (units + waves - 1) / waves);
-    w.blocks[k] = (int)((units + (int64_t)NWAVE * w.per[k] - 1) / ((int64_t)NWAVE * w.per[k]));
-  }
-  if (values) w.vblocks = (int)std::min<int64_t>(1024, ((int64_t)a.T * (a.Hk * a.dh / 8) + NT - 1) / NT);
+  w.chunks[0] = pieces(a.Hq, a.dh, v);
+  w.chunks[1] = pieces(a.Hk, a.dh, v);
+  w.chunks[2] = values ? w.chunks[1] : 0;
+  const int nw = (bwd ? BWD_NT : FWD_NT) / 64;
+  const int64_t C = w.chunks[0] + w.chunks[1] + w.chunks[2];
+  // as few steps as the grid allows, the tokens dealt evenly over them
+  const int64_t at_once = std::max<int64_t>(1, (bwd ? BWD_WAVES : FWD_WAVES) / C);
+  const int64_t steps = std::max<int64_t>(1, (a.T + at_once - 1) / at_once);
+  w.step = (int)((a.T + steps - 1) / steps);
+  w.blocks = (int)((w.step * C + nw - 1) / nw);
   return w;
 }
 
-template <typename T, bool BWD, bool NORM>
-hipError_t dispatch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
-  const dim3 g(w.blocks[0] + w.blocks[1] + w.vblocks);
-  if (g.x == 0) return hipSuccess;
-#define QK(G)                                                                                      \
-  case G:                                                                                          \
-    if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, 4, G, NORM>), g, dim3(NT), 0, s, a, w); \
-    else hipLaunchKernelGGL((qk_fwd_kernel<T, 4, G, NORM>), g, dim3(NT), 0, s, a, w);               \
+template <typename T, bool BWD, bool NORM, int V>
+hipError_t dispatch_v(const QkArgs& a, const QkSplit& w, hipStream_t s) {
+  if (w.blocks == 0) return hipSuccess;
+#define QK(G)                                                                                                    \
+  case G:                                                                                                        \
+    if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w); \
+    else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);               \
     break
-  switch (group_lanes(a.dh)) {
+  switch (group_lanes(a.dh, V)) {
     QK(1);
     QK(2);
     QK(4);
     QK(8);
     QK(16);
-    QK(32);
+    case 32:
+      if constexpr (V == 4) {
+        if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, 32, NORM>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
+        else hipLaunchKernelGGL((qk_fwd_kernel<T, V, 32, NORM>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
+        break;
+      }
     default: return hipErrorInvalidValue;
   }
 #undef QK
   return hipGetLastError();
 }
+template <typename T, bool BWD, bool NORM>
+hipError_t dispatch(const QkArgs& a, bool values, QkSplit* out, hipStream_t s) {
+  const int v = lane_pairs<T, BWD>(a.dh);
+  const QkSplit w = split(a, v, BWD, values);
+  if (out) *out = w;
+  if constexpr (!BWD && sizeof(T) == 2)
+    if (v == 8) return dispatch_v<T, BWD, NORM, 8>(a, w, s);
+  return dispatch_v<T, BWD, NORM, 4>(a, w, s);
+}
 
 }  // namespace
 
 size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh) {
-  // (the workgroups of split(), which takes as many as this or fewer)
-  const int hpw = 64 / group_lanes(dh);
-  int64_t rows = 0;
-  for (int H : {Hq, Hk}) rows += std::min<int64_t>(QK_BWD_BLOCKS, (T_ * ceil_div(H, hpw) + NWAVE - 1) / NWAVE);
-  return (size_t)rows * dh * sizeof(double);
+  const int64_t C = pieces(Hq, dh, 4) + 2 * (int64_t)pieces(Hk, dh, 4);
+  // (split(): a step of at most max(BWD_WAVES, C) wavefronts)
+  const int64_t waves = std::min<int64_t>(T_ * C, std::max<int64_t>(BWD_WAVES, C));
+  return (size_t)((waves + BWD_NT / 64 - 1) / (BWD_NT / 64)) * 2 * dh * sizeof(double);
 }
 
 template <typename T>
 hipError_t launch_qk_fwd(QkArgs a, hipStream_t s) {
   if (a.dh % 8 || a.dh > QK_MAX_DH || a.T < 0) return hipErrorInvalidValue;
   a.inv_n = 1.0 / a.dh;
-  const QkSplit w = split(a, false, a.x_m != a.y_m);
-  return a.gq ? dispatch<T, false, true>(a, w, s) : dispatch<T, false, false>(a, w, s);
+  a.gvec = (((uintptr_t)a.gq | (uintptr_t)a.gk | (uintptr_t)a.vq | (uintptr_t)a.vk) & 15) == 0;
+  const bool values = a.x_m != a.y_m;
+  return a.gq ? dispatch<T, false, true>(a, values, nullptr, s) : dispatch<T, false, false>(a, values, nullptr, s);
 }
 
 template <typename T>
 hipError_t launch_qk_bwd(QkArgs a, float* dgq, float* dgk, bool acc, hipStream_t s) {
   if (a.dh % 8 || a.dh > QK_MAX_DH || a.T < 0) return hipErrorInvalidValue;
   a.inv_n = 1.0 / a.dh;
-  const QkSplit w = split(a, true, true);
-  if (!a.gq) return dispatch<T, true, false>(a, w, s);
-  const hipError_t r = dispatch<T, true, true>(a, w, s);
+  a.gvec = (((uintptr_t)a.gq | (uintptr_t)a.gk | (uintptr_t)a.vq | (uintptr_t)a.vk) & 15) == 0;
+  QkSplit w;
+  if (!a.gq) return dispatch<T, true, false>(a, true, &w, s);
+  const hipError_t r = dispatch<T, true, true>(a, true, &w, s);
   if (r != hipSuccess) return r;
-  hipLaunchKernelGGL(qk_gain_kernel, dim3(ceil_div(a.dh, 16), 2), dim3(1024), 0, s, a.part, w, a.dh, 1.0 / a.eps, dgq, dgk, acc);
+  hipLaunchKernelGGL(qk_gain_kernel, dim3(ceil_div(a.dh, 16), 2), dim3(1024), 0, s, a.part, w.blocks, a.dh, 1.0 / a.eps, dgq, dgk, acc);
   return hipGetLastError();
 }
 

@@ -212,7 +212,8 @@ class Model:
             raise FdhError(st, "fdh_create rejected the configuration")
         self.qk_norm, self.n_axes = bool(qk_norm), max(1, len(sec))
         self._stream = int(getattr(stream, "value", stream) or 0)
-        self._qk_dtype = "float32" if dtype == "f32" else "bfloat16"
+        self._qk_dh = d_model // n_heads
+        self._qk_cols = (n_heads + 2 * (n_kv_heads or n_heads)) * self._qk_dh
         self._h = h
         self._ws = None
         self._keep = []        # tensors the bound operator points to
@@ -389,54 +390,62 @@ class Model:
         return int(n.value)
 
     # ---- the q/k front of a layer ----
-    def _qk_pair(self, pair, what, dtype, T=None):
+    # (these run in a few microseconds on the device, so their checks are kept short)
+    def _qk_pair(self, pair, what, dtype, T, dev):
         """Pointers and row stride of a pair of [T, (n_heads + 2 n_kv_heads) head_dim] tensors."""
         m, d = pair
-        ncol = (self.cfg.n_heads + 2 * self.cfg.n_kv_heads) * (self.cfg.d_model // self.cfg.n_heads)
-        for t in (m, d):
-            if t.dim() != 2 or t.shape[1] != ncol or (T is not None and t.shape[0] != T):
-                raise ValueError(f"{what} must be two [tokens, {ncol}] tensors")
-            if str(t.dtype) != "torch." + dtype:
-                raise ValueError(f"{what} must have dtype {dtype}")
-            if t.stride(1) != 1:
-                raise ValueError(f"{what}: the elements of a row must be contiguous")
-        ld = ncol if m.shape[0] <= 1 else m.stride(0)
-        if d.shape[0] != m.shape[0] or (m.shape[0] > 1 and d.stride(0) != ld):
-            raise ValueError(f"{what}: both tensors must have the same rows and row stride")
-        self._qk_device(m, d)
+        shape, n = m.shape, self._qk_cols
+        if len(shape) != 2 or shape[1] != n or shape[0] != T or d.shape != shape:
+            raise ValueError(f"{what} must be two [{T}, {n}] tensors")
+        if m.dtype is not dtype or d.dtype is not dtype:
+            raise ValueError(f"{what} must have dtype {dtype}")
+        (ld, one), (ld_d, one_d) = m.stride(), d.stride()
+        if one != 1 or one_d != 1:
+            raise ValueError(f"{what}: the elements of a row must be contiguous")
+        if T <= 1:
+            ld = n
+        elif ld != ld_d:
+            raise ValueError(f"{what}: both tensors must have the same row stride")
+        if m.get_device() != dev or d.get_device() != dev:
+            raise ValueError("tensors must lie on the current device")
         return m.data_ptr(), d.data_ptr(), ld
 
-    def _qk_device(self, *tensors):
+    def _qk_args(self, t, seq, gains, eps, positions):
+        """(device, gains, positions pointer, B) of a call whose rows are those of t;
+        refuses a current device or stream that is not the call's."""
         import torch
-        dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-        for t in tensors:
-            if t is not None and (not t.is_cuda or t.device.index != dev):
-                raise ValueError("tensors must lie on the current device")
-
-    def _qk_args(self, T, seq, gains, eps, positions):
-        """(gains, positions pointer, B, S) of a call; refuses a current stream that is not the context's."""
-        import torch
+        dev, T = t.get_device(), t.shape[0] if t.dim() else 0
+        if dev < 0 or dev != torch.cuda.current_device():
+            raise ValueError("tensors must lie on the current device")
         if seq < 1 or T % seq:
             raise ValueError("seq must be positive and divide the number of tokens")
-        if T and torch.cuda.current_stream().cuda_stream != self._stream:
+        if torch.cuda.current_stream().cuda_stream != self._stream:
             raise ValueError("the current stream is not the model's: build the model with stream=<the current stream>")
         g = None
         if gains is not None:
-            dh = self.cfg.d_model // self.cfg.n_heads
             q, k, vq, vk = gains
-            for t, what, dt in ((q, "gains", self._qk_dtype), (k, "gains", self._qk_dtype), (vq, "gain directions", "float32"),
-                                (vk, "gain directions", "float32")):
-                if t is None and what != "gains":
+            for x, what, dt in ((q, "gains", self._qk_dtype), (k, "gains", self._qk_dtype),
+                                (vq, "gain directions", torch.float32), (vk, "gain directions", torch.float32)):
+                if x is None and dt is torch.float32 and what != "gains":
                     continue
-                if t is None or str(t.dtype) != "torch." + dt or t.numel() != dh or not t.is_contiguous():
-                    raise ValueError(f"{what} must be contiguous {dt} tensors of {dh} elements")
-            self._qk_device(q, k, vq, vk)
-            g = C.byref(QkGains(_ptr(q), _ptr(k), _ptr(vq), _ptr(vk), float(eps)))
+                if x is None or x.dtype is not dt or x.numel() != self._qk_dh or not x.is_contiguous():
+                    raise ValueError(f"{what} must be contiguous {dt} tensors of {self._qk_dh} elements")
+                if x.get_device() != dev:
+                    raise ValueError("tensors must lie on the current device")
+            g = C.byref(QkGains(q.data_ptr(), k.data_ptr(), _ptr(vq), _ptr(vk), eps))
+        pos = 0
         if positions is not None:
-            if str(positions.dtype) != "torch.int32" or positions.numel() != self.n_axes * T or not positions.is_contiguous():
+            if positions.dtype is not torch.int32 or positions.numel() != self.n_axes * T or not positions.is_contiguous():
                 raise ValueError(f"positions must be a contiguous int32 tensor of {self.n_axes} x tokens elements")
-            self._qk_device(positions)
-        return g, _ptr(positions), T // seq, seq
+            if positions.get_device() != dev:
+                raise ValueError("tensors must lie on the current device")
+            pos = positions.data_ptr()
+        return dev, g, pos, T // seq
+
+    @property
+    def _qk_dtype(self):
+        import torch
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
 
     def qk_scratch(self, B: int, S: int):
         """A device buffer for qk_backward on B x S tokens (None where it needs none)."""
@@ -454,13 +463,13 @@ class Model:
         tokens], None for 0 .. seq - 1.  out: a pair to write (x itself for in
         place).  Enqueued on the model's stream, which must be the current one."""
         import torch
-        xm, xd, ldx = self._qk_pair(x, "x", self._qk_dtype)
-        T = x[0].shape[0]
-        g, pos, B, S = self._qk_args(T, seq, gains, eps, positions)
+        dev, g, pos, B = self._qk_args(x[0], seq, gains, eps, positions)
+        T, dt = B * seq, self._qk_dtype
+        xm, xd, ldx = self._qk_pair(x, "x", dt, T, dev)
         if out is None:
-            out = tuple(torch.empty(x[0].shape, dtype=x[0].dtype, device=x[0].device) for _ in range(2))
-        ym, yd, ldy = self._qk_pair(out, "out", self._qk_dtype, T)
-        st = self._L.fdh_qk_forward(self._h, g, pos, B, S, xm, xd, ldx, ym, yd, ldy)
+            out = tuple(torch.empty((T, self._qk_cols), dtype=dt, device=x[0].device) for _ in range(2))
+        ym, yd, ldy = self._qk_pair(out, "out", dt, T, dev)
+        st = self._L.fdh_qk_forward(self._h, g, pos, B, seq, xm, xd, ldx, ym, yd, ldy)
         if st < 0:
             self._check(st, "fdh_qk_forward")
         return out
@@ -474,33 +483,33 @@ class Model:
         seq), made here if None; calls that may overlap on the device need one
         each."""
         import torch
-        gm, gd, lddy = self._qk_pair(dy, "dy", "float32")
-        T = dy[0].shape[0]
-        g, pos, B, S = self._qk_args(T, seq, gains, eps, positions)
+        dev, g, pos, B = self._qk_args(dy[0], seq, gains, eps, positions)
+        T, dt = B * seq, self._qk_dtype
+        gm, gd, lddy = self._qk_pair(dy, "dy", torch.float32, T, dev)
         if out is None:
-            dt = getattr(torch, self._qk_dtype)
-            out = tuple(torch.empty(dy[0].shape, dtype=dt, device=dy[0].device) for _ in range(2))
-        om, od, lddx = self._qk_pair(out, "out", self._qk_dtype, T)
+            out = tuple(torch.empty((T, self._qk_cols), dtype=dt, device=dy[0].device) for _ in range(2))
+        om, od, lddx = self._qk_pair(out, "out", dt, T, dev)
         xm = xd = ldx = 0
         dg = (None, None)
         if self.qk_norm:
             if x is None:
                 raise ValueError("a model with qk_norm needs x")
-            xm, xd, ldx = self._qk_pair(x, "x", self._qk_dtype, T)
-            dh = self.cfg.d_model // self.cfg.n_heads
+            xm, xd, ldx = self._qk_pair(x, "x", dt, T, dev)
             if gain_grads is None:
                 if accumulate:
                     raise ValueError("accumulate needs gain_grads")
-                gain_grads = tuple(torch.empty(dh, device=dy[0].device) for _ in range(2))
+                gain_grads = tuple(torch.empty(self._qk_dh, device=dy[0].device) for _ in range(2))
             dg = gain_grads
             for t in dg:
-                if str(t.dtype) != "torch.float32" or t.numel() != dh or not t.is_contiguous():
-                    raise ValueError(f"gain_grads must be contiguous float32 tensors of {dh} elements")
+                if t.dtype is not torch.float32 or t.numel() != self._qk_dh or not t.is_contiguous():
+                    raise ValueError(f"gain_grads must be contiguous float32 tensors of {self._qk_dh} elements")
             if scratch is None:
-                scratch = self.qk_scratch(B, S)
-            self._qk_device(*dg, scratch)
+                scratch = self.qk_scratch(B, seq)
+            for t in (*dg, scratch):
+                if t is not None and t.get_device() != dev:
+                    raise ValueError("tensors must lie on the current device")
         nb = 0 if scratch is None else scratch.numel() * scratch.element_size()
-        st = self._L.fdh_qk_backward(self._h, g, pos, B, S, xm, xd, ldx, gm, gd, lddy, om, od, lddx, _ptr(dg[0]), _ptr(dg[1]),
+        st = self._L.fdh_qk_backward(self._h, g, pos, B, seq, xm, xd, ldx, gm, gd, lddy, om, od, lddx, _ptr(dg[0]), _ptr(dg[1]),
                                      int(accumulate), _ptr(scratch), nb)
         if st < 0:
             self._check(st, "fdh_qk_backward")

@@ -162,8 +162,8 @@ def forward_bound(x, hq, hk, dh, ang, gains=None, eps=1.0, norm_eps=1e-5):
 
 def backward_bound(x, dy, hq, hk, dh, ang, gains=None, eps=1.0, norm_eps=1e-5):
     """Bounds (m, d) for dx and for the two gain gradients.  dz: 3 roundings; du = dz o g: 3
-    more; mean(x o du) fp64, c rounded once: 7; u: 5, u o c: 2 more, 14 in all; du - u o c: 15;
-    times r: 5 more, 20.  Gain terms: dz 3, u 5, product and sum 2, the output's own rounding 1."""
+    more; u: 5; u o du: 12 with the product; c, its mean in fp32: 16 sums in a lane, 5 over
+    lanes, 1 division: 34; u o c: 5 and 2 more, 41; du - u o c: 42; times r: 5 more, 47.  Gain terms: dz 3, u 5, product and sum 2, the output's own rounding 1."""
     T = dy[0].shape[0]
     z = [_abs_turn(t.detach().cpu().to(F64).abs().view(T, hq + 2 * hk, dh)[:, :hq + hk], ang) for t in dy]
     dg = None
@@ -178,7 +178,7 @@ def backward_bound(x, dy, hq, hk, dh, ang, gains=None, eps=1.0, norm_eps=1e-5):
         c = _mul(r, (ud[0].mean(-1, keepdim=True), ud[1].mean(-1, keepdim=True)))
         uc = _mul(u, c)
         z = _mul(r, (du[0] + uc[0], du[1] + uc[1]))
-        k = 20
+        k = 47
     return _bounds(z, k, dy, hq, hk, dh), dg
 
 

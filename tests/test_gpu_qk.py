@@ -403,6 +403,12 @@ def test_binding_refusals_on_the_device():
         m.qk_forward(x, 4, gains=gains, positions=torch.zeros(3, 4, dtype=torch.int64, device="cuda"))
     with pytest.raises(ValueError, match="device"):
         m.qk_forward(x, 4, gains=gains, positions=torch.zeros(3, 4, dtype=torch.int32))
+    with pytest.raises(ValueError, match="dtype"):
+        m.qk_forward(tuple(t.float() for t in x), 4, gains=gains)
+    with pytest.raises(ValueError, match="device"):
+        m.qk_forward((x[0], x[1].cpu()), 4, gains=gains)
+    with pytest.raises(ValueError, match="device"):
+        m.qk_forward(x, 4, gains=(*gains[:3], gains[3].cpu()))
     with pytest.raises(ValueError, match="gains"):
         m.qk_forward(x, 4, gains=(gains[0].float(), *gains[1:]))
     with pytest.raises(fd.FdhError, match="overlaps"):

@@ -231,16 +231,19 @@ def test_binding_refuses_before_any_launch():
     x = tuple(torch.zeros(4, 1024, dtype=torch.bfloat16) for _ in range(2))
     with pytest.raises(ValueError, match="device"):
         m.qk_forward(x, 4)
-    with pytest.raises(ValueError, match="tokens"):
-        m.qk_forward(tuple(t[:, :1016] for t in x), 4)
-    with pytest.raises(ValueError, match="dtype"):
-        m.qk_forward(tuple(t.float() for t in x), 4)
-    with pytest.raises(ValueError, match="contiguous"):
-        m.qk_forward(tuple(torch.zeros(1024, 4, dtype=torch.bfloat16).T for _ in range(2)), 4)
-    with pytest.raises(ValueError, match="same rows"):
-        m.qk_forward((x[0], torch.zeros(4, 1032, dtype=torch.bfloat16)[:, :1024]), 4)
-    with pytest.raises(ValueError, match="dtype"):
-        m.qk_backward(x, 4)
+    with pytest.raises(ValueError, match="device"):
+        m.qk_backward(tuple(t.float() for t in x), 4)
+    pair = lambda x, T=4: m._qk_pair(x, "x", torch.bfloat16, T, -1)
+    assert pair(x) == (x[0].data_ptr(), x[1].data_ptr(), 1024)
+    for bad, word in ((tuple(t[:, :1016] for t in x), "tensors"), (tuple(t[:3] for t in x), "tensors"), ((x[0], x[1][:3]), "tensors"),
+                      (tuple(t[0] for t in x), "tensors"), (tuple(t.float() for t in x), "dtype"), ((x[0], x[1].half()), "dtype"),
+                      (tuple(torch.zeros(1024, 4, dtype=torch.bfloat16).T for _ in range(2)), "contiguous"),
+                      ((x[0], torch.zeros(4, 1032, dtype=torch.bfloat16)[:, :1024]), "row stride")):
+        with pytest.raises(ValueError, match=word):
+            pair(bad)
+    # one row: whatever stride torch reports for it, it is one row
+    one = tuple(torch.zeros(8, 1024, dtype=torch.bfloat16)[::8] for _ in range(2))
+    assert pair(one, 1)[2] == 1024
 
 
 # ---- the SLQ command ----------------------------------------------------------------
