@@ -258,7 +258,7 @@ fdh_status fdh_bind_dataset_positions(fdh_ctx* ctx, const void* params_dev, cons
  * stay as they are); no other overlap.  positions_dev: int32 [axes, B, S] or NULL
  * (0 .. S - 1 in every row).  Pointers 16-byte aligned, strides in multiples of 16
  * bytes; positions and gains of any element alignment.  Any B*S from 0 (nothing is
- * done) to below 2^31; needs no workspace.  Each output is rounded once from fp32
+ * done) to 2^31 - 64; needs no workspace.  Each output is rounded once from fp32
  * arithmetic with fp64 sums; a head that holds a NaN or an infinity is normed to NaN.
  * Only enqueued on the context stream (no wait, no allocation: may be captured in
  * a graph); a layer's call for one token is the call with B = S = 1. */

@@ -1274,7 +1274,7 @@ int Engine::qk_check(const fdh_qk_gains* g, int B, int S, QkArgs* a) {
   if (!llama) { err = "needs a Llama-family context"; return FDH_ERR_UNSUPPORTED; }
   if (dh > QK_MAX_DH) { err = "head_dim must be <= 256"; return FDH_ERR_UNSUPPORTED; }
   if (B < 0 || S < 0) { err = "B and S must not be negative"; return FDH_ERR_INVALID_ARG; }
-  if ((int64_t)B * S > INT32_MAX) { err = "B*S must be < 2^31"; return FDH_ERR_UNSUPPORTED; }
+  if ((int64_t)B * S > QK_MAX_TOKENS) { err = "B*S must be <= 2^31 - 64"; return FDH_ERR_UNSUPPORTED; }
   if (qk_norm) {
     if (!g || !g->q || !g->k) { err = "this context norms its heads: gains are required"; return FDH_ERR_INVALID_ARG; }
     if (!(g->eps > 0.0) || !std::isfinite(g->eps)) { err = "eps must be positive and finite"; return FDH_ERR_INVALID_ARG; }

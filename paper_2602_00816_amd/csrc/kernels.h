@@ -177,6 +177,7 @@ hipError_t launch_rope_table(double* cs, int S, int dh, double base, hipStream_t
 
 // ---- qk.hip: per-head norm and position rotation of the q and k columns ----------
 constexpr int QK_MAX_DH = 256;
+constexpr int64_t QK_MAX_TOKENS = ((int64_t)1 << 31) - 64;   // (a group of 64 tokens stays an int)
 // pair i of a head (elements i, i + dh/2) turns by 2 pi freq[i] pos[axis[i]]
 struct QkRotary {
   double freq[QK_MAX_DH / 2];    // turns per position: base^(-2i/dh) / (2 pi)
@@ -199,9 +200,10 @@ struct QkArgs {
   bool gvec;                     // gains and directions 16-byte aligned
   QkRotary rot;
 };
-// how a launch is split: pieces of a row (queries, keys, values), tokens per step, workgroups
+// how a launch is split: tokens per group, groups, pieces of a group (queries, keys,
+// values), groups per step, workgroups; ceil(2^16 / half)
 struct QkSplit {
-  int chunks[3], step, blocks;
+  int group, groups, chunks[3], step, blocks, rhalf;
 };
 // bytes of part for up to T_ tokens
 size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh);

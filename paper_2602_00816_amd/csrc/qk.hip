@@ -175,30 +175,41 @@ __device__ inline void cos_sin(int pos, double f, float& c, float& s) {
   s = k >= 2 ? -b : b;
 }
 
-// A token's angles: lane l of the wavefront forms pairs l and l + 64, every lane
-// then takes those of its own V pairs from LDS (cs: the wavefront's own part, whose
-// accesses keep their order).  Eight heads of a wavefront share the 45 or so fp64
-// operations of an angle; formed by every lane for its own pairs, they took a third of
-// the forward's time.
-template <int V>
-__device__ inline void token_angles(const QkArgs& a, int t, int i0, float2* cs, float (&c)[V], float (&s)[V]) {
-  const int ts = a.pos ? 0 : t % a.S;
-  for (int i = threadIdx.x & 63; i < a.dh / 2; i += 64) {
-    const int pos = a.pos ? a.pos[(int64_t)a.rot.axis[i] * a.T + t] : ts;
+// Angles of the tokens t0 .. t0 + ntok - 1 that a wavefront's heads belong to, formed
+// by the lanes in turn, to LDS (cs: the wavefront's own part, whose accesses keep
+// their order); every lane then takes those of its token (tok after t0) and its own
+// V pairs.  The heads of a token share the 45 or so fp64 operations of an angle; formed
+// by every lane for its own pairs, they took a third of the forward's time.
+template <int V, bool GROUP>
+__device__ inline void token_angles(const QkArgs& a, const QkSplit& w, int t0, int ntok, int tok, int i0, float2* cs,
+                                    float (&c)[V], float (&s)[V]) {
+  const int half = a.dh / 2, s0 = a.pos ? 0 : t0 % a.S;
+  for (int i = threadIdx.x & 63; i < (GROUP ? ntok * half : half); i += 64) {
+    const int k = GROUP ? i * w.rhalf >> 16 : 0, j = i - k * half;   // i / half, i % half
+    int pos;
+    if (a.pos) {
+      pos = a.pos[(int64_t)a.rot.axis[j] * a.T + (GROUP ? min(t0 + k, a.T - 1) : t0)];
+    } else {
+      pos = s0 + k;
+      if (GROUP && pos >= a.S) pos %= a.S;
+    }
     float x, y;
-    cos_sin(pos, a.rot.freq[i], x, y);
+    cos_sin(pos, a.rot.freq[j], x, y);
     cs[i] = make_float2(x, y);
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  const float2* q = cs + (GROUP ? tok * half : 0) + i0;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float2 x = cs[i0 + e];
-    c[e] = x.x;
-    s[e] = x.y;
+    c[e] = q[e].x;
+    s[e] = q[e].y;
   }
 }
+
+// offset of row t (both below 2^32)
+__device__ inline int64_t row(int t, int64_t ld) { return (int64_t)((uint64_t)(uint32_t)t * (uint32_t)ld); }
 
 // gains of the lane's elements (first and second half of the head), as a pair
 template <typename T, int V>
@@ -233,54 +244,66 @@ __device__ inline void lane_gains(const QkArgs& a, int seg, int i0, float (&gm)[
   }
 }
 
-// Work split: a wavefront takes 64 / G heads of one token at a time, G lanes per
-// head, lane g of a head its pairs g V .. g V + V - 1, so that a lane turns pairs that
-// it holds itself.  G is the power of two from half / V up; lanes past the head and
-// past the last head work on elements of another lane, outside the sums, and store nothing.  A token's row is `chunks` such pieces (query heads, key heads, value heads);
-// a wavefront keeps one piece of the row, its gains and its gain sums, and goes from
-// token to token in steps of `step` tokens, so that the wavefronts of the grid
-// read and write memory in its order.
+// Work split: a wavefront takes 64 / G heads at a time, G lanes per head, lane g of a
+// head its pairs g V .. g V + V - 1, so that a lane turns pairs that it holds itself.
+// G is the power of two from half / V up; lanes past the head and past the last head work
+// on elements of another lane, outside the sums, and store nothing.  The query heads of
+// `group` tokens one after the other, their key heads and their value heads are cut into
+// `chunks` pieces of 64 / G heads (group > 1 where a token's heads would not fill
+// them).  A wavefront keeps one piece, its gains and its gain sums, and goes from
+// group to group in steps of `step`, so that the wavefronts of the grid read and write
+// memory in its order.
 struct Piece {
-  int seg, i0, col;   // 0 queries, 1 keys, 2 values; the lane's first pair in its head, its first column
+  int seg;            // 0 queries, 1 keys, 2 values
+  int t0, ntok, tok;  // first token in the group, tokens, the lane's one after t0
+  int i0, col;        // the lane's first pair in its head, its first column
   bool on, ok;        // a lane of the head; of a head that the piece has
 };
-template <int V, int G>
+template <int V, int G, bool GROUP>
 __device__ inline Piece piece(const QkArgs& a, const QkSplit& w, int c) {
+  constexpr int HPW = 64 / G;
   const int lane = threadIdx.x & 63, i0 = (lane & (G - 1)) * V;
   Piece p;
   p.seg = c < w.chunks[0] ? 0 : c < w.chunks[0] + w.chunks[1] ? 1 : 2;
-  const int c0 = p.seg == 0 ? 0 : p.seg == 1 ? w.chunks[0] : w.chunks[0] + w.chunks[1];
+  const int r0 = HPW * (c - (p.seg == 0 ? 0 : p.seg == 1 ? w.chunks[0] : w.chunks[0] + w.chunks[1]));
   const int h0 = p.seg == 0 ? 0 : p.seg == 1 ? a.Hq : a.Hq + a.Hk;
-  const int head = (c - c0) * (64 / G) + lane / G, H = p.seg ? a.Hk : a.Hq;
+  const int H = p.seg ? a.Hk : a.Hq, rows = GROUP ? w.group * H : H;   // heads of the segment in the group
+  const int r = min(r0 + lane / G, rows - 1);
   p.on = i0 < a.dh / 2;
-  p.ok = p.on && head < H;
+  p.ok = p.on && r0 + lane / G < rows;
   p.i0 = p.on ? i0 : 0;
-  p.col = (h0 + min(head, H - 1)) * a.dh + p.i0;
+  p.t0 = GROUP ? r0 / H : 0;
+  p.ntok = GROUP ? (min(r0 + HPW, rows) - 1) / H - p.t0 + 1 : 1;
+  p.tok = GROUP ? r / H - p.t0 : 0;
+  p.col = (h0 + (GROUP ? r % H : r)) * a.dh + p.i0;
   return p;
 }
 
-template <typename T, int V, int G, bool NORM>
+template <typename T, int V, int G, bool NORM, bool GROUP>
 __global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
-  __shared__ float2 cs[FWD_NT / 64][QK_MAX_DH / 2];
+  __shared__ float2 cs[FWD_NT / 64][64 * V];   // 64 / G tokens of half <= G V pairs
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (FWD_NT / 64) + (threadIdx.x >> 6)));
   const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
   if (wave / C >= w.step) return;
-  const Piece p = piece<V, G>(a, w, wave % C);
+  const Piece p = piece<V, G, GROUP>(a, w, wave % C);
   const int half = a.dh / 2;
   float gm[2 * V], gd[2 * V];
   if constexpr (NORM)
     if (p.seg < 2) lane_gains<T, V>(a, p.seg, p.i0, gm, gd);
-  for (int64_t t = wave / C; t < a.T; t += w.step) {
+  for (int64_t g = wave / C; g < w.groups; g += w.step) {
+    // (a wavefront of heads of one token knows its token as a scalar)
+    const int t0 = GROUP ? (int)g * w.group + p.t0 : (int)g, t = GROUP ? min(t0 + p.tok, a.T - 1) : t0;
+    const bool ok = GROUP ? p.ok && t0 + p.tok < a.T : p.ok;
     Raw<T, V> in[4];   // mean and half difference, first and second half of the head
-    const int64_t o = t * a.ldx + p.col;
+    const int64_t o = row(t, a.ldx) + p.col;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       load<T, V>(in[k], (k & 2 ? xd : xm) + o + (k & 1 ? half : 0));
     }
     float m[2 * V], d[2 * V], c[V], s[V];
-    if (p.seg < 2) token_angles<V>(a, (int)t, p.i0, cs[threadIdx.x >> 6], c, s);
+    if (p.seg < 2) token_angles<V, GROUP>(a, w, t0, p.ntok, p.tok, p.i0, cs[threadIdx.x >> 6], c, s);
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) {
       m[e] = get<T, V>(in[e / V], e % V);
@@ -313,8 +336,8 @@ __global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
         d[V + e] = dh * c[e] + dl * s[e];
       }
     }
-    if (p.ok) {
-      const int64_t q = t * a.ldy + p.col;
+    if (ok) {
+      const int64_t q = row(t, a.ldy) + p.col;
       store<T, V>(ym + q, m);
       store<T, V>(ym + q + half, m + V);
       store<T, V>(yd + q, d);
@@ -325,18 +348,18 @@ __global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
 
 // Backward.  Every workgroup leaves its sums of the gain gradients' half differences
 // (fp64, fixed order) as rows 2 blockIdx.x (queries) and 2 blockIdx.x + 1 (keys) of part.
-template <typename T, int V, int G, bool NORM>
+template <typename T, int V, int G, bool NORM, bool GROUP>
 __global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
   constexpr int NW = BWD_NT / 64;
-  __shared__ float2 cs[NW][QK_MAX_DH / 2];
+  __shared__ float2 cs[NW][64 * V];   // 64 / G tokens of half <= G V pairs
   __shared__ double sh[NORM ? NW : 1][NORM ? 2 * V * G : 1];
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * NW + wv));
   const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
-  const int tokens = wave / C < w.step ? a.T : 0;   // (the last workgroup may hold wavefronts without work)
-  const Piece p = piece<V, G>(a, w, wave % C);
+  const int groups = wave / C < w.step ? w.groups : 0;   // (the last workgroup may hold wavefronts without work)
+  const Piece p = piece<V, G, GROUP>(a, w, wave % C);
   const int half = a.dh / 2;
   float gm[2 * V], gd[2 * V];
   double acc[2 * V];
@@ -345,15 +368,18 @@ __global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) acc[e] = 0.0;
   }
-  for (int64_t t = wave / C; t < tokens; t += w.step) {
+  for (int64_t g = wave / C; g < groups; g += w.step) {
+    const int t0 = GROUP ? (int)g * w.group + p.t0 : (int)g, t = GROUP ? min(t0 + p.tok, a.T - 1) : t0;
+    const bool ok = GROUP ? p.ok && t0 + p.tok < a.T : p.ok;
+    const int64_t og = row(t, a.lddy) + p.col, ox = row(t, a.ldx) + p.col;
     Raw<float, V> dy[4];
     Raw<T, V> in[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int j = p.col + (k & 1 ? half : 0);
-      load<float, V, true>(dy[k], (k & 2 ? a.dy_d : a.dy_m) + t * a.lddy + j);
+      const int j = k & 1 ? half : 0;
+      load<float, V, true>(dy[k], (k & 2 ? a.dy_d : a.dy_m) + og + j);
       if constexpr (NORM)
-        if (p.seg < 2) load<T, V, true>(in[k], (k & 2 ? xd : xm) + t * a.ldx + j);
+        if (p.seg < 2) load<T, V, true>(in[k], (k & 2 ? xd : xm) + ox + j);
     }
     float zm[2 * V], zd[2 * V];
 #pragma unroll
@@ -361,9 +387,13 @@ __global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
       zm[e] = get<float, V>(dy[e / V], e % V);
       zd[e] = get<float, V>(dy[2 + e / V], e % V);
     }
+    if constexpr (NORM && GROUP)
+      if (!ok)   // a token past the last: nothing for the gains' sums
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) zm[e] = zd[e] = 0.f;
     if (p.seg < 2) {
       float c[V], s[V];
-      token_angles<V>(a, (int)t, p.i0, cs[wv], c, s);
+      token_angles<V, GROUP>(a, w, t0, p.ntok, p.tok, p.i0, cs[wv], c, s);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float ml = zm[e], mh = zm[V + e], dl = zd[e], dh = zd[V + e];
@@ -408,8 +438,8 @@ __global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
         }
       }
     }
-    if (p.ok) {
-      const int64_t q = t * a.ldy + p.col;
+    if (ok) {
+      const int64_t q = row(t, a.ldy) + p.col;
       store<T, V, true>(ym + q, zm);
       store<T, V, true>(ym + q + half, zm + V);
       store<T, V, true>(yd + q, zd);
@@ -476,46 +506,56 @@ int group_lanes(int dh, int v) {
   while (v * g < dh / 2) g *= 2;
   return g;
 }
-int pieces(int heads, int dh, int v) { return (int)ceil_div(heads, 64 / group_lanes(dh, v)); }
+int pieces(int64_t heads, int dh, int v) { return (int)ceil_div(heads, 64 / group_lanes(dh, v)); }
 
 QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
   QkSplit w{};
-  w.chunks[0] = pieces(a.Hq, a.dh, v);
-  w.chunks[1] = pieces(a.Hk, a.dh, v);
+  // the group that gives the fewest pieces in all, the smallest such
+  int64_t C = 0, units = INT64_MAX;
+  for (int g = 1; g <= 64 && g <= std::max(1, a.T); g *= 2) {
+    const int64_t c = pieces((int64_t)g * a.Hq, a.dh, v) + (values ? 2 : 1) * (int64_t)pieces((int64_t)g * a.Hk, a.dh, v);
+    const int64_t n = (a.T + g - 1) / g;
+    if (n * c >= units) continue;
+    units = n * c;
+    C = c;
+    w.group = g;
+    w.groups = (int)n;
+  }
+  w.chunks[0] = pieces((int64_t)w.group * a.Hq, a.dh, v);
+  w.chunks[1] = pieces((int64_t)w.group * a.Hk, a.dh, v);
   w.chunks[2] = values ? w.chunks[1] : 0;
   const int nw = (bwd ? BWD_NT : FWD_NT) / 64;
-  const int64_t C = w.chunks[0] + w.chunks[1] + w.chunks[2];
-  // as few steps as the grid allows, the tokens dealt evenly over them
+  // as few steps as the grid allows, the groups dealt evenly over them
   const int64_t at_once = std::max<int64_t>(1, (bwd ? BWD_WAVES : FWD_WAVES) / C);
-  const int64_t steps = std::max<int64_t>(1, (a.T + at_once - 1) / at_once);
-  w.step = (int)((a.T + steps - 1) / steps);
+  const int64_t steps = std::max<int64_t>(1, (w.groups + at_once - 1) / at_once);
+  w.step = (int)((w.groups + steps - 1) / steps);
   w.blocks = (int)((w.step * C + nw - 1) / nw);
+  w.rhalf = (65536 + a.dh / 2 - 1) / (a.dh / 2);   // i * rhalf >> 16 = i / half for i < 512
   return w;
 }
 
+template <typename T, bool BWD, bool NORM, int V, int G>
+void launch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
+  if constexpr (BWD) {
+    if (w.group == 1) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
+    else hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
+  } else {
+    if (w.group == 1) hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
+    else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
+  }
+}
 template <typename T, bool BWD, bool NORM, int V>
 hipError_t dispatch_v(const QkArgs& a, const QkSplit& w, hipStream_t s) {
   if (w.blocks == 0) return hipSuccess;
-#define QK(G)                                                                                                    \
-  case G:                                                                                                        \
-    if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w); \
-    else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);               \
-    break
   switch (group_lanes(a.dh, V)) {
-    QK(1);
-    QK(2);
-    QK(4);
-    QK(8);
-    QK(16);
-    case 32:
-      if constexpr (V == 4) {
-        if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, 32, NORM>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
-        else hipLaunchKernelGGL((qk_fwd_kernel<T, V, 32, NORM>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
-        break;
-      }
-    default: return hipErrorInvalidValue;
+    case 1: launch<T, BWD, NORM, V, 1>(a, w, s); break;
+    case 2: launch<T, BWD, NORM, V, 2>(a, w, s); break;
+    case 4: launch<T, BWD, NORM, V, 4>(a, w, s); break;
+    case 8: launch<T, BWD, NORM, V, 8>(a, w, s); break;
+    case 16: launch<T, BWD, NORM, V, 16>(a, w, s); break;
+    default:   // 32, heads wider than 128
+      if constexpr (V == 4) launch<T, BWD, NORM, V, 32>(a, w, s);
   }
-#undef QK
   return hipGetLastError();
 }
 template <typename T, bool BWD, bool NORM>
@@ -531,9 +571,11 @@ hipError_t dispatch(const QkArgs& a, bool values, QkSplit* out, hipStream_t s) {
 }  // namespace
 
 size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh) {
-  const int64_t C = pieces(Hq, dh, 4) + 2 * (int64_t)pieces(Hk, dh, 4);
-  // (split(): a step of at most max(BWD_WAVES, C) wavefronts)
-  const int64_t waves = std::min<int64_t>(T_ * C, std::max<int64_t>(BWD_WAVES, C));
+  // split(): no more wavefronts than pieces without groups, nor than the larger of
+  // BWD_WAVES and the pieces of one group
+  const int64_t c1 = pieces(Hq, dh, 4) + 2 * (int64_t)pieces(Hk, dh, 4);
+  const int64_t c64 = pieces((int64_t)64 * Hq, dh, 4) + 2 * (int64_t)pieces((int64_t)64 * Hk, dh, 4);
+  const int64_t waves = std::min<int64_t>(T_ * c1, std::max<int64_t>(BWD_WAVES, c64));
   return (size_t)((waves + BWD_NT / 64 - 1) / (BWD_NT / 64)) * 2 * dh * sizeof(double);
 }
 

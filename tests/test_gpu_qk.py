@@ -80,7 +80,7 @@ def test_norm_and_rotation(hq, hk, dh, dtype):
     from paper_2602_00816_amd import fdhvp as fd
     dt, ncol = _dt(torch, dtype), (hq + 2 * hk) * dh
     m = _model(fd, hq, hk, dh, dtype)
-    for i, (B, S, pad) in enumerate([(1, 1, 0), (1, 2, 8), (3, 7, 24), (2, 65, 0), (1, 257, 8)]):
+    for i, (B, S, pad) in enumerate([(1, 1, 0), (1, 2, 8), (3, 7, 24), (2, 65, 0), (1, 257, 8), (70, 1, 0), (43, 3, 8)]):
         x = _pair(torch, B * S, ncol, dt, 10 + i, pad)
         dy = _pair(torch, B * S, ncol, torch.float32, 20 + i, pad, (1e-4, 1e-7))
         gains = _gains(torch, dh, dt, 30 + i, direction=i != 2)
