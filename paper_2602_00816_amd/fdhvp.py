@@ -6,6 +6,7 @@ the current stream.  Loading fails loudly when the library has not been built.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -168,6 +169,14 @@ def _check_vec(t, n: int, what: str, dtypes=("float32",), optional=False):
 def _stream():
     import torch
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _current_stream(dev: int) -> int:
+    """The current stream of a device (torch's own shortcut where it has one: the
+    stream object costs some 3 us)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw else torch.cuda.current_stream(dev).cuda_stream
 
 
 def opts(reorth="full", window=0, basis="f32", tol=0.0) -> LanczosOpts:
@@ -419,7 +428,7 @@ class Model:
             raise ValueError("tensors must lie on the current device")
         if seq < 1 or T % seq:
             raise ValueError("seq must be positive and divide the number of tokens")
-        if torch.cuda.current_stream().cuda_stream != self._stream:
+        if _current_stream(dev) != self._stream:
             raise ValueError("the current stream is not the model's: build the model with stream=<the current stream>")
         g = None
         if gains is not None:
@@ -442,7 +451,7 @@ class Model:
             pos = positions.data_ptr()
         return dev, g, pos, T // seq
 
-    @property
+    @functools.cached_property
     def _qk_dtype(self):
         import torch
         return torch.float32 if self.dtype == "f32" else torch.bfloat16

@@ -269,18 +269,20 @@ def test_accumulate_empty_and_repeated_calls():
     assert all(torch.equal(a, b) for a, b in zip(kept, start))
 
 
-def test_long_batch_sums_and_rows():
-    """More tokens than one run of units per wavefront (several tokens per wavefront,
-    a last workgroup that is not full): sampled rows and the gain gradients."""
+@pytest.mark.parametrize("hq,hk,dh,dtype", [(6, 2, 128, "bf16"), (2, 2, 256, "f32")])
+def test_long_batch_sums_and_rows(hq, hk, dh, dtype):
+    """More tokens than the grid takes at once (several steps per wavefront, a last
+    step and a last workgroup that are not full), heads of several tokens in a wavefront
+    and of one: every row and the gain gradients."""
     torch = need_gpu()
     from paper_2602_00816_amd import fdhvp as fd
-    hq, hk, dh, S = 6, 2, 128, 4099
-    B, ncol = 3, 10 * 128
+    B, S, ncol = 3, 4099, (hq + 2 * hk) * dh
     T = B * S
-    m = _model(fd, hq, hk, dh, "bf16")
-    x = _pair(torch, T, ncol, torch.bfloat16, 1)
+    dt = _dt(torch, dtype)
+    m = _model(fd, hq, hk, dh, dtype)
+    x = _pair(torch, T, ncol, dt, 1)
     dy = _pair(torch, T, ncol, torch.float32, 2)
-    gains = _gains(torch, dh, torch.bfloat16, 3)
+    gains = _gains(torch, dh, dt, 3)
     y = m.qk_forward(x, S, gains=gains, eps=EPS)
     dx, dg = m.qk_backward(dy, S, x=x, gains=gains, eps=EPS)
     want = R.forward(x, hq, hk, dh, R.angles(dh, BASE, T, S), gains, EPS)
@@ -322,6 +324,104 @@ def test_backward_is_the_transpose_of_the_forwards_derivative():
     b = sum(float((d.double() * v.double()).sum()) for d, v in zip(dg, g2[2:])) * EPS * EPS
     size = float((w[0].double() * y2[1].double()).abs().sum())
     assert abs(a - b) <= 40 * R.U32 * size
+
+
+def test_offsets_past_32_bits():
+    """2^20 + 5 tokens of 2048 columns (2^31 elements and more), and three rows 2^30
+    elements apart: rows are independent, so their bits are those of a small call."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    hq, hk, dh = 8, 4, 128
+    ncol, T = 2048, 2 ** 20 + 5
+    m = _model(fd, hq, hk, dh, "bf16")
+    gains = _gains(torch, dh, torch.bfloat16, 3)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    block = 2 ** 16 + 1
+    part = [torch.randn(block, ncol, device="cuda", generator=g) for _ in range(2)]
+    x = tuple(torch.empty(T, ncol, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dy = tuple(torch.empty(T, ncol, device="cuda") for _ in range(2))
+    for i in range(0, T, block):
+        n = min(block, T - i)
+        for k, s in enumerate((1.0, EPS)):
+            x[k][i:i + n] = (part[k][:n] * s).roll(i // block, 1).to(torch.bfloat16)
+            dy[k][i:i + n] = (part[1 - k][:n] * s).roll(i // block, 1)
+    pos = torch.randint(0, 1000, (1, T), dtype=torch.int32, device="cuda", generator=g)
+    y = m.qk_forward(x, T, gains=gains, eps=EPS, positions=pos)
+    dx, dg = m.qk_backward(dy, T, x=x, gains=gains, eps=EPS, positions=pos)
+    for a, b in ((0, 40), (2 ** 19, 2 ** 19 + 33), (T - 70, T)):
+        p = pos[:, a:b].contiguous()
+        ys = m.qk_forward(tuple(t[a:b] for t in x), b - a, gains=gains, eps=EPS, positions=p)
+        dxs, _ = m.qk_backward(tuple(t[a:b] for t in dy), b - a, x=tuple(t[a:b] for t in x), gains=gains, eps=EPS, positions=p)
+        for big, small in zip((*y, *dx), (*ys, *dxs)):
+            assert torch.equal(big[a:b], small)
+    # the gain gradients as a sum over calls: each part and the whole are off by 11
+    # roundings of the terms' absolute values, which the signs' cancellation leaves
+    # well below 1e-3 of the random sums' size
+    acc = [torch.zeros(dh, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for a in range(0, T, 2 ** 18):
+        b = min(T, a + 2 ** 18)
+        _, d = m.qk_backward(tuple(t[a:b] for t in dy), b - a, x=tuple(t[a:b] for t in x), gains=gains, eps=EPS,
+                             positions=pos[:, a:b].contiguous())
+        for k in range(2):
+            acc[k] += d[k].double()
+    for k in range(2):
+        assert float((dg[k].double() - acc[k]).norm()) <= 1e-3 * float(acc[k].norm())
+    del x, dy, y, dx, part
+    # rows far apart
+    ld = 2 ** 30
+    buf = torch.zeros(2 * ld + 4 * ncol, dtype=torch.bfloat16, device="cuda")
+    far = [torch.as_strided(buf, (3, ncol), (ld, 1), j * ncol) for j in range(4)]
+    xs = _pair(torch, 3, ncol, torch.bfloat16, 5)
+    for a, b in zip(far, xs):
+        a.copy_(b)
+    m.qk_forward(tuple(far[:2]), 3, gains=gains, eps=EPS, out=tuple(far[2:]))
+    want = m.qk_forward(xs, 3, gains=gains, eps=EPS)
+    assert all(torch.equal(a, b) for a, b in zip(far[2:], want))
+
+
+def test_shared_inputs_and_plain_positions():
+    """One tensor as mean and half difference (one point is zero), one gain for queries
+    and keys, given positions on a model with one axis."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    hq, hk, dh, T = 4, 2, 64, 21
+    ncol = (hq + 2 * hk) * dh
+    m = _model(fd, hq, hk, dh, "f32")
+    t = _pair(torch, T, ncol, torch.float32, 1)[0]
+    g = _gains(torch, dh, torch.float32, 2)
+    gains = (g[0], g[0], g[2], g[2])
+    pos = torch.randint(-30, 30, (1, 3, 7), dtype=torch.int32, device="cuda")
+    _check_forward(torch, m, (t, t), 7, hq, hk, dh, gains, pos, what="one tensor")
+    dy = _pair(torch, T, ncol, torch.float32, 3)
+    _check_backward(torch, m, (t, t), (dy[0], dy[0]), 7, hq, hk, dh, gains, pos, what="one tensor")
+
+
+def test_calls_on_two_streams_at_once():
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    hq, hk, dh, T = 8, 8, 64, 4000
+    ncol = (hq + 2 * hk) * dh
+    work = []
+    for i in range(2):
+        s = torch.cuda.Stream()
+        m = _model(fd, hq, hk, dh, "bf16", stream=s.cuda_stream)
+        x = _pair(torch, T, ncol, torch.bfloat16, 10 * i)
+        dy = _pair(torch, T, ncol, torch.float32, 10 * i + 1)
+        gains = _gains(torch, dh, torch.bfloat16, 10 * i + 2)
+        with torch.cuda.stream(s):
+            want = m.qk_backward(dy, T, x=x, gains=gains, eps=EPS)
+        torch.cuda.synchronize()
+        work.append((s, m, x, dy, gains, want))
+    got = [[], []]
+    for _ in range(10):
+        for i, (s, m, x, dy, gains, _) in enumerate(work):
+            with torch.cuda.stream(s):
+                got[i].append(m.qk_backward(dy, T, x=x, gains=gains, eps=EPS))
+    torch.cuda.synchronize()
+    for i in range(2):
+        wdx, wdg = work[i][5]
+        for dx, dg in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip((*dx, *dg), (*wdx, *wdg)))
 
 
 def test_rotation_and_back():

@@ -15,6 +15,7 @@ pytestmark = pytest.mark.gpu
 
 EPS = 1e-3
 SMALL = dict(family="llama", n_layers=2, d_model=96, n_heads=6, n_kv_heads=2, d_ff=200, vocab=264, max_seq=40, rope_base=10000.0)
+WIDE = dict(family="llama", n_layers=1, d_model=480, n_heads=2, n_kv_heads=1, d_ff=200, vocab=104, max_seq=24, rope_base=500000.0)
 W64 = dict(family="llama", n_layers=2, d_model=256, n_heads=4, n_kv_heads=2, d_ff=256, vocab=264, max_seq=256, rope_base=10000.0)
 W128 = dict(family="llama", n_layers=2, d_model=256, n_heads=2, n_kv_heads=1, d_ff=256, vocab=264, max_seq=256, rope_base=10000.0)
 
@@ -59,7 +60,7 @@ def _run(torch, fd, w, theta, batches, v, unfused=False, recompute=False, B=None
 
 
 @pytest.mark.parametrize("shape,dtype,B,S,unfused", [
-    (SMALL, "f32", 2, 40, False), (SMALL, "bf16", 2, 40, False), (W64, "bf16", 1, 128, False), (W64, "bf16", 1, 128, True),
+    (SMALL, "f32", 2, 40, False), (WIDE, "f32", 1, 24, False), (SMALL, "bf16", 2, 40, False), (W64, "bf16", 1, 128, False), (W64, "bf16", 1, 128, True),
     (W128, "bf16", 2, 72, False), (W128, "bf16", 2, 72, True), (W128, "bf16", 1, 256, False)])
 @pytest.mark.parametrize("norm,sections,inter,given", [(True, None, False, False), (True, "3", True, True),
                                                        (False, "3", False, True), (False, None, False, True)])
@@ -129,6 +130,58 @@ def test_dataset_recompute_and_lanczos(dtype):
         ao, bo, _ = OL.lanczos(lambda x: OH.lm_hvp_dataset(cfg, theta, x, EPS, batches), q1, mm, OL.FULL)
         lg, lo = (np.sort(np.linalg.eigvalsh(OL.tridiag(p, q))) for p, q in ((a, b), (ao, bo)))
         assert s == mm and abs(lg[-1] - lo[-1]) <= 1e-3 * np.abs(lo).max() and abs(lg[0] - lo[0]) <= 1e-3 * np.abs(lo).max()
+
+
+@pytest.mark.parametrize("S,rows", [(256, 1), (72, 2)])
+def test_recompute_with_fused_attention(S, rows):
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    w = dict(W128, n_layers=3, dtype="bf16", qk_norm=True, rope_sections=(24, 20, 20))
+    theta = _theta(_cfg(w))
+    tok = synth.tokens(2, rows, S, w["vocab"], "zipf")
+    v = synth.gaussian_direction(4, theta.size).astype(np.float32)
+    batches = [(tok, None, _positions(3, rows, S))]
+    a, la, _, _ = _run(torch, fd, w, theta, batches, v)
+    b, lb, _, _ = _run(torch, fd, w, theta, batches, v, recompute=True)
+    assert np.array_equal(a, b) and la == lb
+
+
+def test_cg_and_block_statistics():
+    """The other consumers of the bound operator on a model with the norm: the damped
+    solve's residual, and the layer statistics, whose ranges hold the gains."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    w = dict(SMALL, dtype="f32", qk_norm=True)
+    cfg = _cfg(w)
+    theta = _theta(cfg)
+    tok = synth.tokens(2, 2, 40, w["vocab"], "zipf")
+    mod = fd.Model.from_workload(w)
+    mod.set_workspace(2, 40, 4, fd.opts("none"))
+    th = upload_params(torch, theta, "f32")
+    dt = torch.from_numpy(tok).cuda()
+    mod.bind_dataset(th, [dt], EPS, positions=[torch.from_numpy(_positions(1, 2, 40)).cuda()])
+    b = torch.from_numpy(synth.gaussian_direction(6, theta.size).astype(np.float32)).cuda()
+    # a damping that makes the operator definite: four times the largest of four Ritz values
+    al, be, k, _ = mod.lanczos(4, 3, fd.opts("none"))
+    lam = 4.0 * float(np.abs(np.linalg.eigvalsh(OL.tridiag(al[:k], be[:k]))).max())
+    x, res, s, st = mod.cg_solve(b, lam, 60, 1e-4)
+    r = b - lam * x - mod.hvp_bound(x)
+    say(f"cg: {s} steps, residual {float(r.norm()):.3e}")
+    assert st == 0 and float(r.norm()) <= 2e-3 * float(b.norm())
+    stats = mod.block_stats(b, x)
+    bd = mod.block_diagonal(b)
+    h = mod.hvp_bound(b)
+    for l in range(2):
+        es = [e for e in M.layout(cfg) if e.layer == l]
+        lo, hi = es[0].offset, es[-1].offset + es[-1].numel
+        bb, xx = b[lo:hi].double(), x[lo:hi].double()
+        want = np.array([float(bb @ bb), float(xx @ xx), float(bb @ xx)])
+        assert np.allclose(stats[l], want, rtol=1e-9)
+        vb = torch.zeros_like(b)
+        vb[lo:hi] = b[lo:hi]
+        hb = mod.hvp_bound(vb)
+        diff = float((h[lo:hi].double() - hb[lo:hi].double()).norm())
+        assert abs(bd[l, 0] - diff) <= 1e-4 * diff + 1e-9 and abs(bd[l, 3] - float(h[lo:hi].double().norm())) <= 1e-5 * bd[l, 3]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
