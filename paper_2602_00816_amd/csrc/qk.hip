@@ -33,7 +33,11 @@ namespace {
 
 // threads per workgroup, most wavefronts of a launch (see "Work split")
 constexpr int FWD_NT = 256, FWD_WAVES = 32768;
-constexpr int BWD_NT = 512, BWD_WAVES = 4096;
+constexpr int BWD_WAVES = 4096;
+// (32 lanes per head take 132 to 138 registers in workgroups of 512: one of them per CU.  Held
+// to 128 by a workgroup of 1024, 16 + 16 heads of 192, 256 MB of dy: 218 us against 314; with
+// 16 lanes per head the two are within 2%.)
+constexpr int bwd_threads(int g) { return g == 32 ? 1024 : 512; }
 
 // ---- vectors of V elements ------------------------------------------------------
 // as they lie in memory (4 V or 2 V bytes), so that loads can be held in flight
@@ -349,8 +353,8 @@ __global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
 // Backward.  Every workgroup leaves its sums of the gain gradients' half differences
 // (fp64, fixed order) as rows 2 blockIdx.x (queries) and 2 blockIdx.x + 1 (keys) of part.
 template <typename T, int V, int G, bool NORM, bool GROUP>
-__global__ __launch_bounds__(BWD_NT) void qk_bwd_kernel(QkArgs a, QkSplit w) {
-  constexpr int NW = BWD_NT / 64;
+__global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSplit w) {
+  constexpr int BWD_NT = bwd_threads(G), NW = BWD_NT / 64;
   __shared__ float2 cs[NW][64 * V];   // 64 / G tokens of half <= G V pairs
   __shared__ double sh[NORM ? NW : 1][NORM ? 2 * V * G : 1];
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
@@ -524,7 +528,7 @@ QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
   w.chunks[0] = pieces((int64_t)w.group * a.Hq, a.dh, v);
   w.chunks[1] = pieces((int64_t)w.group * a.Hk, a.dh, v);
   w.chunks[2] = values ? w.chunks[1] : 0;
-  const int nw = (bwd ? BWD_NT : FWD_NT) / 64;
+  const int nw = (bwd ? bwd_threads(group_lanes(a.dh, v)) : FWD_NT) / 64;
   // as few steps as the grid allows, the groups dealt evenly over them
   const int64_t at_once = std::max<int64_t>(1, (bwd ? BWD_WAVES : FWD_WAVES) / C);
   const int64_t steps = std::max<int64_t>(1, (w.groups + at_once - 1) / at_once);
@@ -537,8 +541,8 @@ QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
 template <typename T, bool BWD, bool NORM, int V, int G>
 void launch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
   if constexpr (BWD) {
-    if (w.group == 1) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
-    else hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(BWD_NT), 0, s, a, w);
+    if (w.group == 1) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(bwd_threads(G)), 0, s, a, w);
+    else hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(bwd_threads(G)), 0, s, a, w);
   } else {
     if (w.group == 1) hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
     else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
@@ -576,7 +580,8 @@ size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh) {
   const int64_t c1 = pieces(Hq, dh, 4) + 2 * (int64_t)pieces(Hk, dh, 4);
   const int64_t c64 = pieces((int64_t)64 * Hq, dh, 4) + 2 * (int64_t)pieces((int64_t)64 * Hk, dh, 4);
   const int64_t waves = std::min<int64_t>(T_ * c1, std::max<int64_t>(BWD_WAVES, c64));
-  return (size_t)((waves + BWD_NT / 64 - 1) / (BWD_NT / 64)) * 2 * dh * sizeof(double);
+  const int nw = bwd_threads(group_lanes(dh, 4)) / 64;
+  return (size_t)((waves + nw - 1) / nw) * 2 * dh * sizeof(double);
 }
 
 template <typename T>
