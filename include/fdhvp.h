@@ -148,8 +148,8 @@ typedef struct fdh_ctx fdh_ctx;
  * hipStream_t (NULL = default stream).  *out receives the context. */
 fdh_status fdh_create(const fdh_model_config* cfg, void* hip_stream, fdh_ctx** out);
 /* fdh_create with a per-head norm of queries and keys and position axes (Llama
- * family, head_dim <= 256: FDH_ERR_UNSUPPORTED otherwise; FDH_ERR_INVALID_ARG for
- * sections that do not divide the pairs).  qk NULL or all zero is fdh_create. */
+ * family, head_dim <= 256, n_heads <= 65536: FDH_ERR_UNSUPPORTED otherwise; FDH_ERR_INVALID_ARG
+ * for sections that do not divide the pairs).  qk NULL or all zero is fdh_create. */
 fdh_status fdh_create_qk(const fdh_model_config* cfg, const fdh_qk_config* qk, void* hip_stream, fdh_ctx** out);
 void fdh_destroy(fdh_ctx* ctx);
 int32_t fdh_api_version(void);
@@ -248,7 +248,8 @@ fdh_status fdh_bind_dataset_positions(fdh_ctx* ctx, const void* params_dev, cons
                                       const int32_t* const* positions, int32_t nbatch, double eps, int32_t reduction,
                                       int64_t* n_targets);
 
-/* The q/k front of a layer on caller-owned device memory, as the HVP runs it:
+/* The q/k front of a layer on caller-owned device memory, as the HVP runs it, for contexts of
+ * the Llama family with head_dim <= 256 and n_heads <= 65536 (else FDH_ERR_UNSUPPORTED):
  * every tensor is a pair, _m the mean and _d the half difference of its values
  * at two points.  x: the q/k/v projection's output, B*S rows of
  * (n_heads + 2 n_kv_heads) head_dim elements of the context's dtype (query heads,

@@ -60,7 +60,7 @@ fdh_status validate_qk(const fdh_model_config* cfg, const fdh_qk_config* qk) {
   if (!qk->norm && !qk->n_axes) return FDH_OK;
   if (cfg->family != FDH_FAMILY_LLAMA) return FDH_ERR_UNSUPPORTED;
   const int half = cfg->d_model / cfg->n_heads / 2;
-  if (2 * half > fdh::QK_MAX_DH) return FDH_ERR_UNSUPPORTED;
+  if (2 * half > fdh::QK_MAX_DH || cfg->n_heads > fdh::QK_MAX_HEADS) return FDH_ERR_UNSUPPORTED;
   if (!qk->n_axes) return FDH_OK;
   int64_t sum = 0;
   for (int a = 0; a < qk->n_axes; ++a) {
@@ -228,7 +228,7 @@ fdh_status fdh_bind_dataset_positions(fdh_ctx* ctx, const void* params_dev, cons
 fdh_status fdh_qk_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes) {
   if (!ctx || !ctx->eng || !bytes || B < 0 || S < 0) return FDH_ERR_INVALID_ARG;
   const fdh::Engine& e = *ctx->eng;
-  if (!e.llama || e.dh > fdh::QK_MAX_DH || (int64_t)B * S > fdh::QK_MAX_TOKENS) return FDH_ERR_UNSUPPORTED;
+  if (!e.llama || e.dh > fdh::QK_MAX_DH || e.Hq > fdh::QK_MAX_HEADS || (int64_t)B * S > fdh::QK_MAX_TOKENS) return FDH_ERR_UNSUPPORTED;
   *bytes = e.qk_norm ? fdh::qk_scratch_bytes((int64_t)B * S, e.Hq, e.Hk, e.dh) : 0;
   return FDH_OK;
 }

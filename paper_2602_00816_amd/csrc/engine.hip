@@ -1174,8 +1174,8 @@ int Engine::bind_batches(const void* params, const BatchRef* bt, int nb, double 
   for (int i = 0; i < nb; ++i) {
     const int rc = check_batch(bt[i].tok, bt[i].B, bt[i].S);
     if (rc != FDH_OK) return rc;
-    if (bt[i].pos && (!llama || dh > QK_MAX_DH)) {
-      err = "positions need the Llama family and head_dim <= 256";
+    if (bt[i].pos && (!llama || dh > QK_MAX_DH || Hq > QK_MAX_HEADS)) {
+      err = "positions need the Llama family, head_dim <= 256 and n_heads <= 65536";
       return FDH_ERR_UNSUPPORTED;
     }
   }
@@ -1272,7 +1272,7 @@ bool bad_rows(const void* p, int64_t ld, int64_t cols, int size) {
 // the shape and gains of a call, shared by both directions
 int Engine::qk_check(const fdh_qk_gains* g, int B, int S, QkArgs* a) {
   if (!llama) { err = "needs a Llama-family context"; return FDH_ERR_UNSUPPORTED; }
-  if (dh > QK_MAX_DH) { err = "head_dim must be <= 256"; return FDH_ERR_UNSUPPORTED; }
+  if (dh > QK_MAX_DH || Hq > QK_MAX_HEADS) { err = "head_dim must be <= 256 and n_heads <= 65536"; return FDH_ERR_UNSUPPORTED; }
   if (B < 0 || S < 0) { err = "B and S must not be negative"; return FDH_ERR_INVALID_ARG; }
   if ((int64_t)B * S > QK_MAX_TOKENS) { err = "B*S must be <= 2^31 - 64"; return FDH_ERR_UNSUPPORTED; }
   if (qk_norm) {

@@ -176,7 +176,7 @@ hipError_t launch_qkv_bwd_post(PairT<T> out, float* gm, float* gd, int T_, int S
 hipError_t launch_rope_table(double* cs, int S, int dh, double base, hipStream_t s);
 
 // ---- qk.hip: per-head norm and position rotation of the q and k columns ----------
-constexpr int QK_MAX_DH = 256;
+constexpr int QK_MAX_DH = 256, QK_MAX_HEADS = 65536;
 constexpr int64_t QK_MAX_TOKENS = ((int64_t)1 << 31) - 64;   // (a group of 64 tokens stays an int)
 // pair i of a head (elements i, i + dh/2) turns by 2 pi freq[i] pos[axis[i]]
 struct QkRotary {
