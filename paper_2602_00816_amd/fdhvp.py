@@ -221,7 +221,7 @@ class Model:
             raise FdhError(st, "fdh_create rejected the configuration")
         self.qk_norm, self.n_axes = bool(qk_norm), max(1, len(sec))
         self._stream = int(getattr(stream, "value", stream) or 0)
-        self._qk_dh = d_model // n_heads
+        self._qk_dh = d_model // max(1, n_heads)
         self._qk_cols = (n_heads + 2 * (n_kv_heads or n_heads)) * self._qk_dh
         self._h = h
         self._ws = None
@@ -514,6 +514,8 @@ class Model:
                     raise ValueError(f"gain_grads must be contiguous float32 tensors of {self._qk_dh} elements")
             if scratch is None:
                 scratch = self.qk_scratch(B, seq)
+            elif not scratch.is_contiguous():
+                raise ValueError("scratch must be contiguous")
             for t in (*dg, scratch):
                 if t is not None and t.get_device() != dev:
                     raise ValueError("tensors must lie on the current device")

@@ -520,5 +520,7 @@ def test_binding_refusals_on_the_device():
         m.qk_backward(dy, 4, gains=gains)
     with pytest.raises(ValueError, match="gain_grads"):
         m.qk_backward(dy, 4, x=x, gains=gains, accumulate=True)
+    with pytest.raises(ValueError, match="scratch"):
+        m.qk_backward(dy, 4, x=x, gains=gains, scratch=torch.empty(1 << 16, dtype=torch.uint8, device="cuda")[::2])
     with pytest.raises(fd.FdhError, match="scratch"):
         m.qk_backward(dy, 4, x=x, gains=gains, scratch=torch.empty(8, dtype=torch.uint8, device="cuda"))

@@ -252,6 +252,27 @@ def test_front_as_the_layer_runs_it():
         assert err <= 1e-4      # fp32 pairs: some ten steps of 2^-24 over an eps of 1e-3
 
 
+def test_bind_refuses_positions_of_another_shape():
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    w = dict(SMALL, dtype="f32", rope_sections=(3, 3, 2))
+    mod = fd.Model.from_workload(w)
+    mod.set_workspace(2, 40)
+    th = mod.init_params(1)
+    tok = mod.make_tokens(2, 40, 2)
+    good = torch.zeros(3, 2, 40, dtype=torch.int32, device="cuda")
+    assert mod.bind_dataset(th, [tok], EPS, positions=[good]) == 2 * 39
+    for bad in (good[:2], good.transpose(1, 2), good[:, :, :39], good.long(), good.cpu(), good.reshape(3, 80), good[:, :, ::2]):
+        with pytest.raises(ValueError, match="positions"):
+            mod.bind_dataset(th, [tok], EPS, positions=[bad])
+    with pytest.raises(ValueError, match="positions"):
+        mod.bind_dataset(th, [tok], EPS, positions=[good, None])
+    gpt = fd.Model("gpt2", 1, 64, 4, 4, 64, 32, 64)
+    gpt.set_workspace(2, 40)
+    with pytest.raises(fd.FdhError, match="positions"):
+        gpt.bind_dataset(gpt.init_params(1), [gpt.make_tokens(2, 40, 2)], EPS, positions=[good[:1].contiguous()])
+
+
 def test_slq_command_with_norm_and_axes(monkeypatch, tmp_path):
     """The command on a small Llama workload: its Ritz values and trace estimate
     against the oracle's Lanczos run."""

@@ -68,6 +68,13 @@ def test_layout_matches_oracle(sections):
     assert m.workspace_bytes(2, 64) - plain.workspace_bytes(2, 64) >= 3 * 2 * 128 * 8 * 24 * 4
 
 
+def test_models_without_heads_are_made_as_before():
+    assert fd.Model("quad_diag", quad_n=10).num_params == 10
+    assert fd.Model("quad_diag", n_heads=0, quad_n=10).num_params == 10
+    with pytest.raises(fd.FdhError):
+        fd.Model("llama", 1, 96, 0, 0, 64, 32, 64)
+
+
 def test_interleaved_axes():
     cfg = M.ModelConfig("llama", 1, 96, 4, 64, 32, 64, rope_sections=(6, 4, 2), rope_interleaved=True)
     assert M.axis_of_pairs(cfg).tolist() == [0, 1, 2, 0, 1, 2, 0, 1, 0, 0, 1, 0]
