@@ -23,9 +23,9 @@
 //
 // Memory-bound: 8 bytes per bf16 element forward and 16 backward against some 30 and 45
 // vector instructions.  One layer of 16 + 16 + 16 heads of 128 at 8192 tokens, bf16:
-// forward 76 us (403 MB, 5.3 TB/s), backward 145 us with the gains' sums (738 MB, 5.1 TB/s);
-// rotation alone of 32 + 8 + 8 heads at 16384 tokens 147 us (805 MB, 5.5 TB/s).  A plain
-// copy of as many bytes runs at 6.0 TB/s; the vector units are busy for half the time.
+// forward 76 us (403 MB, 5.3 TB/s), backward 142 us with the gains' sums (738 MB, 5.2 TB/s);
+// rotation alone of 32 + 8 + 8 heads at 16384 tokens 143 us (805 MB, 5.6 TB/s).  A plain
+// copy of as many bytes runs at 6.0 TB/s; the vector units are busy for less than half the time.
 #include "kernels.h"
 
 #include <algorithm>
@@ -34,13 +34,10 @@ namespace fdh {
 
 namespace {
 
-// Threads per workgroup and most wavefronts of a launch (see "Work split").  Forward:
-// short runs, which the scheduler interleaves (the layer above: 76 us; 84 us with 8192
-// wavefronts, 86 with loads ahead of the arithmetic in longer runs).  Backward: as many as
-// are resident at once (four per SIMD at 126 registers), as each workgroup leaves a row of
-// gain sums: 145 us; 154 with 8192, 187 with 32768.
-constexpr int FWD_NT = 256, FWD_WAVES = 32768;
-constexpr int BWD_WAVES = 4096;
+// Threads per workgroup; most wavefronts of a backward with gains: as many as are resident
+// at once (four per SIMD at 126 registers), as each workgroup leaves a row of gain sums (the
+// layer above: 145 us with 4096, 154 with 8192, 187 with 32768).
+constexpr int FWD_NT = 256, BWD_WAVES = 4096;
 // (32 lanes per head take 132 to 138 registers in workgroups of 512: one of them per CU.  Held
 // to 128 by a workgroup of 1024, 16 + 16 heads of 192, 256 MB of dy: 218 us against 314; with
 // 16 lanes per head the two are within 2%.)
@@ -524,7 +521,7 @@ int group_lanes(int dh, int v) {
 }
 int pieces(int64_t heads, int dh, int v) { return (int)ceil_div(heads, 64 / group_lanes(dh, v)); }
 
-QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
+QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   QkSplit w{};
   // The group that gives the fewest pieces in all, the smallest such.  (8 + 1 + 1 heads of
   // 128, bf16, 16384 tokens, forward: 46 us in groups of 8, 57 without.  One token per piece
@@ -544,10 +541,28 @@ QkSplit split(const QkArgs& a, int v, bool bwd, bool values) {
   w.chunks[1] = pieces((int64_t)w.group * a.Hk, a.dh, v);
   w.chunks[2] = values ? w.chunks[1] : 0;
   const int nw = (bwd ? bwd_threads(group_lanes(a.dh, v)) : FWD_NT) / 64;
-  // as few steps as the grid allows, the groups dealt evenly over them
-  const int64_t at_once = std::max<int64_t>(1, (bwd ? BWD_WAVES : FWD_WAVES) / C);
-  const int64_t steps = std::max<int64_t>(1, (w.groups + at_once - 1) / at_once);
-  w.step = (int)((w.groups + steps - 1) / steps);
+  // Groups per wavefront.  Backward with the norm: as few as a resident grid leaves.  Elsewhere
+  // short runs: many wavefronts, which the scheduler interleaves and which walk through memory
+  // closer to its order (the layer above forward 76 us, 84 with the 8 to 12 of a resident grid;
+  // rotation alone, backward: 98 against 109).  The norm pays for its gains with two tokens per
+  // wavefront in bf16 (65536 tokens: 562 us, 587 with one, 593 with four; fp32, 16384: 96 with
+  // one, 100 with two), and with twice as many where a quarter or more of the lanes are idle
+  // (80-wide bf16 heads: 115 us with four, 128 with two), four times in heads wider than 128
+  // (136-wide in fp32: 118 us with four, 127 with two; 96-wide: 102 with four, 97 with two).
+  // Up to SHORT units the chip is not full: one.
+  constexpr int64_t SHORT = 16384, MOST = (int64_t)1 << 25;   // (a launch has fewer than 2^32 threads)
+  int64_t step;
+  if (bwd && a.gq) {
+    // full steps of the resident grid and a rest (dealt evenly, 2048 tokens took seven steps of 293 where
+    // six of 341 and one of 2 do: 46.0 us against 44.8; the layer above 145.8 against 141.3)
+    step = std::max<int64_t>(1, BWD_WAVES / C);
+  } else {
+    const int lanes = group_lanes(a.dh, v);
+    const bool idle = 2 * a.dh <= 3 * lanes * v;
+    const int64_t run = !a.gq || units <= SHORT ? 1 : (bf16 ? 2 : 1) * (!idle ? 1 : a.dh > 128 ? 4 : 2);
+    step = std::min((w.groups + run - 1) / run, std::max<int64_t>(1, MOST / C));
+  }
+  w.step = (int)std::min<int64_t>(w.groups, step);
   w.blocks = (int)((w.step * C + nw - 1) / nw);
   w.rhalf = (65536 + a.dh / 2 - 1) / (a.dh / 2);   // i * rhalf >> 16 = i / half for i < 512
   return w;
@@ -582,7 +597,7 @@ hipError_t dispatch_v(const QkArgs& a, const QkSplit& w, hipStream_t s) {
 template <typename T, bool BWD, bool NORM>
 hipError_t dispatch(const QkArgs& a, bool values, QkSplit* out, hipStream_t s) {
   const int v = lane_pairs<T, BWD>(a.dh);
-  const QkSplit w = split(a, v, BWD, values);
+  const QkSplit w = split(a, v, sizeof(T) == 2, BWD, values);
   if (out) *out = w;
   if constexpr (!BWD && sizeof(T) == 2)
     if (v == 8) return dispatch_v<T, BWD, NORM, 8>(a, w, s);

@@ -379,6 +379,77 @@ def test_offsets_past_32_bits():
     assert all(torch.equal(a, b) for a, b in zip(far[2:], want))
 
 
+@pytest.mark.parametrize("hq,hk,dh", [(3, 1, 24), (5, 5, 48), (9, 3, 72), (17, 1, 96), (3, 3, 144), (2, 1, 168), (6, 2, 192)])
+def test_widths_of_twelves(hq, hk, dh):
+    """bf16 heads that divide into six pairs per lane."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    for norm in (True, False):
+        m = _model(fd, hq, hk, dh, "bf16", norm)
+        for i, (B, S, pad) in enumerate([(1, 1, 0), (3, 7, 24), (1, 257, 8), (70, 1, 0)]):
+            x = _pair(torch, B * S, (hq + 2 * hk) * dh, torch.bfloat16, 40 + i, pad)
+            gains = _gains(torch, dh, torch.bfloat16, 50 + i, direction=i != 1) if norm else None
+            what = f"{hq}/{hk} heads of {dh}, {B}x{S}{' norm' if norm else ''}"
+            say(what)
+            _check_forward(torch, m, x, S, hq, hk, dh, gains, None, what=what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("hq,hk,dh", [(64, 64, 16), (5, 1, 64), (40, 8, 72), (32, 8, 80), (16, 4, 128), (14, 2, 136), (12, 4, 144),
+                                      (12, 4, 192), (4, 1, 256)])
+def test_runs_of_tokens(hq, hk, dh, norm, dtype):
+    """Batches long enough for several tokens (or groups of them) per wavefront, the last
+    run cut short: rows are independent, so their bits are those of a shorter call."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    T, ncol, n = 64 * 173 + 5, (hq + 2 * hk) * dh, 64 * 7   # (parts of whole groups of tokens)
+    dt = _dt(torch, dtype)
+    m = _model(fd, hq, hk, dh, dtype, norm)
+    g = torch.Generator(device="cuda").manual_seed(dh)
+    gains = _gains(torch, dh, dt, 3) if norm else None
+    x = tuple((torch.randn(T, ncol, device="cuda", generator=g) * s).to(dt) for s in (1.0, EPS))
+    dy = tuple(torch.randn(T, ncol, device="cuda", generator=g) * s for s in (1.0, EPS))
+    pos = torch.randint(0, 5000, (1, T), dtype=torch.int32, device="cuda", generator=g)
+    say(f"{hq}/{hk} heads of {dh}, {T} tokens {dtype}{' norm' if norm else ''}")
+    y = m.qk_forward(x, T, gains=gains, eps=EPS, positions=pos)
+    dx = m.qk_backward(dy, T, x=x if norm else None, gains=gains, eps=EPS, positions=pos)
+    dx = dx[0] if norm else dx
+    for a in (*range(0, T - n, n), T - n):
+        b = a + n
+        p = pos[:, a:b].contiguous()
+        ys = m.qk_forward(tuple(t[a:b] for t in x), b - a, gains=gains, eps=EPS, positions=p)
+        ds = m.qk_backward(tuple(t[a:b] for t in dy), b - a, x=tuple(t[a:b] for t in x) if norm else None, gains=gains, eps=EPS,
+                           positions=p)
+        for big, small in zip((*y, *dx), (*ys, *(ds[0] if norm else ds))):
+            assert torch.equal(big[a:b], small), (a, b)
+
+
+def test_more_wavefronts_than_a_launch_holds():
+    """2^21 + 2^12 tokens of 62 + 2 heads of 136, in place: at one token per
+    wavefront 32 of them a token, 2^26 and more, above the 2^32 threads of a launch."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    hq, hk, dh = 62, 2, 136
+    S, B = 2 ** 12, 2 ** 9 + 1
+    T, ncol = S * B, (hq + 2 * hk) * dh
+    if torch.cuda.mem_get_info()[0] < 4 * T * ncol + 2 ** 32:
+        pytest.skip("80 GB of free memory needed")
+    m = _model(fd, hq, hk, dh, "bf16", norm=False)
+    x = tuple(torch.zeros(T, ncol, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rows = _pair(torch, 2 * S, ncol, torch.bfloat16, 9)
+    want = m.qk_forward(rows, S)
+    at = (0, T // 2 // S * S, T - 2 * S)
+    for a in at:
+        for t, r in zip(x, rows):
+            t[a:a + 2 * S] = r
+    y = m.qk_forward(x, S, out=x)
+    for a in at:
+        assert all(torch.equal(t[a:a + 2 * S], w) for t, w in zip(y, want)), a
+    del x, y
+    torch.cuda.empty_cache()
+
+
 def test_shared_inputs_and_plain_positions():
     """One tensor as mean and half difference (one point is zero), one gain for queries
     and keys, given positions on a model with one axis."""
