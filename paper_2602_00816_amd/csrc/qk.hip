@@ -45,11 +45,14 @@ constexpr int bwd_threads(int g) { return g == 32 ? 1024 : 512; }
 
 // ---- vectors of V elements ------------------------------------------------------
 // as they lie in memory (4 V or 2 V bytes), so that loads can be held in flight
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// (N words by fours, twos or, at their own alignment, threes)
+template <int K> struct Words;
+template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Words<3> { typedef uint32_t type __attribute__((ext_vector_type(3), aligned(4))); };
+template <> struct Words<4> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <typename T, int V>
 struct Raw {
-  static constexpr int N = V * sizeof(T) / 4;
+  static constexpr int N = V * sizeof(T) / 4, K = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 3;   // words, words of an access
   uint32_t w[N];
 };
 // STREAM: nontemporal accesses, in the backward, which reads dy and x for the last time: the
@@ -57,18 +60,16 @@ struct Raw {
 // stores alone; in the forward the loads cost 2 us.
 template <typename T, int V, bool STREAM = false>
 __device__ inline void load(Raw<T, V>& r, const T* p) {
-  constexpr int N = Raw<T, V>::N;
-  if constexpr (N % 4 == 0) {
+  constexpr int N = Raw<T, V>::N, K = Raw<T, V>::K;
+  typedef typename Words<K>::type W;
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const u32x4* q = reinterpret_cast<const u32x4*>(p + i * 4 / sizeof(T));
-      const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
-      r.w[i] = v[0]; r.w[i + 1] = v[1]; r.w[i + 2] = v[2]; r.w[i + 3] = v[3];
-    }
-  } else {
-    const u32x2* q = reinterpret_cast<const u32x2*>(p);
-    const u32x2 v = STREAM ? __builtin_nontemporal_load(q) : *q;
-    r.w[0] = v[0]; r.w[1] = v[1];
+  for (int i = 0; i < N; i += K) {
+    const W* q = reinterpret_cast<const W*>(p + i * 4 / sizeof(T));
+    W v;
+    if constexpr (STREAM) v = __builtin_nontemporal_load(q);
+    else v = *q;
+#pragma unroll
+    for (int k = 0; k < K; ++k) r.w[i + k] = v[k];
   }
 }
 template <typename T, int V>
@@ -79,23 +80,17 @@ __device__ inline float get(const Raw<T, V>& r, int e) {
 template <typename T, int V, bool STREAM = false>
 __device__ inline void store(T* p, const float* x) {
   Raw<T, V> r;
-  constexpr int N = Raw<T, V>::N;
+  constexpr int N = Raw<T, V>::N, K = Raw<T, V>::K;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if constexpr (sizeof(T) == 4) r.w[i] = __builtin_bit_cast(uint32_t, x[i]);
     else r.w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
   }
-  if constexpr (N % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const u32x4 v = {r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]};
-      u32x4* q = reinterpret_cast<u32x4*>(p + i * 4 / sizeof(T));
-      if constexpr (STREAM) __builtin_nontemporal_store(v, q);
-      else *q = v;
-    }
-  } else {
-    const u32x2 v = {r.w[0], r.w[1]};
-    u32x2* q = reinterpret_cast<u32x2*>(p);
+  for (int i = 0; i < N; i += K) {
+    typename Words<K>::type v, *q = reinterpret_cast<typename Words<K>::type*>(p + i * 4 / sizeof(T));
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = r.w[i + k];
     if constexpr (STREAM) __builtin_nontemporal_store(v, q);
     else *q = v;
   }
@@ -507,17 +502,25 @@ __global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, int r
   *out = acc ? (float)((double)*out + t) : (float)t;
 }
 
-// Pairs per lane: 8 (16-byte accesses) in the bf16 forward where a head divides into
-// them, 4 otherwise.  8192 tokens of 48 heads of 128, norm: 76 us against 78 with 4;
-// 16384, rotation alone: 147 against 152.  In the backward 8 leaves two wavefronts per
-// SIMD (204 registers): 155 us against 145.
-template <typename T, bool BWD>
-int lane_pairs(int dh) { return !BWD && sizeof(T) == 2 && dh % 16 == 0 ? 8 : 4; }
 // lanes per head
 int group_lanes(int dh, int v) {
   int g = 1;
   while (v * g < dh / 2) g *= 2;
   return g;
+}
+// Pairs per lane: 4; in the bf16 forward 8 or 6 where a head divides into them (accesses of
+// 16 or 12 bytes), the number that leaves the fewest lanes idle, the larger of two alike.  The layer
+// above: 76 us with 8, 78 with 4; 16 + 4 + 4 heads of 256, 104 against 114; with the norm, 72-wide
+// heads take 115 us with 6 and 150 with 4, 144-wide ones 128 with 6 and 139 with 8, 96-wide ones
+// 109 with either.  In fp32 6 is slower (96-wide 104 us, 98 with 4), and so is more than 4 in
+// the backward: 8 leaves two wavefronts per SIMD (204 registers), 155 us against 145.
+template <typename T, bool BWD>
+int lane_pairs(int dh) {
+  int v = 4;
+  if (!BWD && sizeof(T) == 2)
+    for (int c = 6; c <= 8; c += 2)
+      if (dh / 2 % c == 0 && c * group_lanes(dh, c) <= v * group_lanes(dh, v)) v = c;
+  return v;
 }
 int pieces(int64_t heads, int dh, int v) { return (int)ceil_div(heads, 64 / group_lanes(dh, v)); }
 
@@ -581,12 +584,19 @@ void launch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
 template <typename T, bool BWD, bool NORM, int V>
 hipError_t dispatch_v(const QkArgs& a, const QkSplit& w, hipStream_t s) {
   if (w.blocks == 0) return hipSuccess;
+  // (widths that reach no other count: the bf16 forward takes 4 pairs per lane at 8, 40, 56 and
+  // other odd multiples of 8 alone, and 6 at 24, 48, 72, 96, 144, 168 and 192)
+  constexpr bool ALL = BWD || sizeof(T) == 4;
   switch (group_lanes(a.dh, V)) {
-    case 1: launch<T, BWD, NORM, V, 1>(a, w, s); break;
-    case 2:   // (bf16 heads of 16 take 8 pairs per lane in the forward)
-      if constexpr (BWD || sizeof(T) == 4 || V == 8) launch<T, BWD, NORM, V, 2>(a, w, s);
+    case 1:
+      if constexpr (V != 6) launch<T, BWD, NORM, V, 1>(a, w, s);
       break;
-    case 4: launch<T, BWD, NORM, V, 4>(a, w, s); break;
+    case 2:
+      if constexpr (ALL || V != 4) launch<T, BWD, NORM, V, 2>(a, w, s);
+      break;
+    case 4:
+      if constexpr (ALL || V != 4) launch<T, BWD, NORM, V, 4>(a, w, s);
+      break;
     case 8: launch<T, BWD, NORM, V, 8>(a, w, s); break;
     case 16: launch<T, BWD, NORM, V, 16>(a, w, s); break;
     default:   // 32, heads wider than 128
@@ -599,8 +609,10 @@ hipError_t dispatch(const QkArgs& a, bool values, QkSplit* out, hipStream_t s) {
   const int v = lane_pairs<T, BWD>(a.dh);
   const QkSplit w = split(a, v, sizeof(T) == 2, BWD, values);
   if (out) *out = w;
-  if constexpr (!BWD && sizeof(T) == 2)
+  if constexpr (!BWD && sizeof(T) == 2) {
     if (v == 8) return dispatch_v<T, BWD, NORM, 8>(a, w, s);
+    if (v == 6) return dispatch_v<T, BWD, NORM, 6>(a, w, s);
+  }
   return dispatch_v<T, BWD, NORM, 4>(a, w, s);
 }
 
