@@ -23,7 +23,7 @@
 //
 // Memory-bound: 8 bytes per bf16 element forward and 16 backward against some 30 and 45
 // vector instructions.  One layer of 16 + 16 + 16 heads of 128 at 8192 tokens, bf16:
-// forward 76 us (403 MB, 5.3 TB/s), backward 142 us with the gains' sums (738 MB, 5.2 TB/s);
+// forward 76 us (403 MB, 5.3 TB/s), backward 140 us with the gains' sums (738 MB, 5.2 TB/s);
 // rotation alone of 32 + 8 + 8 heads at 16384 tokens 143 us (805 MB, 5.6 TB/s).  A plain
 // copy of as many bytes runs at 6.0 TB/s; the vector units are busy for less than half the time.
 #include "kernels.h"
@@ -45,32 +45,47 @@ constexpr int bwd_threads(int g) { return g == 32 ? 1024 : 512; }
 
 // ---- vectors of V elements ------------------------------------------------------
 // as they lie in memory (4 V or 2 V bytes), so that loads can be held in flight
-// (N words by fours, twos or, at their own alignment, threes)
-template <int K> struct Words;
-template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
-template <> struct Words<3> { typedef uint32_t type __attribute__((ext_vector_type(3), aligned(4))); };
-template <> struct Words<4> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x3 __attribute__((ext_vector_type(3), aligned(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T, int V>
 struct Raw {
-  static constexpr int N = V * sizeof(T) / 4, K = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 3;   // words, words of an access
+  static constexpr int N = V * sizeof(T) / 4;
   uint32_t w[N];
 };
 // STREAM: nontemporal accesses, in the backward, which reads dy and x for the last time: the
-// layer above takes 145 us with them, 158 without, 157 with the loads alone, 151 with the
-// stores alone; in the forward the loads cost 2 us.
-template <typename T, int V, bool STREAM = false>
-__device__ inline void load(Raw<T, V>& r, const T* p) {
-  constexpr int N = Raw<T, V>::N, K = Raw<T, V>::K;
-  typedef typename Words<K>::type W;
+// layer above takes 141 us with them, 154 with the loads alone; 32 + 8 + 8 heads of 128 in fp32,
+// 5456 tokens, 143 and 154.  In the forward the loads cost 2 us.  (A store whose vector is
+// filled element by element, or through a dependent type, loses the hint in hipcc.)
+__device__ inline u32x2 words(const uint32_t* w, u32x2) { return {w[0], w[1]}; }
+__device__ inline u32x3 words(const uint32_t* w, u32x3) { return {w[0], w[1], w[2]}; }
+__device__ inline u32x4 words(const uint32_t* w, u32x4) { return {w[0], w[1], w[2], w[3]}; }
+template <typename W, int K, int N, bool STREAM>
+__device__ inline void load_words(uint32_t (&w)[N], const void* p) {
 #pragma unroll
   for (int i = 0; i < N; i += K) {
-    const W* q = reinterpret_cast<const W*>(p + i * 4 / sizeof(T));
-    W v;
-    if constexpr (STREAM) v = __builtin_nontemporal_load(q);
-    else v = *q;
+    const W* q = reinterpret_cast<const W*>((const uint32_t*)p + i);
+    const W v = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
-    for (int k = 0; k < K; ++k) r.w[i + k] = v[k];
+    for (int k = 0; k < K; ++k) w[i + k] = v[k];
   }
+}
+template <typename W, int K, int N, bool STREAM>
+__device__ inline void store_words(const uint32_t (&w)[N], void* p) {
+#pragma unroll
+  for (int i = 0; i < N; i += K) {
+    W* q = reinterpret_cast<W*>((uint32_t*)p + i);
+    const W v = words(w + i, W{});
+    if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+    else *q = v;
+  }
+}
+template <typename T, int V, bool STREAM = false>
+__device__ inline void load(Raw<T, V>& r, const T* p) {
+  constexpr int N = Raw<T, V>::N;
+  if constexpr (N % 4 == 0) load_words<u32x4, 4, N, STREAM>(r.w, p);
+  else if constexpr (N % 2 == 0) load_words<u32x2, 2, N, STREAM>(r.w, p);
+  else load_words<u32x3, 3, N, STREAM>(r.w, p);
 }
 template <typename T, int V>
 __device__ inline float get(const Raw<T, V>& r, int e) {
@@ -80,20 +95,15 @@ __device__ inline float get(const Raw<T, V>& r, int e) {
 template <typename T, int V, bool STREAM = false>
 __device__ inline void store(T* p, const float* x) {
   Raw<T, V> r;
-  constexpr int N = Raw<T, V>::N, K = Raw<T, V>::K;
+  constexpr int N = Raw<T, V>::N;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if constexpr (sizeof(T) == 4) r.w[i] = __builtin_bit_cast(uint32_t, x[i]);
     else r.w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
   }
-#pragma unroll
-  for (int i = 0; i < N; i += K) {
-    typename Words<K>::type v, *q = reinterpret_cast<typename Words<K>::type*>(p + i * 4 / sizeof(T));
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = r.w[i + k];
-    if constexpr (STREAM) __builtin_nontemporal_store(v, q);
-    else *q = v;
-  }
+  if constexpr (N % 4 == 0) store_words<u32x4, 4, N, STREAM>(r.w, p);
+  else if constexpr (N % 2 == 0) store_words<u32x2, 2, N, STREAM>(r.w, p);
+  else store_words<u32x3, 3, N, STREAM>(r.w, p);
 }
 
 // ---- sums over aligned groups of G lanes ------------------------------------------
@@ -481,14 +491,23 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
 }
 
 // out[seg][j] (+)= scale * sum over the workgroups' rows of the segment: 16 columns
-// and 64 row groups per workgroup, added in a fixed order
+// and 64 row groups per workgroup, added in a fixed order.  GU rows in flight per
+// thread: with one after the other a backward of 492 rows takes 1 to 1.5 us more; 8 or 4
+// columns per workgroup take as long.
 __global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, int rows, int dh, double scale, float* dgq,
                                                        float* dgk, bool acc) {
+  constexpr int GU = 8;
   __shared__ double sh[16][16];
   const int seg = blockIdx.y, cl = threadIdx.x & 15, j = blockIdx.x * 16 + cl;
   double t = 0.0;
   if (j < dh)
-    for (int r = threadIdx.x >> 4; r < rows; r += 64) t += part[(int64_t)(2 * r + seg) * dh + j];
+    for (int r = threadIdx.x >> 4; r < rows; r += 64 * GU) {
+      double v[GU];
+#pragma unroll
+      for (int u = 0; u < GU; ++u) v[u] = r + 64 * u < rows ? part[(int64_t)(2 * (r + 64 * u) + seg) * dh + j] : 0.0;
+#pragma unroll
+      for (int u = 0; u < GU; ++u) t += v[u];
+    }
   t += __shfl_xor(t, 16, 64);
   t += __shfl_xor(t, 32, 64);
   if ((threadIdx.x & 63) < 16) sh[threadIdx.x >> 6][cl] = t;
