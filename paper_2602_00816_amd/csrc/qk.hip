@@ -545,15 +545,20 @@ int pieces(int64_t heads, int dh, int v) { return (int)ceil_div(heads, 64 / grou
 
 QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   QkSplit w{};
-  // The group that gives the fewest pieces in all, the smallest such.  (8 + 1 + 1 heads of
-  // 128, bf16, 16384 tokens, forward: 46 us in groups of 8, 57 without.  One token per piece
-  // is a kernel of its own, which knows the token as a scalar: the layer above takes 145 us
-  // backward in it and 151 in the general one.)
-  int64_t C = 0, units = INT64_MAX;
+  // The group that gives the fewest pieces in all, the smallest such, if it saves enough: one
+  // token per piece is a kernel of its own, which knows the token as a scalar and shares no
+  // piece's angles with lanes of other tokens.  A fifth in the bf16 norm forward, whose arithmetic
+  // weighs most (28 + 4 + 4 heads of 128, a quarter saved: 106 us, 109 without), a third in other
+  // bf16 kernels (the same heads turned alone 102, 93 without; 5 + 5 + 5 of 40, three eighths
+  // saved, 128 and 150), two fifths in fp32 (8 + 1 + 1 of 128, three eighths saved, norm
+  // backward: 166 and 141; half of 4 + 1 + 1: 165 either way).
+  const int worth = !bf16 ? 60 : !bwd && a.gq ? 80 : 66;
+  int64_t C = 0, units = 0, most = 0;
   for (int g = 1; g <= 64 && g <= std::max(1, a.T); g *= 2) {
     const int64_t c = pieces((int64_t)g * a.Hq, a.dh, v) + (values ? 2 : 1) * (int64_t)pieces((int64_t)g * a.Hk, a.dh, v);
     const int64_t n = (a.T + g - 1) / g;
-    if (n * c >= units) continue;
+    if (g > 1 && n * c >= most) continue;
+    most = g == 1 ? n * c * worth / 100 : n * c;
     units = n * c;
     C = c;
     w.group = g;
