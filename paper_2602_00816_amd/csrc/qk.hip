@@ -34,10 +34,14 @@ namespace fdh {
 
 namespace {
 
-// Threads per workgroup; most wavefronts of a backward with gains: as many as are resident
-// at once (four per SIMD at 126 registers), as each workgroup leaves a row of gain sums (the
-// layer above: 145 us with 4096, 154 with 8192, 187 with 32768).
-constexpr int FWD_NT = 256, BWD_WAVES = 4096;
+// Threads per workgroup.  Forward: 256, but 128 where the bf16 norm's registers and angles
+// leave fewer wavefronts ready (2^26 elements in 4 + 1 + 1 heads of 128: 116 us against 123, 14 + 2 + 2 of
+// 64: 110 against 114, 32 + 8 + 8 of 128: 97 either way; rotation alone, of 64: 110 against 93).
+constexpr int fwd_threads(bool bf16, bool norm) { return bf16 && norm ? 128 : 256; }
+// Most wavefronts of a backward with gains: as many as are resident at once (four per SIMD at
+// 126 registers), as each workgroup leaves a row of gain sums (the layer above: 145 us with
+// 4096, 154 with 8192, 187 with 32768).
+constexpr int BWD_WAVES = 4096;
 // (32 lanes per head take 132 to 138 registers in workgroups of 512: one of them per CU.  Held
 // to 128 by a workgroup of 1024, 16 + 16 heads of 192, 256 MB of dy: 218 us against 314; with
 // 16 lanes per head the two are within 2%.)
@@ -298,7 +302,8 @@ __device__ inline Piece piece(const QkArgs& a, const QkSplit& w, int c) {
 }
 
 template <typename T, int V, int G, bool NORM, bool GROUP>
-__global__ __launch_bounds__(FWD_NT) void qk_fwd_kernel(QkArgs a, QkSplit w) {
+__global__ __launch_bounds__(fwd_threads(sizeof(T) == 2, NORM)) void qk_fwd_kernel(QkArgs a, QkSplit w) {
+  constexpr int FWD_NT = fwd_threads(sizeof(T) == 2, NORM);
   __shared__ float2 cs[FWD_NT / 64][64 * V];   // 64 / G tokens of half <= G V pairs
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
@@ -567,7 +572,7 @@ QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   w.chunks[0] = pieces((int64_t)w.group * a.Hq, a.dh, v);
   w.chunks[1] = pieces((int64_t)w.group * a.Hk, a.dh, v);
   w.chunks[2] = values ? w.chunks[1] : 0;
-  const int nw = (bwd ? bwd_threads(group_lanes(a.dh, v)) : FWD_NT) / 64;
+  const int nw = (bwd ? bwd_threads(group_lanes(a.dh, v)) : fwd_threads(bf16, a.gq)) / 64;
   // Groups per wavefront.  Backward with the norm: as few as a resident grid leaves.  Elsewhere
   // short runs: many wavefronts, which the scheduler interleaves and which walk through memory
   // closer to its order (the layer above forward 76 us, 84 with the 8 to 12 of a resident grid;
@@ -601,8 +606,9 @@ void launch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
     if (w.group == 1) hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(bwd_threads(G)), 0, s, a, w);
     else hipLaunchKernelGGL((qk_bwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(bwd_threads(G)), 0, s, a, w);
   } else {
-    if (w.group == 1) hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
-    else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(FWD_NT), 0, s, a, w);
+    constexpr int NT = fwd_threads(sizeof(T) == 2, NORM);
+    if (w.group == 1) hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, false>), dim3(w.blocks), dim3(NT), 0, s, a, w);
+    else hipLaunchKernelGGL((qk_fwd_kernel<T, V, G, NORM, true>), dim3(w.blocks), dim3(NT), 0, s, a, w);
   }
 }
 template <typename T, bool BWD, bool NORM, int V>
