@@ -23,7 +23,7 @@
 //
 // Memory-bound: 8 bytes per bf16 element forward and 16 backward against some 30 and 45
 // vector instructions.  One layer of 16 + 16 + 16 heads of 128 at 8192 tokens, bf16:
-// forward 76 us (403 MB, 5.3 TB/s), backward 140 us with the gains' sums (738 MB, 5.2 TB/s);
+// forward 76 us (403 MB, 5.3 TB/s), backward 140 us with the gains' sums (738 MB, 5.3 TB/s);
 // rotation alone of 32 + 8 + 8 heads at 16384 tokens 143 us (805 MB, 5.6 TB/s).  A plain
 // copy of as many bytes runs at 6.0 TB/s; the vector units are busy for less than half the time.
 #include "kernels.h"
