@@ -4,6 +4,8 @@ hundred, strides, axes, far positions, gains with and without a direction, value
 the ends of the range, NaN and infinities, in place, accumulation, repeated calls,
 graphs, other streams.  Every element is held to half a step of its type plus a
 bound of the fp32 arithmetic's error that is worked out beside it in qk_ref."""
+import gc
+
 import numpy as np
 import pytest
 
@@ -433,6 +435,8 @@ def test_more_wavefronts_than_a_launch_holds():
     hq, hk, dh = 62, 2, 136
     S, B = 2 ** 12, 2 ** 9 + 1
     T, ncol = S * B, (hq + 2 * hk) * dh
+    gc.collect()   # what earlier tests left
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 4 * T * ncol + 2 ** 32:
         pytest.skip("80 GB of free memory needed")
     m = _model(fd, hq, hk, dh, "bf16", norm=False)
