@@ -3,8 +3,8 @@
 // (mean m and half difference d of the two points theta +- eps v).
 //
 // With the pair product (a o b).m = a.m b.m + a.d b.d, (a o b).d = a.m b.d + a.d b.m
-// (exact, and free of differences of nearly equal values), per token and head
-// of n elements, e the norm's epsilon:
+// (exact, and free of differences of nearly equal values where the two points are of like
+// size), per token and head of n elements, e the norm's epsilon:
 //   forward   S+- = mean((x.m +- x.d)^2) + e,  b = 2 mean(x.m x.d) = (S+ - S-) / 2,
 //             r+- = S+-^(-1/2),  r.m = (r+ + r-) / 2,
 //             rho = r.d / r.m = (r+ - r-) / (r+ + r-) = -2 b (r+ r-)^2 / (r+ + r-)^2,
@@ -13,6 +13,17 @@
 //             c = mean(u o du) = r o mean(x o du),  dx = r o (du - u o c).
 // R turns pair i (elements i and i + n/2) by base^(-2i/n) times the token's
 // position along the axis of pair i; without a norm y = R x and dx = R^T dy.
+//
+// Heads with a small point, that is x.d close to x.m (sigma = 1, S- small) or to -x.m
+// (sigma = -1, S+ small): there the smaller S is itself a difference, and u's terms are larger
+// than u+- by up to half the ratio of the r's.  From a ratio of 8 on (up to it, 4.5 times) the
+// smaller S is the mean of (x.m - sigma x.d)^2, and forward
+//   u = (x.m - sigma x.d + kappa x.d, x.d - sigma x.m + kappa x.m) r.m,
+//   kappa = sigma + rho = 2 sigma r / (r+ + r-),  r the smaller of the two,
+// whose terms are no larger than u+- (other heads: sigma = 0).  Backward all of it is done at the
+// two points, whose gradients may differ as much: u+- = (x.m +- x.d) r+-, du+- = dz+- g+-,
+// dx+- = r+- (du+- - u+- mean(u+- du+-)), then the mean and half difference of the two.
+// (Elsewhere the points would lose a half difference that is small.)
 //
 // The sums behind r and all that is formed from them once per head are fp64, with
 // S+- = mean(x.m^2 + x.d^2) +- 2 mean(x.m x.d) + e (no overflow or underflow; rho in
@@ -155,13 +166,18 @@ __device__ inline double rcp_nr(double x) {
   const double y = __builtin_amdgcn_rcp(x);
   return fma(fma(-x, y, 1.0), y, y);
 }
-// r.m and rho = r.d / r.m of the head from sum (m^2 + d^2) and sum m d
-struct Rms { double m, rho; };
+// r.m and rho = r.d / r.m of the head from sum (m^2 + d^2) and sum m d, the smaller r, and whether the
+// other one, of a small point, is more than 8 times that: |rho| = |r+ - r-| / (r+ + r-) > 7/9.
+// (A NaN is no small point.)
+struct Rms {
+  double m, rho, large;   // (large: the larger point's, the smaller r)
+  bool small;
+};
 __device__ inline Rms rms_pair(double sq, double md, double inv_n, double neps) {
   const double b = 2.0 * md, p = sq + b, q = sq - b;   // sums of (m + d)^2, (m - d)^2
-  const double rp = rsqrt_nr(fma(p < 0.0 ? 0.0 : p, inv_n, neps)), rm = rsqrt_nr(fma(q < 0.0 ? 0.0 : q, inv_n, neps));
-  const double s = rp + rm, x = rp * rm * rcp_nr(s);
-  return {0.5 * s, -2.0 * b * inv_n * x * x};
+  const double rp = rsqrt_nr(fma(p < 0.0 ? 0.0 : p, inv_n, neps)), rn = rsqrt_nr(fma(q < 0.0 ? 0.0 : q, inv_n, neps));
+  const double s = rp + rn, x = rp * rn * rcp_nr(s), rho = -2.0 * b * inv_n * x * x;
+  return {0.5 * s, rho, rho < 0.0 ? rp : rn, fabs(rho) > 7.0 / 9.0};
 }
 
 // ---- angles --------------------------------------------------------------------
@@ -282,9 +298,9 @@ struct Piece {
   bool on, ok;        // a lane of the head; of a head that the piece has
 };
 template <int V, int G, bool GROUP>
-__device__ inline Piece piece(const QkArgs& a, const QkSplit& w, int c) {
+__device__ inline Piece piece(const QkArgs& a, const QkSplit& w, int c, int lane) {
   constexpr int HPW = 64 / G;
-  const int lane = threadIdx.x & 63, i0 = (lane & (G - 1)) * V;
+  const int i0 = (lane & (G - 1)) * V;
   Piece p;
   p.seg = c < w.chunks[0] ? 0 : c < w.chunks[0] + w.chunks[1] ? 1 : 2;
   const int r0 = HPW * (c - (p.seg == 0 ? 0 : p.seg == 1 ? w.chunks[0] : w.chunks[0] + w.chunks[1]));
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(fwd_threads(sizeof(T) == 2, NORM)) void qk_fwd_kern
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (FWD_NT / 64) + (threadIdx.x >> 6)));
   const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
   if (wave / C >= w.step) return;
-  const Piece p = piece<V, G, GROUP>(a, w, wave % C);
+  const Piece p = piece<V, G, GROUP>(a, w, wave % C, threadIdx.x & 63);
   const int half = a.dh / 2;
   float gm[2 * V], gd[2 * V];
   if constexpr (NORM)
@@ -342,10 +358,23 @@ __global__ __launch_bounds__(fwd_threads(sizeof(T) == 2, NORM)) void qk_fwd_kern
           md = fma(x, y, md);
         }
         const Rms r = rms_pair(group_sum<G>(p.on ? sq : 0.0), group_sum<G>(p.on ? md : 0.0), a.inv_n, a.neps);
-        const float rm = (float)r.m, rho = (float)r.rho;
+        float rm = (float)r.m, kappa = (float)r.rho, sigma = 0.f;
+        if (r.small) {   // (all lanes of a head alike)
+          sigma = r.rho < 0.0 ? 1.f : -1.f;
+          double q = 0.0;
+#pragma unroll
+          for (int e = 0; e < 2 * V; ++e) {
+            const double x = fmaf(-sigma, d[e], m[e]);
+            q = fma(x, x, q);
+          }
+          const double rs = rsqrt_nr(fma(group_sum<G>(p.on ? q : 0.0), a.inv_n, a.neps)), t = r.large + rs;
+          rm = (float)(0.5 * t);
+          kappa = sigma * (float)(2.0 * r.large * rcp_nr(t));
+        }
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) {
-          const float um = (m[e] + d[e] * rho) * rm, ud = (m[e] * rho + d[e]) * rm;
+          const float um = fmaf(d[e], kappa, fmaf(-sigma, d[e], m[e])) * rm;
+          const float ud = fmaf(m[e], kappa, fmaf(-sigma, m[e], d[e])) * rm;
           m[e] = um * gm[e] + ud * gd[e];
           d[e] = um * gd[e] + ud * gm[e];
         }
@@ -369,6 +398,78 @@ __global__ __launch_bounds__(fwd_threads(sizeof(T) == 2, NORM)) void qk_fwd_kern
   }
 }
 
+// ---- backward of heads with a small point ---------------------------------------------
+// Rare, so it comes after the loop over the wavefront's groups, from memory to memory, an element
+// after the other: inside the loop it took the kernel from 126 registers to 138 or more, three
+// wavefronts per SIMD instead of four (4 + 1 + 1 heads of 128: 306 us against 209).
+// One head of a layer in a thousand: 152 us where there are none 141, all of them: 523.
+struct Points { float p, n; };
+template <typename T>
+__device__ inline Points points(const T* m, const T* d, int64_t i) {
+  const float x = ldf(m, i), y = ldf(d, i);
+  return {x + y, x - y};
+}
+template <typename T>
+__device__ inline Points gain_points(const QkArgs& a, int seg, int j) {
+  const float* v = seg ? a.vk : a.vq;
+  const float g = ldf((const T*)(seg ? a.gk : a.gq), j), w = v ? (float)(a.eps * (double)v[j]) : 0.f;
+  return {g + w, g - w};
+}
+// The heads of token t that the wavefront's lanes hold, by the whole wavefront; cs: the angles of the
+// lane's pairs.  The gain's terms are added over the wavefront's heads to sums[e G + lane].
+template <typename T, int V, int G>
+__device__ inline void bwd_points(const QkArgs& a, const Piece& p, int t, bool ok, const float2* cs, double* sums) {
+  const int half = a.dh / 2, lane = threadIdx.x & 63;
+  const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
+  const int64_t o = row(t, a.ldx) + p.col, og = row(t, a.lddy) + p.col, oy = row(t, a.ldy) + p.col;
+  double sq = 0.0, md = 0.0, sp = 0.0, sn = 0.0;
+#pragma unroll 1
+  for (int e = 0; e < 2 * V; ++e) {
+    const int64_t i = o + (e < V ? e : half + e - V);
+    const double x = ldf(xm, i), y = ldf(xd, i);
+    sq = fma(x, x, fma(y, y, sq));   // as the loop over the groups adds them: the same heads are small
+    md = fma(x, y, md);
+    sp = fma(x + y, x + y, sp);
+    sn = fma(x - y, x - y, sn);
+  }
+  const bool take = rms_pair(group_sum<G>(p.on ? sq : 0.0), group_sum<G>(p.on ? md : 0.0), a.inv_n, a.neps).small && ok;
+  if (!__ballot(take)) return;
+  const Points r = {(float)rsqrt_nr(fma(group_sum<G>(p.on ? sp : 0.0), a.inv_n, a.neps)),
+                    (float)rsqrt_nr(fma(group_sum<G>(p.on ? sn : 0.0), a.inv_n, a.neps))};
+  Points c = {0.f, 0.f};
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+    for (int e = 0; e < V; ++e) {
+      const float co = cs[e].x, si = cs[e].y;
+      const Points lo = points(a.dy_m, a.dy_d, og + e), hi = points(a.dy_m, a.dy_d, og + e + half);
+      const Points z[2] = {{lo.p * co + hi.p * si, lo.n * co + hi.n * si}, {hi.p * co - lo.p * si, hi.n * co - lo.n * si}};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = e + h * half;
+        const Points x = points(xm, xd, o + j), g = gain_points<T>(a, p.seg, p.i0 + j);
+        const Points u = {x.p * r.p, x.n * r.n}, du = {z[h].p * g.p, z[h].n * g.n};
+        if (pass == 0) {
+          c.p += u.p * du.p;
+          c.n += u.n * du.n;
+          double w = take ? 0.5 * (double)(z[h].p * u.p - z[h].n * u.n) : 0.0;
+#pragma unroll
+          for (int k = G; k < 64; k <<= 1) w += __shfl_xor(w, k, 64);
+          if (lane < G) sums[(h * V + e) * G + lane] += w;
+        } else if (take) {
+          const Points dx = {(du.p - u.p * c.p) * r.p, (du.n - u.n * c.n) * r.n};
+          stf((T*)a.y_m, oy + j, 0.5f * (dx.p + dx.n));
+          stf((T*)a.y_d, oy + j, 0.5f * (dx.p - dx.n));
+        }
+      }
+    }
+    if (pass == 0) {
+      c.p = group_sum<G>(p.on ? c.p : 0.f) * (float)a.inv_n;
+      c.n = group_sum<G>(p.on ? c.n : 0.f) * (float)a.inv_n;
+    }
+  }
+}
+
 // Backward.  Every workgroup leaves its sums of the gain gradients' half differences
 // (fp64, fixed order) as rows 2 blockIdx.x (queries) and 2 blockIdx.x + 1 (keys) of part.
 template <typename T, int V, int G, bool NORM, bool GROUP>
@@ -379,13 +480,15 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
   const T *xm = (const T*)a.x_m, *xd = (const T*)a.x_d;
   T *ym = (T*)a.y_m, *yd = (T*)a.y_d;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * NW + wv));
+  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * NW + wv)), id = wave;
   const int C = w.chunks[0] + w.chunks[1] + w.chunks[2];
   const int groups = wave / C < w.step ? w.groups : 0;   // (the last workgroup may hold wavefronts without work)
-  const Piece p = piece<V, G, GROUP>(a, w, wave % C);
+  const Piece p = piece<V, G, GROUP>(a, w, wave % C, lane);
   const int half = a.dh / 2;
   float gm[2 * V], gd[2 * V];
   double acc[2 * V];
+  uint64_t small = 0;   // steps (modulo 64) with a head that has a small point
+  int step = 0;
   if constexpr (NORM) {
     if (p.seg < 2) lane_gains<T, V>(a, p.seg, p.i0, gm, gd);
 #pragma unroll
@@ -405,6 +508,7 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
         if (p.seg < 2) load<T, V, true>(in[k], (k & 2 ? xd : xm) + ox + j);
     }
     float zm[2 * V], zd[2 * V];
+    bool leave = false;
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) {
       zm[e] = get<float, V>(dy[e / V], e % V);
@@ -437,7 +541,9 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
           md = fma(x, y, md);
         }
         const Rms r = rms_pair(group_sum<G>(p.on ? sq : 0.0), group_sum<G>(p.on ? md : 0.0), a.inv_n, a.neps);
-        const float rm = (float)r.m, rho = (float)r.rho;
+        leave = r.small;
+        if (__ballot(leave)) small |= 1ull << (step & 63);
+        const float rm = leave ? 0.f : (float)r.m, rho = (float)r.rho;   // (u = 0: nothing to the gains' sums here)
         float cm = 0.f, cd = 0.f;
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) {
@@ -461,15 +567,26 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
         }
       }
     }
-    if (ok) {
+    if (ok && !leave) {
       const int64_t q = row(t, a.ldy) + p.col;
       store<T, V, true>(ym + q, zm);
       store<T, V, true>(ym + q + half, zm + V);
       store<T, V, true>(yd + q, zd);
       store<T, V, true>(yd + q + half, zd + V);
     }
+    ++step;
   }
   if constexpr (NORM) {
+    // Thread, wavefront and arguments once more, as values of their own: what follows uses them, and
+    // kept through the loop above they cost it registers (138 of them in fp32 where tokens share a
+    // wavefront, 129 so).
+    struct Kernarg { QkArgs a; QkSplit w; };   // as the kernel's arguments lie
+    auto again = (const __attribute__((address_space(4))) Kernarg*)__builtin_amdgcn_kernarg_segment_ptr();
+    int tid = threadIdx.x, wave = id;
+    asm volatile("" : "+v"(tid), "+s"(wave), "+s"(again));
+    const QkArgs& a = *(const QkArgs*)&again->a;
+    const QkSplit& w = *(const QkSplit*)&again->w;
+    const int C = w.chunks[0] + w.chunks[1] + w.chunks[2], half = a.dh / 2, lane = tid & 63, wv = wave % NW;
     // over the wavefront's heads, then over the wavefronts of each segment
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) {
@@ -478,8 +595,19 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
       for (int o = G; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
       if (lane < G) sh[wv][e * G + lane] = acc[e];
     }
+    if (small) {
+      const Piece p = piece<V, G, GROUP>(a, w, wave % C, lane);
+      int step = 0;
+      for (int64_t g = wave / C; g < w.groups; g += w.step, ++step) {
+        if (!(small >> (step & 63) & 1)) continue;
+        const int t0 = GROUP ? (int)g * w.group + p.t0 : (int)g, t = GROUP ? min(t0 + p.tok, a.T - 1) : t0;
+        float c[V], s[V];
+        token_angles<V, GROUP>(a, w, t0, p.ntok, p.tok, p.i0, cs[wv], c, s);
+        bwd_points<T, V, G>(a, p, t, GROUP ? p.ok && t0 + p.tok < a.T : p.ok, cs[wv] + (GROUP ? p.tok * half : 0) + p.i0, sh[wv]);
+      }
+    }
     __syncthreads();
-    for (int k = threadIdx.x; k < 2 * 2 * V * G; k += BWD_NT) {
+    for (int k = tid; k < 2 * 2 * V * G; k += BWD_NT) {
       const int seg = k / (2 * V * G), j = k % (2 * V * G);
       double x = 0.0;
 #pragma unroll

@@ -189,3 +189,51 @@ def check(got, want, bound, what):
     bad = ~((g - want).abs() <= tol)
     assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} elements off, worst "
                            f"{float(((g - want).abs() / tol).nan_to_num(float('inf')).max()):.3g} x the bound")
+
+
+# ---- heads one of whose points is much smaller than the other -------------------------
+# Where x.d is close to x.m or -x.m, the sums above are much larger than the result
+# (|x.m| r.m + |x.d| |r.d| against |u+| + |u-|, as r of the small point is the larger),
+# so a result that has lost every digit would pass.  Such heads are held to sums of
+# absolute values taken at each point on its own, in which nothing cancels; a mean or
+# half difference is off by half of what its two points are off by together.
+def point_ratio(x, hq, hk, dh, norm_eps=1e-5):
+    """[T, hq + hk]: the smaller of a head's mean squares (with epsilon) over the larger."""
+    s = [(p.view(-1, hq + 2 * hk, dh)[:, :hq + hk] ** 2).mean(-1) + norm_eps for p in points(x)]
+    return torch.minimum(*s) / torch.maximum(*s)
+
+
+def _point_parts(x, hq, hk, dh, gains, eps, norm_eps):
+    """|u| and r at each point, and |gain| + |its half difference|."""
+    q, k, vq, vk = (torch.zeros(dh, dtype=F64) if t is None else t.detach().cpu().to(F64).abs() for t in gains)
+    g = torch.cat([(q + eps * vq).expand(hq, dh), (k + eps * vk).expand(hk, dh)])
+    out = []
+    for p in points(x):
+        p = p.view(-1, hq + 2 * hk, dh)[:, :hq + hk]
+        r = ((p * p).mean(-1, keepdim=True) + norm_eps).rsqrt()
+        out.append((p.abs() * r, r))
+    return out, g
+
+
+def forward_point_bound(x, hq, hk, dh, ang, gains, eps=1.0, norm_eps=1e-5):
+    """Bound of either channel's turned columns, [T, (hq + hk) dh].  u is formed as
+    ((m -+ d) + d kappa) r.m, kappa = 2 r / (r+ + r-) with the smaller r: with |d|, |m| <=
+    (|x+| + |x-|) / 2 and one r at least 8 times the other, the terms' sum is at most 5/4 of
+    (|u+| + |u-|) / 2.  Roundings: difference (or kappa) and sum 2, r.m and its product 4, gain's half
+    difference, product, sum 7; rotation 10; and one for what the products of roundings
+    add: 11, of 5/4: 14."""
+    parts, g = _point_parts(x, hq, hk, dh, gains, eps, norm_eps)
+    b = 0.5 * sum(_abs_turn(u * g, ang) for u, _ in parts)
+    return ((14 * U32 + REF) * b).reshape(b.shape[0], -1)
+
+
+def backward_point_bound(x, dy, hq, hk, dh, ang, gains, eps=1.0, norm_eps=1e-5):
+    """(bound of either channel of dx's turned columns, of the two gain gradients).  Roundings: dy.m
+    +- dy.d, rotation 3: dz 4; gain 2, product: du 7; u: 3; u du 11; its mean in fp32, 16 sums in
+    a lane, 5 over lanes, 1 / n and its product: c 34; u c 38; du - u c 39; r and its product 41; half
+    the sum of two points 42; one more as above.  Gain terms: dz 4, u 3, product, difference: 9, and one."""
+    parts, g = _point_parts(x, hq, hk, dh, gains, eps, norm_eps)
+    z = [_abs_turn(p.abs().view(-1, hq + 2 * hk, dh)[:, :hq + hk], ang) for p in points(dy)]
+    b = 0.5 * sum(r * (a * g + u * (u * a * g).mean(-1, keepdim=True)) for (u, r), a in zip(parts, z))
+    t = (10 * U32 + REF) * 0.5 * sum(u * a for (u, _), a in zip(parts, z)) / eps
+    return ((43 * U32 + REF) * b).reshape(b.shape[0], -1), (t[:, :hq].sum((0, 1)), t[:, hq:].sum((0, 1)))
