@@ -79,6 +79,15 @@ fdh_status fdh_testing_gemm_epilogue(int32_t dtype, int32_t M, int32_t N, int32_
 fdh_status fdh_testing_gemm_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t batch, size_t scratch_bytes,
                                  int32_t* out4);
 
+/* How fdh_qk_forward (backward = 0) or fdh_qk_backward would split T tokens of
+ * n_heads query and n_kv_heads key heads of head_dim elements (host arithmetic only), with the norm
+ * or without, in place or not (forward without a copy of the value heads): out12 = tokens per
+ * group, groups, pieces of a group (queries, keys, values), groups per step, workgroups, threads
+ * per workgroup, lanes per head, pairs per lane, the factor f with i f / 2^16 = i / (head_dim / 2)
+ * in whole numbers, bytes of scratch written. */
+fdh_status fdh_testing_qk_split(int32_t dtype, int64_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                int32_t norm, int32_t backward, int32_t in_place, int64_t* out12);
+
 /* on != 0 makes the next fdh_set_workspace plan the unfused attention path
  * (score, probability and score-gradient matrices in the workspace, MFMA
  * GEMMs and row kernels) even where the fused kernels apply (bf16 operands;

@@ -553,6 +553,24 @@ extern "C" fdh_status fdh_testing_gemm_plan(int32_t dtype, int32_t M, int32_t N,
   return FDH_OK;
 }
 
+extern "C" fdh_status fdh_testing_qk_split(int32_t dtype, int64_t T, int32_t n_heads, int32_t n_kv_heads,
+                                           int32_t head_dim, int32_t norm, int32_t backward, int32_t in_place,
+                                           int64_t* out12) {
+  if (!out12 || (dtype != FDH_F32 && dtype != FDH_BF16) || T < 0 || T > fdh::QK_MAX_TOKENS || n_heads < 1 ||
+      n_heads > fdh::QK_MAX_HEADS || n_kv_heads < 1 || n_kv_heads > n_heads || head_dim < 8 || head_dim % 8 ||
+      head_dim > fdh::QK_MAX_DH)
+    return FDH_ERR_INVALID_ARG;
+  fdh::QkArgs a{};
+  a.T = (int)T; a.Hq = n_heads; a.Hk = n_kv_heads; a.dh = head_dim;
+  a.gq = norm ? out12 : nullptr;   // (only looked at for being there)
+  const fdh::QkPlan p = fdh::qk_plan(a, dtype == FDH_BF16, backward != 0, backward || !in_place);
+  const fdh::QkSplit& w = p.split;
+  const int64_t out[12] = {w.group, w.groups, w.chunks[0], w.chunks[1], w.chunks[2], w.step, w.blocks, p.threads,
+                           p.lanes, p.pairs, w.rhalf, (int64_t)p.part_bytes};
+  std::copy(out, out + 12, out12);
+  return FDH_OK;
+}
+
 extern "C" fdh_status fdh_testing_unfused_attention(fdh_ctx* ctx, int32_t on) {
   return run(ctx, [&](fdh::Engine& e) -> int {
     e.force_unfused = on != 0;

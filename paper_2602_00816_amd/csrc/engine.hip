@@ -624,6 +624,7 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
     }
     a.eps = eps; a.neps = (double)neps;
     a.part = (double*)(ws + gpart.off);
+    a.part_bytes = gpart.bytes;
     a.rot = rot;
     return a;
   };
@@ -1355,6 +1356,7 @@ int Engine::qk_backward(const fdh_qk_gains* g, const int32_t* pos, int B, int S,
   a.dy_m = dy_m; a.dy_d = dy_d; a.lddy = lddy;
   a.y_m = dx_m; a.y_d = dx_d; a.ldy = lddx;
   a.part = (double*)scratch;
+  a.part_bytes = need;
   if (bf16) CK(launch_qk_bwd<bf16_t>(a, dgq, dgk, acc, stream));
   else CK(launch_qk_bwd<float>(a, dgq, dgk, acc, stream));
   return FDH_OK;

@@ -195,7 +195,8 @@ struct QkArgs {
   const void *gq, *gk;           // gains [dh], operand type; null: no norm
   const float *vq, *vk;          // their directions (null: the same gains at both points)
   double eps, neps;
-  double* part;                  // backward with gains: qk_scratch_bytes
+  double* part;                  // backward with gains: qk_scratch_bytes ...
+  size_t part_bytes;             // ... of which there are these (a launch that needs more is refused)
   double inv_n;                  // set by the launchers, as is
   bool gvec;                     // gains and directions 16-byte aligned
   QkRotary rot;
@@ -207,6 +208,14 @@ struct QkSplit {
 };
 // bytes of part for up to T_ tokens
 size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh);
+// the split of a launch (T, Hq, Hk, dh and whether there are gains are read; values: with the value
+// columns): threads per workgroup, lanes per head, pairs per lane, and the bytes of part that it writes
+struct QkPlan {
+  QkSplit split;
+  int threads, lanes, pairs;
+  size_t part_bytes;
+};
+QkPlan qk_plan(const QkArgs& a, bool bf16, bool bwd, bool values);
 // y = rotated (normed) q and k columns of x, v columns copied unless y is x
 // (in place: the same pointers and row strides)
 template <typename T>

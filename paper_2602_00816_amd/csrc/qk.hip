@@ -728,6 +728,9 @@ QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   return w;
 }
 
+// what the workgroups of a backward with gains write of part
+size_t part_bytes(const QkArgs& a, const QkSplit& w) { return (size_t)w.blocks * 2 * a.dh * sizeof(double); }
+
 template <typename T, bool BWD, bool NORM, int V, int G>
 void launch(const QkArgs& a, const QkSplit& w, hipStream_t s) {
   if constexpr (BWD) {
@@ -766,6 +769,7 @@ template <typename T, bool BWD, bool NORM>
 hipError_t dispatch(const QkArgs& a, bool values, QkSplit* out, hipStream_t s) {
   const int v = lane_pairs<T, BWD>(a.dh);
   const QkSplit w = split(a, v, sizeof(T) == 2, BWD, values);
+  if (BWD && NORM && part_bytes(a, w) > a.part_bytes) return hipErrorInvalidValue;
   if (out) *out = w;
   if constexpr (!BWD && sizeof(T) == 2) {
     if (v == 8) return dispatch_v<T, BWD, NORM, 8>(a, w, s);
@@ -784,6 +788,16 @@ size_t qk_scratch_bytes(int64_t T_, int Hq, int Hk, int dh) {
   const int64_t waves = std::min<int64_t>(T_ * c1, std::max<int64_t>(BWD_WAVES, c64));
   const int nw = bwd_threads(group_lanes(dh, 4)) / 64;
   return (size_t)((waves + nw - 1) / nw) * 2 * dh * sizeof(double);
+}
+
+QkPlan qk_plan(const QkArgs& a, bool bf16, bool bwd, bool values) {
+  QkPlan p;
+  p.pairs = bf16 ? (bwd ? lane_pairs<bf16_t, true>(a.dh) : lane_pairs<bf16_t, false>(a.dh)) : lane_pairs<float, false>(a.dh);
+  p.lanes = group_lanes(a.dh, p.pairs);
+  p.threads = bwd ? bwd_threads(p.lanes) : fwd_threads(bf16, a.gq);
+  p.split = split(a, p.pairs, bf16, bwd, values);
+  p.part_bytes = bwd && a.gq ? part_bytes(a, p.split) : 0;
+  return p;
 }
 
 template <typename T>

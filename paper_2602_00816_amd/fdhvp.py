@@ -119,6 +119,7 @@ def lib():
         "fdh_testing_gemm_epilogue": (i32, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i64, i32, C.c_float, C.c_float,
                                             vp, vp, C.c_float, vp, i32, i32, vp, C.c_size_t, vp]),
         "fdh_testing_gemm_plan": (i32, [i32, i32, i32, i32, i32, C.c_size_t, C.POINTER(i32)]),
+        "fdh_testing_qk_split": (i32, [i32, i64, i32, i32, i32, i32, i32, i32, C.POINTER(i64)]),
         "fdh_testing_unfused_attention": (i32, [vp, i32]),
         "fdh_testing_unsplit_wgrad": (i32, [vp, i32]),
         "fdh_testing_timing": (i32, [vp, i32]),
