@@ -361,8 +361,8 @@ class Model:
         self._check_params(params)
         _check_tokens(tokens)
         B, S = (tokens.shape if tokens is not None else (0, 0))
-        self._keep = [params, tokens]
         self._check(self._L.fdh_bind(self._h, _ptr(params), _ptr(tokens), B, S, float(eps)), "fdh_bind")
+        self._keep = [params, tokens]   # (a refused call leaves the operator bound before, and its tensors)
 
     def bind_dataset(self, params, batches, eps: float, reduction: str = "mean", positions=None) -> int:
         """Bind the token-weighted dataset operator over ``batches``: a list of
@@ -389,7 +389,6 @@ class Model:
         parr = (C.c_void_p * len(items))(*[_ptr(p) for p in pos])
         arr = (Batch * len(items))(*[Batch(_ptr(t), _ptr(l), t.shape[0], t.shape[1]) for t, l in items])
         n = C.c_int64()
-        self._keep = [params] + [x for it in items for x in it if x is not None] + [p for p in pos if p is not None]
         if positions is None:
             st = self._L.fdh_bind_dataset(self._h, _ptr(params), arr, len(items), float(eps), REDUCTION[reduction],
                                           C.byref(n))
@@ -397,6 +396,7 @@ class Model:
             st = self._L.fdh_bind_dataset_positions(self._h, _ptr(params), arr, parr, len(items), float(eps),
                                                     REDUCTION[reduction], C.byref(n))
         self._check(st, "fdh_bind_dataset")
+        self._keep = [params] + [x for it in items for x in it if x is not None] + [p for p in pos if p is not None]
         return int(n.value)
 
     # ---- the q/k front of a layer ----
