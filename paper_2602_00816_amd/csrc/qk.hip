@@ -32,10 +32,10 @@
 // are fp64; each output is rounded once to its type.  A head that holds a NaN or an
 // infinity gives NaN in all its elements, other heads are not touched by it.
 //
-// Memory-bound: 8 bytes per bf16 element forward and 16 backward against some 30 and 45
+// Memory-bound: 8 bytes per bf16 element forward and 16 backward against some 35 and 45
 // vector instructions.  One layer of 16 + 16 + 16 heads of 128 at 8192 tokens, bf16:
 // forward 76 us (403 MB, 5.3 TB/s), backward 140 us with the gains' sums (738 MB, 5.3 TB/s);
-// rotation alone of 32 + 8 + 8 heads at 16384 tokens 143 us (805 MB, 5.6 TB/s).  A plain
+// rotation alone of 32 + 8 + 8 heads at 16384 tokens 144 us (805 MB, 5.6 TB/s).  A plain
 // copy of as many bytes runs at 6.0 TB/s; the vector units are busy for less than half the time.
 #include "kernels.h"
 
@@ -46,16 +46,18 @@ namespace fdh {
 namespace {
 
 // Threads per workgroup.  Forward: 256, but 128 where the bf16 norm's registers and angles
-// leave fewer wavefronts ready (2^26 elements in 4 + 1 + 1 heads of 128: 116 us against 123, 14 + 2 + 2 of
-// 64: 110 against 114, 32 + 8 + 8 of 128: 97 either way; rotation alone, of 64: 110 against 93).
+// leave fewer wavefronts ready (2^26 elements in 4 + 1 + 1 heads of 128: 117 us against 127, 14 + 2 + 2 of
+// 64: 111 against 115, 32 + 8 + 8 of 128: 97 against 98; rotation alone, of 64: 110 against 93).
 constexpr int fwd_threads(bool bf16, bool norm) { return bf16 && norm ? 128 : 256; }
-// Most wavefronts of a backward with gains: as many as are resident at once (four per SIMD at
-// 126 registers), as each workgroup leaves a row of gain sums (the layer above: 145 us with
-// 4096, 154 with 8192, 187 with 32768).
+// Most wavefronts of a backward with gains, as each workgroup leaves a row of gain sums: as many as are
+// resident at once, four per SIMD, in kernels of up to 128 registers (the layer above: 140 us
+// with 4096, 143 with 8192, 152 with 32768).  Those are all but the fp32 ones of 2 to 16 lanes per head where tokens share a
+// wavefront: at 129 registers and 512 threads two per SIMD are resident, and the grid takes two rounds.
 constexpr int BWD_WAVES = 4096;
-// (32 lanes per head take 132 to 138 registers in workgroups of 512: one of them per CU.  Held
-// to 128 by a workgroup of 1024, 16 + 16 heads of 192, 256 MB of dy: 218 us against 314; with
-// 16 lanes per head the two are within 2%.)
+// 32 lanes per head (wider than 128): a workgroup of 1024 threads holds the kernel to 128 registers and so
+// four wavefronts per SIMD.  fp32 spills 24 bytes per lane for it (36 where tokens share a wavefront):
+// 16 + 8 + 8 heads of 144, 164 us against 220 with 512 threads, of 192, 149 against 178; bf16 spills
+// nothing: of 144, 255 against 273, of 192 and 256 within 2%.  With 16 lanes the two are within 2%.
 constexpr int bwd_threads(int g) { return g == 32 ? 1024 : 512; }
 
 // ---- vectors of V elements ------------------------------------------------------
@@ -69,8 +71,8 @@ struct Raw {
   uint32_t w[N];
 };
 // STREAM: nontemporal accesses, in the backward, which reads dy and x for the last time: the
-// layer above takes 141 us with them, 154 with the loads alone; 32 + 8 + 8 heads of 128 in fp32,
-// 5456 tokens, 143 and 154.  In the forward the loads cost 2 us.  (A store whose vector is
+// layer above takes 140 us with them, 154 with the loads alone; 32 + 8 + 8 heads of 128 in fp32,
+// 5456 tokens, 143 and 155.  In the forward the loads gain nothing (77 us against 76).  (A store whose vector is
 // filled element by element, or through a dependent type, loses the hint in hipcc.)
 __device__ inline u32x2 words(const uint32_t* w, u32x2) { return {w[0], w[1]}; }
 __device__ inline u32x3 words(const uint32_t* w, u32x3) { return {w[0], w[1], w[2]}; }
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(fwd_threads(sizeof(T) == 2, NORM)) void qk_fwd_kern
 // ---- backward of heads with a small point ---------------------------------------------
 // Rare, so it comes after the loop over the wavefront's groups, from memory to memory, an element
 // after the other: inside the loop it took the kernel from 126 registers to 138 or more, three
-// wavefronts per SIMD instead of four (4 + 1 + 1 heads of 128: 306 us against 209).
+// wavefronts per SIMD instead of four (4 + 1 + 1 heads of 128: 306 us against 220).
 // One head of a layer in a thousand: 152 us where there are none 141, all of them: 523.
 struct Points { float p, n; };
 template <typename T>
@@ -625,7 +627,7 @@ __global__ __launch_bounds__(bwd_threads(G)) void qk_bwd_kernel(QkArgs a, QkSpli
 
 // out[seg][j] (+)= scale * sum over the workgroups' rows of the segment: 16 columns
 // and 64 row groups per workgroup, added in a fixed order.  GU rows in flight per
-// thread: with one after the other a backward of 492 rows takes 1 to 1.5 us more; 8 or 4
+// thread: with one after the other a backward of 512 rows takes 1.5 us more or longer; 8 or 4
 // columns per workgroup take as long.
 __global__ __launch_bounds__(1024) void qk_gain_kernel(const double* part, int rows, int dh, double scale, float* dgq,
                                                        float* dgk, bool acc) {
@@ -662,10 +664,10 @@ int group_lanes(int dh, int v) {
 }
 // Pairs per lane: 4; in the bf16 forward 8 or 6 where a head divides into them (accesses of
 // 16 or 12 bytes), the number that leaves the fewest lanes idle, the larger of two alike.  The layer
-// above: 76 us with 8, 78 with 4; 16 + 4 + 4 heads of 256, 104 against 114; with the norm, 72-wide
-// heads take 115 us with 6 and 150 with 4, 144-wide ones 128 with 6 and 139 with 8, 96-wide ones
-// 109 with either.  In fp32 6 is slower (96-wide 104 us, 98 with 4), and so is more than 4 in
-// the backward: 8 leaves two wavefronts per SIMD (204 registers), 155 us against 145.
+// above: 76 us with 8, 77 with 4; 16 + 4 + 4 heads of 256, 105 against 132; with the norm, 72-wide
+// heads take 114 us with 6 and 150 with 4, 144-wide ones 132 with 6 and 142 with 8, 96-wide ones
+// 110 with 6 and 111 with 8.  In fp32 6 is slower (96-wide 104 us, 98 with 4), and so is more than 4 in
+// the backward: 8 leaves two wavefronts per SIMD (204 registers) and takes the layer above 7% longer.
 template <typename T, bool BWD>
 int lane_pairs(int dh) {
   int v = 4;
@@ -681,10 +683,12 @@ QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   // The group that gives the fewest pieces in all, the smallest such, if it saves enough: one
   // token per piece is a kernel of its own, which knows the token as a scalar and shares no
   // piece's angles with lanes of other tokens.  A fifth in the bf16 norm forward, whose arithmetic
-  // weighs most (28 + 4 + 4 heads of 128, a quarter saved: 106 us, 109 without), a third in other
-  // bf16 kernels (the same heads turned alone 102, 93 without; 5 + 5 + 5 of 40, three eighths
-  // saved, 128 and 150), two fifths in fp32 (8 + 1 + 1 of 128, three eighths saved, norm
-  // backward: 166 and 141; half of 4 + 1 + 1: 165 either way).
+  // weighs most (28 + 4 + 4 heads of 128, a quarter saved: 107 us, 108 without), a third in other
+  // bf16 kernels (the same heads turned alone, forward: 101, 94 without; 5 + 5 + 5 of 40, three
+  // eighths saved, 130 and 151, backward 192 and 189), two fifths in fp32 (8 + 1 + 1 of 128, three
+  // eighths saved, norm backward: 170 and 142).  Forward and backward share a threshold; at half
+  // saved in fp32 (4 + 1 + 1 of 128) the norm's forward gains by it, 101 and 116, and its
+  // backward loses, 169 and 141.
   const int worth = !bf16 ? 60 : !bwd && a.gq ? 80 : 66;
   int64_t C = 0, units = 0, most = 0;
   for (int g = 1; g <= 64 && g <= std::max(1, a.T); g *= 2) {
@@ -703,18 +707,19 @@ QkSplit split(const QkArgs& a, int v, bool bf16, bool bwd, bool values) {
   const int nw = (bwd ? bwd_threads(group_lanes(a.dh, v)) : fwd_threads(bf16, a.gq)) / 64;
   // Groups per wavefront.  Backward with the norm: as few as a resident grid leaves.  Elsewhere
   // short runs: many wavefronts, which the scheduler interleaves and which walk through memory
-  // closer to its order (the layer above forward 76 us, 84 with the 8 to 12 of a resident grid;
-  // rotation alone, backward: 98 against 109).  The norm pays for its gains with two tokens per
-  // wavefront in bf16 (65536 tokens: 562 us, 587 with one, 593 with four; fp32, 16384: 96 with
+  // closer to its order (the layer above forward 76 us, 86 with the 8 of a resident grid;
+  // rotation alone, backward: 98 against 108).  The norm pays for its gains with two tokens per
+  // wavefront in bf16 (65536 tokens: 562 us, 563 with one, 610 with four; fp32, 16384: 95 with
   // one, 100 with two), and with twice as many where a quarter or more of the lanes are idle
-  // (80-wide bf16 heads: 115 us with four, 128 with two), four times in heads wider than 128
-  // (136-wide in fp32: 118 us with four, 127 with two; 96-wide: 102 with four, 97 with two).
+  // (80-wide bf16 heads: 118 us with four, 125 with two; 96-wide fp32 ones 100 with two, 97 with one,
+  // 103 with four), four times in heads wider than 128 (136-wide in fp32: 121 us with four, 131 with
+  // two).
   // Up to SHORT units the chip is not full: one.
   constexpr int64_t SHORT = 16384, MOST = (int64_t)1 << 25;   // (a launch has fewer than 2^32 threads)
   int64_t step;
   if (bwd && a.gq) {
     // full steps of the resident grid and a rest (dealt evenly, 2048 tokens took seven steps of 293 where
-    // six of 341 and one of 2 do: 46.0 us against 44.8; the layer above 145.8 against 141.3)
+    // six of 341 and one of 2 do: 44.0 us against 42.3; the layer above 142.3 against 139.6)
     step = std::max<int64_t>(1, BWD_WAVES / C);
   } else {
     const int lanes = group_lanes(a.dh, v);
