@@ -28,7 +28,7 @@
 // The sums behind r and all that is formed from them once per head are fp64, with
 // S+- = mean(x.m^2 + x.d^2) +- 2 mean(x.m x.d) + e (no overflow or underflow; rho in
 // place of r.d keeps the elements' arithmetic in the normal range, too, up to |x| of
-// 1e37); the elements, and c, whose terms are bounded by du, are fp32; the gains' sums
+// 1e37, kappa up to 1e35 for e = 1e-5); the elements, and c, whose terms are bounded by du, are fp32; the gains' sums
 // are fp64; each output is rounded once to its type.  A head that holds a NaN or an
 // infinity gives NaN in all its elements, other heads are not touched by it.
 //

@@ -11,7 +11,7 @@ from tests.test_gpu_qk import BASE, EPS, _dt, _gains, _model, _pair
 pytestmark = pytest.mark.gpu
 
 # (magnitude, sign, 1 - x.d / x.m); None: an ordinary head
-KINDS = [None] + [(a, s, e) for a in (1.0, 1e2, 1e3, 1e5, 1e15, 1e30) for s in (1.0, -1.0) for e in (0.0, 1e-6, 2.0 ** -7)]
+KINDS = [None] + [(a, s, e) for a in (1.0, 1e2, 1e3, 1e5, 1e15, 1e30, 1e35) for s in (1.0, -1.0) for e in (0.0, 1e-6, 2.0 ** -7)]
 # about the ratio at which the smaller point's mean square counts as small: (0.1 / 0.9)^2 and (1 / 7)^2
 # lie on either side of 2^-6
 KINDS += [(1e3, s, e) for s in (1.0, -1.0) for e in (0.2, 0.25, 0.5)] + [None]
@@ -144,3 +144,38 @@ def test_a_few_of_them_in_a_long_batch(hq, hk, dh, dtype):
     og = R.backward_bound(x, cleared[1], hq, hk, dh, ang, gains, EPS)[1]
     for p, w, e, f, c in zip(dg, wg, pg, og, "qk"):
         R.check(p, w, e + f, f"dg.{c}")
+
+
+def test_replayed_in_a_graph():
+    """Heads with a small point in some replays, at places that change, and in none."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    hq, hk, dh, T = 4, 1, 128, 700
+    ncol = (hq + 2 * hk) * dh
+    side = torch.cuda.Stream()
+    m, eager = _model(fd, hq, hk, dh, "f32", stream=side.cuda_stream), _model(fd, hq, hk, dh, "f32")
+    gains = _gains(torch, dh, torch.float32, 1)
+    x = _pair(torch, T, ncol, torch.float32, 2)
+    dy = _pair(torch, T, ncol, torch.float32, 3)
+    y, dx = (tuple(torch.empty_like(t) for t in x) for _ in range(2))
+    dg = tuple(torch.empty(dh, device="cuda") for _ in range(2))
+    sc = m.qk_scratch(1, T)
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            m.qk_forward(x, T, gains=gains, eps=EPS, out=y)
+            m.qk_backward(dy, T, x=x, gains=gains, eps=EPS, out=dx, gain_grads=dg, scratch=sc)
+    torch.cuda.synchronize()
+    for step, few in enumerate((0, 5, 0, T, 1)):
+        for t, s in zip(x, _pair(torch, T, ncol, torch.float32, 10 + step)):
+            t.copy_(s)
+        rows = torch.randperm(T, generator=torch.Generator().manual_seed(step))[:few].cuda()
+        x[0][rows] *= 1e4
+        x[1][rows] = x[0][rows] if step % 2 else -x[0][rows]
+        want = (*eager.qk_forward(x, T, gains=gains, eps=EPS),)
+        wdx, wdg = eager.qk_backward(dy, T, x=x, gains=gains, eps=EPS)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*y, *dx, *dg), (*want, *wdx, *wdg))), step
