@@ -142,6 +142,15 @@ typedef struct fdh_qk_gains {
   double eps;               /* the points are q + eps v_q and q - eps v_q; positive, finite */
 } fdh_qk_gains;
 
+/* The tables of the token embedding (device pointers). */
+typedef struct fdh_embed_tables {
+  const void* e;            /* [vocab][d_model] of the context's dtype */
+  const float* v_e;         /* its direction; NULL: the same table at both points */
+  const void* p;            /* GPT-2 family: [>= S][d_model] learned positions; Llama family: NULL */
+  const float* v_p;         /* their direction or NULL */
+  double eps;               /* the points are e + eps v_e and e - eps v_e; positive, finite */
+} fdh_embed_tables;
+
 typedef struct fdh_ctx fdh_ctx;
 
 /* Create a context for one model on the current HIP device; hip_stream is a
@@ -281,6 +290,37 @@ fdh_status fdh_qk_backward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_
                            int64_t lddy, void* dx_m, void* dx_d, int64_t lddx, float* dgq, float* dgk,
                            int32_t accumulate, void* scratch, size_t scratch_bytes);
 fdh_status fdh_qk_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes);
+
+/* Scale of the token embedding (1 after fdh_create): the model's first layer reads
+ * scale * e[token] (+ p[position] for the GPT-2 family, whose positions and tied head
+ * are not scaled).  Positive and finite.  Takes effect for every following call, the
+ * products of a bound operator among them. */
+fdh_status fdh_set_embed_scale(fdh_ctx* ctx, double scale);
+
+/* The token embedding on caller-owned device memory, as the HVP runs it (language-model
+ * families).  x: float32 pair (_m mean, _d half difference of the values at the two
+ * points), B*S rows ldx elements apart, row t = scale e[token t] + p[t % S].  Tables and x
+ * 16-byte aligned, ldx a multiple of 4; directions and tokens of any element alignment.
+ * x overlaps neither an input nor itself.  A token outside [0, vocab) has no row: its
+ * row of x is NaN.  Any B*S from 0 to 2^31 - 64; S <= max_seq for the GPT-2 family.
+ * Outputs are rounded once.  Only enqueued on the context stream (no wait, no
+ * allocation: may be captured in a graph); one token is the call with B = S = 1. */
+fdh_status fdh_embed_forward(fdh_ctx* ctx, const fdh_embed_tables* tables, const int32_t* tokens_dev, int32_t B, int32_t S,
+                             float* x_m, float* x_d, int64_t ldx);
+
+/* Its backward: the tables' entries of Hv from dx_d, the half difference of the gradient of
+ * x (float32, rows lddx apart, 16-byte aligned):
+ *   hv_e[r] = scale / eps * sum of dx_d over the positions of token r   [vocab][d_model]
+ *   hv_p[s] = 1 / eps * sum over the batch of dx_d at position s        [max_seq][d_model]
+ * (hv_p: GPT-2 family, NULL otherwise), both whole, with zeros in the other rows, or with
+ * accumulate != 0 added to what is there.  fp64 sums in an order that the tokens alone
+ * set: the same bits in every call.  Positions of tokens outside [0, vocab) are left out.
+ * scratch: device memory, 16-byte aligned, of at least fdh_embed_scratch_bytes, in use
+ * until the call's work is done: calls that may overlap on the device need scratch of
+ * their own.  No output overlaps an input.  Only enqueued, as fdh_embed_forward. */
+fdh_status fdh_embed_backward(fdh_ctx* ctx, const int32_t* tokens_dev, int32_t B, int32_t S, const float* dx_d, int64_t lddx,
+                              double eps, float* hv_e, float* hv_p, int32_t accumulate, void* scratch, size_t scratch_bytes);
+fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes);
 
 /* hv = H v of the bound operator (fdh_bind or fdh_bind_dataset): one FD-HVP
  * per batch, accumulated into hv in batch order; fdh_last_losses then returns

@@ -1,6 +1,7 @@
 // C ABI (include/fdhvp.h): argument validation and dispatch to the engine.
 // No exception crosses this boundary.
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -245,6 +246,35 @@ fdh_status fdh_qk_backward(fdh_ctx* ctx, const fdh_qk_gains* gains, const int32_
   return run(ctx, [&](fdh::Engine& e) {
     return e.qk_backward(gains, positions_dev, B, S, x_m, x_d, ldx, dy_m, dy_d, lddy, dx_m, dx_d, lddx, dgq, dgk,
                          accumulate != 0, scratch, scratch_bytes);
+  });
+}
+
+fdh_status fdh_set_embed_scale(fdh_ctx* ctx, double scale) {
+  return run(ctx, [&](fdh::Engine& e) -> int {
+    if (e.quad) { e.err = "needs a language-model context"; return FDH_ERR_UNSUPPORTED; }
+    if (!(scale > 0.0) || !std::isfinite(scale)) { e.err = "the scale must be positive and finite"; return FDH_ERR_INVALID_ARG; }
+    e.embed_scale = scale;
+    return FDH_OK;
+  });
+}
+
+fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes) {
+  if (!ctx || !ctx->eng || !bytes || B < 0 || S < 0) return FDH_ERR_INVALID_ARG;
+  const fdh::Engine& e = *ctx->eng;
+  if (e.quad || (int64_t)B * S > fdh::END_MAX_TOKENS) return FDH_ERR_UNSUPPORTED;
+  *bytes = fdh::embed_scratch_bytes((int64_t)B * S, e.d);
+  return FDH_OK;
+}
+
+fdh_status fdh_embed_forward(fdh_ctx* ctx, const fdh_embed_tables* tables, const int32_t* tokens_dev, int32_t B, int32_t S,
+                             float* x_m, float* x_d, int64_t ldx) {
+  return run(ctx, [&](fdh::Engine& e) { return e.embed_forward(tables, tokens_dev, B, S, x_m, x_d, ldx); });
+}
+
+fdh_status fdh_embed_backward(fdh_ctx* ctx, const int32_t* tokens_dev, int32_t B, int32_t S, const float* dx_d, int64_t lddx,
+                              double eps, float* hv_e, float* hv_p, int32_t accumulate, void* scratch, size_t scratch_bytes) {
+  return run(ctx, [&](fdh::Engine& e) {
+    return e.embed_backward(tokens_dev, B, S, dx_d, lddx, eps, hv_e, hv_p, accumulate != 0, scratch, scratch_bytes);
   });
 }
 

@@ -73,7 +73,7 @@ struct WsLayout {
   std::vector<LayerSpans> ls;
   Span xL_m, xL_d, f_m, f_d, lo, sc_m, sc_d, log_m, log_d, dlog_m, dlog_d, rowloss, losses;
   Span dx0_m, dx0_d, dx1_m, dx1_d, dxo_m, dxo_d, dz_m, dz_d, dgu_m, dgu_d, db_m, db_d, gpart, do_m, do_d, dS_m, dS_d;
-  Span dqkv_m, dqkv_d, dqkvo_m, dqkvo_d, gqa_m, gqa_d, dl, da_m, da_d, keys, rope, cdf, gpartial, bpart, bout;
+  Span dqkv_m, dqkv_d, dqkvo_m, dqkvo_d, gqa_m, gqa_d, dl, da_m, da_d, emb, rope, cdf, gpartial, bpart, bout;
   Span tcount;  // two int64 counters of fdh_bind_dataset
   Span nfflag;  // non-finite flags of the input direction and the product (two int32)
   Span wsplit;  // split-K partial products of the weight-gradient GEMMs
@@ -101,6 +101,7 @@ class Engine : public WsLayout {
   fdh_model_config cfg;
   bool qk_norm = false;
   int n_axes = 1;
+  double embed_scale = 1.0;   // of the token rows (not of learned positions)
   QkRotary rot{};   // angles of the position rotation (Llama, head_dim <= QK_MAX_DH)
   hipStream_t stream;
   bool gpt2 = false, llama = false, quad = false, bf16 = false;
@@ -161,6 +162,11 @@ class Engine : public WsLayout {
   int qk_backward(const fdh_qk_gains* g, const int32_t* pos, int B, int S, const void* x_m, const void* x_d, int64_t ldx,
                   const float* dy_m, const float* dy_d, int64_t lddy, void* dx_m, void* dx_d, int64_t lddx, float* dgq,
                   float* dgk, bool acc, void* scratch, size_t scratch_bytes);
+  // the embedding on caller-owned memory (fdh_embed_forward, fdh_embed_backward)
+  int embed_check(const int32_t* tok, int B, int S);
+  int embed_forward(const fdh_embed_tables* w, const int32_t* tok, int B, int S, float* x_m, float* x_d, int64_t ldx);
+  int embed_backward(const int32_t* tok, int B, int S, const float* dx_d, int64_t lddx, double eps, float* hv_e, float* hv_p,
+                     bool acc, void* scratch, size_t scratch_bytes);
   std::vector<int64_t> layer_ranges() const;
 
  private:

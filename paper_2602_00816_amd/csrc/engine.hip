@@ -15,6 +15,7 @@
 // and the half difference themselves, without a difference of nearly equal
 // values.  theta is never written.
 #include "engine.h"
+#include "regions.h"
 
 #include <algorithm>
 #include <functional>
@@ -336,7 +337,7 @@ size_t Engine::plan(int B, int S, int m, const fdh_lanczos_opts* o, WsLayout* ou
       if (nm > 1) mx = std::max(mx, (size_t)nm * d * F * 4);
       take(W.wsplit, mx);
     }
-    take(W.keys, T_ * 4);
+    take(W.emb, embed_scratch_bytes((int64_t)T_, d));
     take(W.rope, (size_t)Smax * dh * 8);
     take(W.cdf, (size_t)V * 8);
   }
@@ -415,7 +416,7 @@ uint64_t Engine::layout_digest() const {
   for (const Span* x : {&xL_m, &xL_d, &f_m, &f_d, &lo, &sc_m, &sc_d, &log_m, &log_d, &dlog_m, &dlog_d, &rowloss,
                         &losses, &dx0_m, &dx0_d, &dx1_m, &dx1_d, &dxo_m, &dxo_d, &dz_m, &dz_d, &dgu_m, &dgu_d,
                         &db_m, &db_d, &gpart, &do_m, &do_d, &dS_m, &dS_d, &dqkv_m, &dqkv_d, &dqkvo_m, &dqkvo_d, &gqa_m,
-                        &gqa_d, &dl, &da_m, &da_d, &keys, &rope, &cdf, &gpartial, &bpart, &bout, &tcount,
+                        &gqa_d, &dl, &da_m, &da_d, &emb, &rope, &cdf, &gpartial, &bpart, &bout, &tcount,
                         &nfflag, &wsplit, &lz_w, &lz_q, &lz_qp, &lz_basis, &lz_alpha, &lz_beta, &lz_coef, &lz_gram,
                         &lz_partial, &lz_flag, &lz_maxabs})
     sp(*x);
@@ -763,8 +764,8 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
   // ================= forward =================
   {
     PairF x0{F32(ls.empty() ? xL_m : ls[0].x_in_m), F32(ls.empty() ? xL_d : ls[0].x_in_d)};
-    CK(launch_embed_fwd<T>(x0, tok, T_, S, d, V, th + wte.off, v + wte.off, gpt2 ? th + wpe.off : nullptr,
-                           gpt2 ? v + wpe.off : nullptr, eps, nf + 2, st));
+    const EmbedTables et{th + wte.off, v + wte.off, gpt2 ? th + wpe.off : nullptr, gpt2 ? v + wpe.off : nullptr, eps, embed_scale};
+    CK(launch_embed_fwd<T>(x0, d, tok, T_, S, d, V, et, nf + 2, st));
   }
   // one decoder layer's forward from its stored input pair x_in: norm 1, qkv,
   // attention, output projection + residual, norm 2, MLP and, with
@@ -1071,14 +1072,9 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
     std::swap(dxd, dyd);
   }
   // embeddings (difference channel of the gradient w.r.t. the embedding output)
-  CK(launch_token_sort((uint32_t*)(ws + keys.off), tok, T_, V, st));
   // (GPT-2 ties the embedding to the head, whose gradient is already in hv)
-  if (!gpt2 && !acc) CK(launch_fill_f32(hv + wte.off, (int64_t)V * d, 0.f, st));
-  CK(launch_embed_bwd(hv + wte.off, (const uint32_t*)(ws + keys.off), dxd, T_, d, 1.0 / eps, gpt2 || acc, st));
-  if (gpt2) {
-    CK(launch_pos_bwd(hv + wpe.off, dxd, B, S, d, 1.0 / eps, acc, st));
-    if (Smax > S && !acc) CK(launch_fill_f32(hv + wpe.off + (int64_t)S * d, (int64_t)(Smax - S) * d, 0.f, st));
-  }
+  CK(launch_embed_bwd(hv + wte.off, tok, dxd, d, T_, d, V, embed_scale / eps, gpt2 || acc, ws + emb.off, st));
+  if (gpt2) CK(launch_pos_bwd(hv + wpe.off, dxd, d, B, S, d, 1.0 / eps, Smax, acc, st));
   (void)dxm;
   return FDH_OK;
 #undef RC
@@ -1232,44 +1228,6 @@ int Engine::last_losses(double* lp, double* lm) {
 // ---------------------------------------------------------------------------
 // the q/k front of a layer on caller-owned pairs
 // ---------------------------------------------------------------------------
-namespace {
-
-// rows of `width` bytes, `ld` bytes apart
-struct Region {
-  const char* p;
-  int64_t rows, ld, width;
-};
-Region flat(const void* p, int64_t bytes) { return {(const char*)p, 1, bytes, bytes}; }
-
-// whether a byte of one may lie in the other: regions of the same row stride are
-// told apart by their columns (two slices of one wide buffer do not overlap)
-bool overlap(const Region& a, const Region& b) {
-  if (!a.p || !b.p || a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0) return false;
-  const Region &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
-  const int64_t gap = hi.p - lo.p;
-  if (gap >= (lo.rows - 1) * lo.ld + lo.width) return false;
-  if (lo.ld != hi.ld) return true;
-  const int64_t c = gap % lo.ld;
-  return !(c >= lo.width && lo.ld - c >= hi.width);
-}
-
-bool any_overlap(const Region* w, int nw, const Region* r, int nr) {
-  for (int i = 0; i < nw; ++i) {
-    for (int j = i + 1; j < nw; ++j)
-      if (overlap(w[i], w[j])) return true;
-    for (int j = 0; j < nr; ++j)
-      if (overlap(w[i], r[j])) return true;
-  }
-  return false;
-}
-
-// a [rows][ld] operand of `size`-byte elements: 16-byte accesses and row offsets in 64 bits
-bool bad_rows(const void* p, int64_t ld, int64_t cols, int size) {
-  return !p || (uintptr_t)p % 16 || ld < cols || ld > ((int64_t)1 << 31) || ld * size % 16;
-}
-
-}  // namespace
-
 // the shape and gains of a call, shared by both directions
 int Engine::qk_check(const fdh_qk_gains* g, int B, int S, QkArgs* a) {
   if (!llama) { err = "needs a Llama-family context"; return FDH_ERR_UNSUPPORTED; }

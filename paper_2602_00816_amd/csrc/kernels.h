@@ -112,13 +112,6 @@ template <typename T> struct PairT { T* m; T* d; };
 template <typename T>
 hipError_t launch_cast_pair(PairT<T> out, const float* m, const float* d, int64_t n, hipStream_t s);
 
-// x = E[tok] (+ Pos[s]);  m = theta rows, d = eps * v rows; bad_tok[0] = 1
-// (when bad_tok is not null) if a token lies outside [0, V) (it is clamped)
-template <typename T>
-hipError_t launch_embed_fwd(PairF x, const int32_t* tok, int T_, int S, int dmodel, int V,
-                            const T* th_e, const float* v_e, const T* th_p, const float* v_p, double eps, int* bad_tok,
-                            hipStream_t s);
-
 // Norm forward at both points: y = norm(x; g +- eps vg, b +- eps vb)
 template <typename T>
 hipError_t launch_norm_fwd(PairT<T> y, const float* xm, const float* xd, int rows, int dmodel, bool layernorm,
@@ -289,11 +282,30 @@ hipError_t launch_loss_sum(double* out2, const double* rowloss, int T_, bool acc
 // than IGNORE_LABEL (lab may be null: next-token targets), out3[2] += tokens outside [0, V)
 hipError_t launch_count_targets(int64_t* out3, const int32_t* tok, const int32_t* lab, int B, int S, int V, hipStream_t s);
 
-// embedding backward (difference channel only): deterministic sort + segment sums
-hipError_t launch_token_sort(uint32_t* keys, const int32_t* tok, int T_, int V, hipStream_t s);
-hipError_t launch_embed_bwd(float* hv_e, const uint32_t* keys, const float* dxd, int T_, int dmodel, double inv_eps,
-                            bool accumulate, hipStream_t s);
-hipError_t launch_pos_bwd(float* hv_p, const float* dxd, int B, int S, int dmodel, double inv_eps, bool accumulate,
+// ---- embed.hip: token embedding and the gradients of its tables -----------------------
+// (v, hv and dx of any element alignment; the tables' rows 16-byte aligned)
+constexpr int64_t END_MAX_TOKENS = ((int64_t)1 << 31) - 64;
+struct EmbedTables {
+  const void* e;        // [V][dm], operand type
+  const float* ve;      // its direction or null
+  const void* p;        // [>= S][dm] positions or null
+  const float* vp;      // their direction or null
+  double eps, scale;
+};
+// x (rows ldx apart) = scale e[tok] (+ p[t % S]);  m from the tables, d = eps times their
+// directions' rows.  Rows of tokens outside [0, V) are NaN, and bad_tok[0] = 1 where
+// bad_tok is not null
+template <typename T>
+hipError_t launch_embed_fwd(PairF x, int64_t ldx, const int32_t* tok, int64_t T_, int S, int dm, int V, const EmbedTables& w,
+                            int* bad_tok, hipStream_t s);
+size_t embed_scratch_bytes(int64_t T_, int dm);
+// hv_e[r] = mul * sum over positions t of token r of dxd[t] (zeros for the others), or with
+// acc added to the rows of the batch's tokens.  scratch: embed_scratch_bytes, 16-byte aligned
+hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, int64_t ld, int64_t T_, int dm, int V, double mul,
+                            bool acc, void* scratch, hipStream_t s);
+// hv_p[s] = inv_eps * sum_b dxd[b S + s] for s < S and 0 for S <= s < rows, or with acc
+// added to the first min(S, rows) rows
+hipError_t launch_pos_bwd(float* hv_p, const float* dxd, int64_t ld, int B, int S, int dm, double inv_eps, int64_t rows, bool acc,
                           hipStream_t s);
 
 }  // namespace fdh

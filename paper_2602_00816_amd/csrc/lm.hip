@@ -38,32 +38,9 @@ __global__ void cast_pair_kernel(PairT<T> o, const float* m, const float* d, int
   }
 }
 
-// ---- embedding ----------------------------------------------------------------
-// token ids outside [0, V) are clamped so that no access leaves the tables;
-// the embedding forward reports them (bad_tok[0] = 1) and the call that
-// launched it turns that into an invalid-argument error
+// token ids outside [0, V) are clamped where a target is read, so that no access leaves
+// the logits; the embedding reports them
 __device__ inline int clamp_tok(int t, int V) { return t < 0 ? 0 : (t >= V ? V - 1 : t); }
-
-template <typename T>
-__global__ void embed_fwd_kernel(PairF x, const int32_t* tok, int T_, int S, int dm, int V, const T* the, const float* ve,
-                                 const T* thp, const float* vp, double eps, int* bad_tok) {
-  const int64_t n = (int64_t)T_ * dm;
-  GRID_LOOP(i, n) {
-    const int t = (int)(i / dm), j = (int)(i % dm);
-    const int tk = tok[t];
-    if ((tk < 0 || tk >= V) && bad_tok && j == 0) bad_tok[0] = 1;
-    const int64_t r = (int64_t)clamp_tok(tk, V) * dm + j;
-    double xp = (double)ldf(the, r) + eps * (double)ve[r];
-    double xm = (double)ldf(the, r) - eps * (double)ve[r];
-    if (thp) {
-      const int64_t pr = (int64_t)(t % S) * dm + j;
-      xp += (double)ldf(thp, pr) + eps * (double)vp[pr];
-      xm += (double)ldf(thp, pr) - eps * (double)vp[pr];
-    }
-    x.m[i] = (float)(0.5 * (xp + xm));
-    x.d[i] = (float)(0.5 * (xp - xm));
-  }
-}
 
 // ---- LayerNorm / RMSNorm ---------------------------------------------------------
 // one workgroup per row
@@ -1149,114 +1126,12 @@ __global__ void count_targets_kernel(int64_t* out, const int32_t* tok, const int
   }
 }
 
-// ---- embedding backward --------------------------------------------------------------
-// Sorted keys by rank: keys = token << 14 | position (positions < 2^14) are
-// distinct, so the rank of a key is the number of smaller ones.  A workgroup
-// holds all keys in LDS and ranks 32 of them, 8 lanes each (T^2 / 8 comparisons
-// per lane group over the whole chip; one workgroup's bitonic sort of 8192 keys
-// took 100 us, this 26).
-constexpr int SORT_N = 16384;
-__global__ __launch_bounds__(NT) void token_sort_kernel(uint32_t* keys, const int32_t* tok, int T_, int V) {
-  extern __shared__ uint32_t k[];   // [round_up(T, 4)]
-  const int n4 = (T_ + 3) / 4;
-  for (int i0 = threadIdx.x; i0 < 4 * n4; i0 += 8 * NT) {
-    int t[8];   // eight loads in flight
-#pragma unroll
-    for (int u = 0; u < 8; ++u) t[u] = tok[min(i0 + u * NT, T_ - 1)];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int i = i0 + u * NT;
-      if (i < 4 * n4) k[i] = i < T_ ? (((uint32_t)clamp_tok(t[u], V) << 14) | (uint32_t)i) : 0xFFFFFFFFu;
-    }
-  }
-  __syncthreads();
-  const int i = blockIdx.x * (NT / 8) + (threadIdx.x >> 3);
-  const uint32_t own = k[min(i, T_ - 1)];
-  int rank = 0;
-  for (int q = threadIdx.x & 7; q < n4; q += 8) {
-    const uint4 x = *reinterpret_cast<const uint4*>(k + 4 * q);
-    rank += (int)(x.x < own) + (int)(x.y < own) + (int)(x.z < own) + (int)(x.w < own);
-  }
-  rank += __shfl_xor(rank, 1, 64);
-  rank += __shfl_xor(rank, 2, 64);
-  rank += __shfl_xor(rank, 4, 64);
-  if ((threadIdx.x & 7) == 0 && i < T_) keys[rank] = own;
-}
-
-// One workgroup per (sorted position, NT-column chunk); only segment starts
-// work.  The segment end is found by binary search in the sorted keys, and the
-// segment's rows are summed with 16 partial sums (row q of the segment into
-// partial q % 16, combined in a fixed order), the next rows' keys loaded ahead:
-// a frequent token (hundreds of rows under a Zipf distribution) is a chain of
-// loads, which bounds the kernel.  8192 x 512: 81 -> 70 us (8 rows in flight).
-__global__ void embed_bwd_kernel(float* hv, const uint32_t* keys, const float* dxd, int T_, int dm, double inv_eps,
-                                 bool acc) {
-  const int j = blockIdx.x;
-  const uint32_t tk = keys[j] >> 14;
-  if (j > 0 && (keys[j - 1] >> 14) == tk) return;
-  int lo = j + 1, hi = T_;   // first position with a larger token
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if ((keys[mid] >> 14) == tk) lo = mid + 1;
-    else hi = mid;
-  }
-  const int e = lo;
-  const int c = blockIdx.y * NT + threadIdx.x;
-  if (c >= dm) return;
-  constexpr int U = 16;
-  double s[U];
-  uint32_t pos[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    s[u] = 0.0;
-    pos[u] = keys[min(j + u, T_ - 1)] & 0x3FFFu;
-  }
-  int q = j;
-  for (; q + U <= e; q += U) {
-    float x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = dxd[(int64_t)pos[u] * dm + c];
-#pragma unroll
-    for (int u = 0; u < U; ++u) pos[u] = keys[min(q + U + u, T_ - 1)] & 0x3FFFu;
-#pragma unroll
-    for (int u = 0; u < U; ++u) s[u] += (double)x[u];
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (q + u < e) s[u] += (double)dxd[(int64_t)pos[u] * dm + c];
-#pragma unroll
-  for (int w = U / 2; w > 0; w /= 2)
-#pragma unroll
-    for (int u = 0; u < w; ++u) s[u] += s[u + w];
-  const int64_t idx = (int64_t)tk * dm + c;
-  hv[idx] = acc ? (float)((double)hv[idx] + s[0] * inv_eps) : (float)(s[0] * inv_eps);
-}
-
-__global__ void pos_bwd_kernel(float* hv, const float* dxd, int B, int S, int dm, double inv_eps, bool acc) {
-  const int64_t n = (int64_t)S * dm;
-  GRID_LOOP(i, n) {
-    const int s = (int)(i / dm), c = (int)(i % dm);
-    double a = 0.0;
-    for (int b = 0; b < B; ++b) a += (double)dxd[((int64_t)b * S + s) * dm + c];
-    const float x = (float)(a * inv_eps);
-    hv[i] = acc ? hv[i] + x : x;
-  }
-}
-
 }  // namespace
 
 // ================================ launchers ==============================================
 template <typename T>
 hipError_t launch_cast_pair(PairT<T> out, const float* m, const float* d, int64_t n, hipStream_t s) {
   hipLaunchKernelGGL(cast_pair_kernel<T>, dim3(grid_for(n)), dim3(NT), 0, s, out, m, d, n);
-  return hipGetLastError();
-}
-
-template <typename T>
-hipError_t launch_embed_fwd(PairF x, const int32_t* tok, int T_, int S, int dm, int V, const T* the, const float* ve,
-                            const T* thp, const float* vp, double eps, int* bad_tok, hipStream_t s) {
-  hipLaunchKernelGGL(embed_fwd_kernel<T>, dim3(grid_for((int64_t)T_ * dm)), dim3(NT), 0, s, x, tok, T_, S, dm, V, the,
-                     ve, thp, vp, eps, bad_tok);
   return hipGetLastError();
 }
 
@@ -1441,26 +1316,8 @@ hipError_t launch_count_targets(int64_t* out3, const int32_t* tok, const int32_t
   return hipGetLastError();
 }
 
-hipError_t launch_token_sort(uint32_t* keys, const int32_t* tok, int T_, int V, hipStream_t s) {
-  if (T_ > SORT_N) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(token_sort_kernel, dim3(ceil_div(T_, NT / 8)), dim3(NT), (size_t)(T_ + 3) / 4 * 16, s, keys, tok, T_, V);
-  return hipGetLastError();
-}
-hipError_t launch_embed_bwd(float* hv, const uint32_t* keys, const float* dxd, int T_, int dm, double inv_eps, bool acc,
-                            hipStream_t s) {
-  hipLaunchKernelGGL(embed_bwd_kernel, dim3(T_, (dm + NT - 1) / NT), dim3(NT), 0, s, hv, keys, dxd, T_, dm, inv_eps,
-                     acc);
-  return hipGetLastError();
-}
-hipError_t launch_pos_bwd(float* hv, const float* dxd, int B, int S, int dm, double inv_eps, bool acc, hipStream_t s) {
-  hipLaunchKernelGGL(pos_bwd_kernel, dim3(grid_for((int64_t)S * dm)), dim3(NT), 0, s, hv, dxd, B, S, dm, inv_eps, acc);
-  return hipGetLastError();
-}
-
 #define INST_T(T)                                                                                                     \
   template hipError_t launch_cast_pair<T>(PairT<T>, const float*, const float*, int64_t, hipStream_t);                 \
-  template hipError_t launch_embed_fwd<T>(PairF, const int32_t*, int, int, int, int, const T*, const float*, const T*, \
-                                          const float*, double, int*, hipStream_t);                                    \
   template hipError_t launch_norm_fwd<T>(PairT<T>, const float*, const float*, int, int, bool, const T*, const float*, \
                                          const T*, const float*, double, float, hipStream_t);                          \
   template hipError_t launch_norm_bwd<T>(PairF, PairT<T>, const float*, const float*, const float*, const float*,      \

@@ -50,6 +50,10 @@ class QkGains(C.Structure):
     _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v_q", C.c_void_p), ("v_k", C.c_void_p), ("eps", C.c_double)]
 
 
+class EmbedTables(C.Structure):
+    _fields_ = [("e", C.c_void_p), ("v_e", C.c_void_p), ("p", C.c_void_p), ("v_p", C.c_void_p), ("eps", C.c_double)]
+
+
 class LanczosOpts(C.Structure):
     _fields_ = [("reorth", C.c_int32), ("window", C.c_int32), ("basis_dtype", C.c_int32),
                 ("breakdown_tol", C.c_float)]
@@ -101,6 +105,10 @@ def lib():
         "fdh_qk_forward": (i32, [vp, C.POINTER(QkGains), vp, i32, i32, vp, vp, i64, vp, vp, i64]),
         "fdh_qk_backward": (i32, [vp, C.POINTER(QkGains), vp, i32, i32, vp, vp, i64, vp, vp, i64, vp, vp, i64, vp, vp,
                                   i32, vp, C.c_size_t]),
+        "fdh_set_embed_scale": (i32, [vp, f64]),
+        "fdh_embed_scratch_bytes": (i32, [vp, i32, i32, C.POINTER(C.c_size_t)]),
+        "fdh_embed_forward": (i32, [vp, C.POINTER(EmbedTables), vp, i32, i32, vp, vp, i64]),
+        "fdh_embed_backward": (i32, [vp, vp, i32, i32, vp, i64, f64, vp, vp, i32, vp, C.c_size_t]),
         "fdh_hvp_bound": (i32, [vp, vp, vp]),
         "fdh_set_basis_offload": (i32, [vp, i32, vp, C.c_size_t]),
         "fdh_lanczos": (i32, [vp, i32, u64, C.POINTER(LanczosOpts), pd, pd, pi]),
@@ -201,12 +209,13 @@ class Model:
     Llama family: qk_norm norms every query and key head before the rotation;
     rope_sections (rotated pairs per position axis, together head_dim / 2)
     rotates over several axes, rope_interleaved deals the axes' pairs in turn.
+    embed_scale: factor of the token embedding (set_embed_scale).
     stream: a hipStream_t (torch's ``stream.cuda_stream``); None is the default
     stream."""
 
     def __init__(self, family: str, n_layers=0, d_model=0, n_heads=1, n_kv_heads=0, d_ff=0, vocab=0,
                  max_seq=0, dtype="f32", norm_eps=1e-5, rope_base=10000.0, quad_n=0, stream=None, qk_norm=False,
-                 rope_sections=None, rope_interleaved=False):
+                 rope_sections=None, rope_interleaved=False, embed_scale=1.0):
         self._L = lib()
         self.cfg = ModelConfig(FAMILY[family], n_layers, d_model, n_heads, n_kv_heads or n_heads, d_ff, vocab,
                                max_seq, DTYPE[dtype], norm_eps, rope_base, 0, quad_n)
@@ -228,13 +237,16 @@ class Model:
         self._ws = None
         self._keep = []        # tensors the bound operator points to
         self._diag = None      # QUAD_DIAG diagonal the context points to
+        self._d, self._vocab, self._max_seq = d_model, vocab, max_seq
+        if embed_scale != 1.0:
+            self.set_embed_scale(embed_scale)
 
     @classmethod
     def from_workload(cls, w: dict, stream=None):
         return cls(w["family"], w["n_layers"], w["d_model"], w["n_heads"], w["n_kv_heads"], w["d_ff"],
                    w["vocab"], w["max_seq"], w["dtype"], rope_base=w["rope_base"], stream=stream,
                    qk_norm=w.get("qk_norm", False), rope_sections=w.get("rope_sections"),
-                   rope_interleaved=w.get("rope_interleaved", False))
+                   rope_interleaved=w.get("rope_interleaved", False), embed_scale=w.get("embed_scale", 1.0))
 
     def close(self):
         if getattr(self, "_h", None):
@@ -289,6 +301,10 @@ class Model:
         set_workspace: keep only each layer's input pair and rerun the layer's
         forward before its backward (same results, less memory)."""
         self._check(self._L.fdh_set_recompute(self._h, 1 if on else 0), "fdh_set_recompute")
+
+    def set_embed_scale(self, scale: float):
+        """Factor of the token embedding in every following call (1 by default)."""
+        self._check(self._L.fdh_set_embed_scale(self._h, float(scale)), "fdh_set_embed_scale")
 
     # ---- memory ----
     def set_workspace(self, B=0, S=0, m=0, o: LanczosOpts | None = None):
@@ -452,6 +468,55 @@ class Model:
             pos = positions.data_ptr()
         return dev, g, pos, T // seq
 
+    def _call_device(self, t):
+        """The device of a call on caller-owned tensors; refuses a current device or stream
+        that is not the call's."""
+        import torch
+        dev = t.get_device()
+        if dev < 0 or dev != torch.cuda.current_device():
+            raise ValueError("tensors must lie on the current device")
+        if _current_stream(dev) != self._stream:
+            raise ValueError("the current stream is not the model's: build the model with stream=<the current stream>")
+        return dev
+
+    @staticmethod
+    def _rows(t, what, dtype, T, n, dev):
+        """Pointer and row stride of a [T, n] tensor with contiguous rows."""
+        if t.dim() != 2 or t.shape[0] != T or t.shape[1] != n or t.dtype is not dtype:
+            raise ValueError(f"{what} must be a [{T}, {n}] tensor of {dtype}")
+        ld, one = t.stride()
+        if one != 1 and n > 1:
+            raise ValueError(f"{what}: the elements of a row must be contiguous")
+        if t.get_device() != dev:
+            raise ValueError("tensors must lie on the current device")
+        return t.data_ptr(), n if T <= 1 else ld
+
+    def _row_pair(self, pair, what, dtype, T, n, dev):
+        """Pointers and the common row stride of a pair of them."""
+        m, d = pair
+        pm, lm = self._rows(m, what, dtype, T, n, dev)
+        pd, ld = self._rows(d, what, dtype, T, n, dev)
+        if lm != ld:
+            raise ValueError(f"{what}: both tensors must have the same row stride")
+        return pm, pd, lm
+
+    @staticmethod
+    def _whole(t, what, dtype, n, dev):
+        """Pointer of a contiguous tensor of n elements."""
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} elements")
+        if t.get_device() != dev:
+            raise ValueError("tensors must lie on the current device")
+        return t.data_ptr()
+
+    @staticmethod
+    def _scratch_arg(t, dev):
+        if t is None:
+            return 0, 0
+        if not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError("scratch must be contiguous and lie on the current device")
+        return t.data_ptr(), t.numel() * t.element_size()
+
     @functools.cached_property
     def _qk_dtype(self):
         import torch
@@ -526,6 +591,81 @@ class Model:
         if st < 0:
             self._check(st, "fdh_qk_backward")
         return (out, gain_grads) if self.qk_norm else out
+
+    # ---- the two ends of the model ----
+    def _embed_tokens(self, tokens):
+        import torch
+        if tokens.dtype is not torch.int32 or tokens.dim() != 2 or not tokens.is_contiguous():
+            raise ValueError("tokens must be a contiguous int32 [B, S] tensor on the device")
+        dev = self._call_device(tokens)
+        B, S = tokens.shape
+        return dev, B, S
+
+    def embed_scratch(self, B: int, S: int):
+        """A device buffer for embed_backward on B x S tokens (None where it needs none)."""
+        import torch
+        n = C.c_size_t()
+        self._check(self._L.fdh_embed_scratch_bytes(self._h, B, S, C.byref(n)), "fdh_embed_scratch_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device="cuda") if n.value else None
+
+    def embed_forward(self, tokens, table, eps: float = 1.0, positions=None, out=None):
+        """The token embedding of int32 [B, S] tokens at both points: the float32 pair (mean,
+        half difference) of [B S, d_model] rows embed_scale * e[token] (+ p[position]).
+        table = (e, v): [vocab, d_model] of the model's dtype and its float32 direction (or
+        None), taken at e +- eps v; positions = (p, v_p) likewise, [>= S, d_model], for the
+        GPT-2 family.  out: a pair to write, rows of any stride.  A token outside the
+        vocabulary gives a row of NaN.  Enqueued on the model's stream, which must be the
+        current one."""
+        import torch
+        dev, B, S = self._embed_tokens(tokens)
+        T, d, dt, f32 = B * S, self._d, self._qk_dtype, torch.float32
+        e, ve = table
+        pe, pve = self._whole(e, "table", dt, self._vocab * d, dev), 0
+        if ve is not None:
+            pve = self._whole(ve, "the table's direction", f32, self._vocab * d, dev)
+        pp = pvp = 0
+        if positions is not None:
+            p, vp = positions
+            if p.dim() != 2 or p.shape[0] < S:
+                raise ValueError(f"positions must have at least {S} rows")
+            pp = self._whole(p, "positions", dt, p.shape[0] * d, dev)
+            if vp is not None:
+                pvp = self._whole(vp, "the positions' direction", f32, p.shape[0] * d, dev)
+        if out is None:
+            out = tuple(torch.empty((T, d), dtype=f32, device=tokens.device) for _ in range(2))
+        xm, xd, ldx = self._row_pair(out, "out", f32, T, d, dev)
+        st = self._L.fdh_embed_forward(self._h, C.byref(EmbedTables(pe, pve, pp, pvp, eps)), tokens.data_ptr(), B, S, xm, xd, ldx)
+        if st < 0:
+            self._check(st, "fdh_embed_forward")
+        return out
+
+    def embed_backward(self, dx, tokens, eps: float = 1.0, out=None, out_positions=None, accumulate: bool = False, scratch=None):
+        """The tables' entries of Hv from dx, the float32 [B S, d_model] half difference of the
+        gradient of embed_forward's rows: float32 [vocab, d_model], for the GPT-2 family a
+        tuple with [max_seq, d_model] positions.  With accumulate they are added to out (and
+        out_positions).  scratch: embed_scratch(B, S), made here if None; calls that may
+        overlap on the device need one each."""
+        import torch
+        dev, B, S = self._embed_tokens(tokens)
+        d, f32 = self._d, torch.float32
+        pd, ldd = self._rows(dx, "dx", f32, B * S, d, dev)
+        gpt2 = self.family == "gpt2"
+        if accumulate and (out is None or (gpt2 and out_positions is None)):
+            raise ValueError("accumulate needs out (and out_positions)")
+        if out is None:
+            out = torch.empty((self._vocab, d), dtype=f32, device=tokens.device)
+        if gpt2 and out_positions is None:
+            out_positions = torch.empty((self._max_seq, d), dtype=f32, device=tokens.device)
+        po, pp = self._whole(out, "out", f32, self._vocab * d, dev), 0
+        if out_positions is not None:
+            pp = self._whole(out_positions, "out_positions", f32, self._max_seq * d, dev)
+        if scratch is None:
+            scratch = self.embed_scratch(B, S)
+        ps, ns = self._scratch_arg(scratch, dev)
+        st = self._L.fdh_embed_backward(self._h, tokens.data_ptr(), B, S, pd, ldd, eps, po, pp, int(accumulate), ps, ns)
+        if st < 0:
+            self._check(st, "fdh_embed_backward")
+        return (out, out_positions) if gpt2 else out
 
     def hvp_bound(self, v, out=None):
         """H v of the bound operator (float32 [P]); enqueued on the context stream."""

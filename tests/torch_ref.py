@@ -62,7 +62,7 @@ def _rope(x, base):
     return torch.cat([x1 * c - x2 * s, x2 * c + x1 * s], -1)
 
 
-def loss(cfg, flat, tokens, labels=None):
+def loss(cfg, flat, tokens, labels=None, embed_scale=1.0):
     W = _params(cfg, flat)
     tok = torch.as_tensor(tokens, dtype=torch.long)
     B, S = tok.shape
@@ -70,7 +70,7 @@ def loss(cfg, flat, tokens, labels=None):
     dh = d // H
     eps = 1e-5
     gpt2 = cfg["family"] == "gpt2"
-    x = W["wte"][tok] + W["wpe"][:S] if gpt2 else W["emb"][tok]
+    x = embed_scale * W["wte"][tok] + W["wpe"][:S] if gpt2 else embed_scale * W["emb"][tok]
     mask = torch.ones(S, S, dtype=torch.bool).triu(1)
     for l in range(cfg["n_layers"]):
         a = _ln(x, W[f"{l}.g1"], W[f"{l}.b1"], eps) if gpt2 else _rms(x, W[f"{l}.g1"], eps)
@@ -113,9 +113,9 @@ def loss(cfg, flat, tokens, labels=None):
         logits[:, :-1].reshape(-1, cfg["vocab"]), tgt[:, 1:].reshape(-1), ignore_index=-100)
 
 
-def grad(cfg, theta, tokens, labels=None):
+def grad(cfg, theta, tokens, labels=None, embed_scale=1.0):
     t = torch.tensor(theta, dtype=torch.float64, requires_grad=True)
-    (g,) = torch.autograd.grad(loss(cfg, t, tokens, labels), t)
+    (g,) = torch.autograd.grad(loss(cfg, t, tokens, labels, embed_scale), t)
     return g.numpy()
 
 
