@@ -151,6 +151,29 @@ typedef struct fdh_embed_tables {
   double eps;               /* the points are e + eps v_e and e - eps v_e; positive, finite */
 } fdh_embed_tables;
 
+/* Inputs of the loss over the vocabulary (device pointers): logits x w^T at the points
+ * x_m +- x_d and w_m +- w_d, one target per row. */
+typedef struct fdh_head_inputs {
+  const void *x_m, *x_d;    /* [T] rows of d_model elements of the context's dtype, ldx elements apart */
+  int64_t ldx;
+  const void *w_m, *w_d;    /* [vocab][d_model] of the context's dtype (w_d: eps v in that dtype) */
+  const int32_t* targets;   /* [T], -100: the row has none */
+  int32_t T;                /* rows, 0 .. 2^20 */
+  int32_t piece;            /* columns of the vocabulary handled at a time (rounded up to 256); 0: chosen */
+  int32_t reserved;         /* 0 */
+} fdh_head_inputs;
+
+/* Gradients of the loss (device pointers). */
+typedef struct fdh_head_grads {
+  void *dx_m, *dx_d;        /* [T] rows of d_model elements, lddx apart: the gradient of x, a pair */
+  int64_t lddx;
+  void* dw;                 /* [vocab][d_model]: the half difference of the gradient of w over eps (Hv's entries) */
+  double scale;             /* weight of every row's loss, e.g. 1 / targets; finite */
+  double eps;               /* positive, finite */
+  int32_t dtype;            /* of dx and dw: FDH_F32 or the context's dtype */
+  int32_t accumulate;       /* != 0: dw is added to what is there (FDH_F32) */
+} fdh_head_grads;
+
 typedef struct fdh_ctx fdh_ctx;
 
 /* Create a context for one model on the current HIP device; hip_stream is a
@@ -193,6 +216,15 @@ fdh_status fdh_set_workspace(fdh_ctx* ctx, void* dev, size_t bytes, int32_t B, i
  * fdh_set_workspace; the carve in use keeps its mode until then.  Off by
  * default; no effect for QUAD_DIAG. */
 fdh_status fdh_set_recompute(fdh_ctx* ctx, int32_t on);
+
+/* The head of the HVP in pieces of the vocabulary: with columns > 0 the logits are formed
+ * `columns` (rounded up to 256) at a time by the kernels of fdh_head_grad and never kept, so the
+ * workspace holds 12 bytes (bf16) or 8 (fp32) per token and column of one piece in place of 12 or
+ * 16 per token and word of the vocabulary; the logits are formed twice (3 more products of the
+ * head's size, where it has 8).  0 keeps whole logits (the default).  Results agree to the rounding
+ * of the context's dtype.  Takes effect for the following fdh_workspace_bytes / fdh_set_workspace;
+ * the carve in use keeps its mode until then. */
+fdh_status fdh_set_vocab_piece(fdh_ctx* ctx, int32_t columns);
 
 /* Synthetic inputs (the SplitMix64 counter generator of Steele, Lea and Flood,
  * OOPSLA 2014, in counter form): theta with N(0, 0.02) matrices, unit gains, zero biases (bf16 by
@@ -321,6 +353,32 @@ fdh_status fdh_embed_forward(fdh_ctx* ctx, const fdh_embed_tables* tables, const
 fdh_status fdh_embed_backward(fdh_ctx* ctx, const int32_t* tokens_dev, int32_t B, int32_t S, const float* dx_d, int64_t lddx,
                               double eps, float* hv_e, float* hv_p, int32_t accumulate, void* scratch, size_t scratch_bytes);
 fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes);
+
+/* The softmax cross-entropy of x w^T against the rows' targets on caller-owned device
+ * memory, a piece of the vocabulary at a time: the logits are formed piece by piece and
+ * never kept (language-model families, d_model <= 2^16).
+ *   loss[t] = log sum_j e^(l_tj) - l_ty as a float32 pair: _m the mean, _d the half difference of
+ *   its values at the two points, not scaled; 0 for a row without a target.
+ * fdh_head_grad also gives the gradients of scale * sum_t loss[t] (the loss pointers may be
+ * NULL).  It forms the logits twice (once where one piece holds the vocabulary) and rounds
+ * their gradient to the context's dtype, as the HVP's products do; sums and statistics are
+ * fp32 or wider, the order of the additions is fixed (the same bits in every call).  The
+ * logits' mean leaves out x_d w_d^T, of second order in the step, as the HVP does.
+ * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude.
+ * Rows without a target may hold anything (NaN among it): their dx is 0 and they take no
+ * part in dw.  A target outside [0, vocab) other than -100, or a NaN in its row, makes the row's
+ * loss and gradient, and with it dw, NaN.  Pointers 16-byte aligned (targets and losses
+ * 4-byte), row strides in multiples of 16 bytes, ldx <= 2^20.  scratch: device memory, 256-byte
+ * aligned, of at least fdh_head_scratch_bytes for the same T and piece, in use until the
+ * call's work is done: calls that may overlap on the device need scratch of their own.  No
+ * output overlaps an input, the scratch or another output.  T = 0 does nothing, but fdh_head_grad
+ * sets dw to zero unless it accumulates.  Only enqueued on the context stream (no wait, no
+ * allocation: may be captured in a graph); a single token is the call with T = 1. */
+fdh_status fdh_head_loss(fdh_ctx* ctx, const fdh_head_inputs* in, float* loss_m, float* loss_d, void* scratch, size_t scratch_bytes);
+fdh_status fdh_head_grad(fdh_ctx* ctx, const fdh_head_inputs* in, float* loss_m, float* loss_d, const fdh_head_grads* grads,
+                         void* scratch, size_t scratch_bytes);
+/* grads != 0: for fdh_head_grad (any dtype and eps); 0: for fdh_head_loss */
+fdh_status fdh_head_scratch_bytes(const fdh_ctx* ctx, int32_t T, int32_t piece, int32_t grads, size_t* bytes);
 
 /* hv = H v of the bound operator (fdh_bind or fdh_bind_dataset): one FD-HVP
  * per batch, accumulated into hv in batch order; fdh_last_losses then returns

@@ -163,6 +163,16 @@ fdh_status fdh_set_recompute(fdh_ctx* ctx, int32_t on) {
   });
 }
 
+fdh_status fdh_set_vocab_piece(fdh_ctx* ctx, int32_t columns) {
+  return run(ctx, [&](fdh::Engine& e) -> int {
+    if (e.quad) { e.err = "needs a language-model context"; return FDH_ERR_UNSUPPORTED; }
+    if (columns < 0) { e.err = "columns must not be negative"; return FDH_ERR_INVALID_ARG; }
+    if (columns > 0 && e.d > fdh::HEAD_MAX_WIDTH) { e.err = "d_model must be <= 2^16"; return FDH_ERR_UNSUPPORTED; }
+    e.vocab_piece = columns;
+    return FDH_OK;
+  });
+}
+
 fdh_status fdh_init_params(fdh_ctx* ctx, void* params_dev, uint64_t seed) {
   return run(ctx, [&](fdh::Engine& e) { return e.init_params(params_dev, seed); });
 }
@@ -276,6 +286,27 @@ fdh_status fdh_embed_backward(fdh_ctx* ctx, const int32_t* tokens_dev, int32_t B
   return run(ctx, [&](fdh::Engine& e) {
     return e.embed_backward(tokens_dev, B, S, dx_d, lddx, eps, hv_e, hv_p, accumulate != 0, scratch, scratch_bytes);
   });
+}
+
+fdh_status fdh_head_scratch_bytes(const fdh_ctx* ctx, int32_t T, int32_t piece, int32_t grads, size_t* bytes) {
+  if (!ctx || !ctx->eng || !bytes || T < 0 || piece < 0) return FDH_ERR_INVALID_ARG;
+  const fdh::Engine& e = *ctx->eng;
+  if (e.quad || T > fdh::HEAD_MAX_ROWS || e.d > fdh::HEAD_MAX_WIDTH) return FDH_ERR_UNSUPPORTED;
+  try {
+    *bytes = e.head_carve(T, piece, grads != 0).total;
+  } catch (...) {
+    return FDH_ERR_INVALID_ARG;
+  }
+  return FDH_OK;
+}
+
+fdh_status fdh_head_loss(fdh_ctx* ctx, const fdh_head_inputs* in, float* loss_m, float* loss_d, void* scratch, size_t scratch_bytes) {
+  return run(ctx, [&](fdh::Engine& e) { return e.head_loss(in, loss_m, loss_d, scratch, scratch_bytes); });
+}
+
+fdh_status fdh_head_grad(fdh_ctx* ctx, const fdh_head_inputs* in, float* loss_m, float* loss_d, const fdh_head_grads* grads,
+                         void* scratch, size_t scratch_bytes) {
+  return run(ctx, [&](fdh::Engine& e) { return e.head_grad(in, loss_m, loss_d, grads, scratch, scratch_bytes); });
 }
 
 fdh_status fdh_set_basis_offload(fdh_ctx* ctx, int32_t device_rows, void* host_rows, size_t host_bytes) {

@@ -1,5 +1,5 @@
 // The two ends of a model on caller-owned memory: argument checks and dispatch of
-// fdh_embed_* (include/fdhvp.h).
+// fdh_embed_* and fdh_head_* (include/fdhvp.h), and the loop over the vocabulary's pieces.
 #include <algorithm>
 #include <cmath>
 
@@ -84,6 +84,301 @@ int Engine::embed_backward(const int32_t* tok, int B, int S, const float* dx_d, 
   CK(launch_embed_bwd(hv_e, tok, dx_d, lddx, T_, d, V, embed_scale / eps, acc, scratch, stream));
   if (gpt2) CK(launch_pos_bwd(hv_p, dx_d, lddx, B, S, d, 1.0 / eps, Smax, acc, stream));
   return FDH_OK;
+}
+
+// ---------------------------------------------------------------------------
+// loss over the vocabulary in pieces
+// ---------------------------------------------------------------------------
+namespace {
+
+// elements of one channel of a piece's logits that are aimed at
+constexpr int64_t HEAD_PIECE_ELEMS = (int64_t)64 << 20;
+constexpr int HEAD_PIECE_ROUND = 256, HEAD_PIECE_MIN = 1024;
+// scratch that the plan of a split contraction may take
+constexpr size_t HEAD_SPLIT = (size_t)512 << 20;
+
+GemmOperand kmaj(const void* p, int64_t ld) {
+  GemmOperand o;
+  o.ptr = p;
+  o.s_row = ld;
+  o.s_k = 1;
+  return o;
+}
+GemmOperand mnmaj(const void* p, int64_t ld) {
+  GemmOperand o;
+  o.ptr = p;
+  o.s_row = 1;
+  o.s_k = ld;
+  return o;
+}
+
+// the products of a piece of C columns: shapes for the plans of split contractions
+template <typename T>
+size_t piece_split(int T_, int Tp, int C, int d, bool grads) {
+  GemmArgs g[2];
+  auto need = [&](int M, int N, int K, int n) {
+    for (int p = 0; p < 2; ++p) {
+      g[p].M = M;
+      g[p].N = N;
+      g[p].K = K;
+      g[p].ldc = N;
+      g[p].npairs = 2 - p;
+    }
+    return gemm_scratch<T>(g, n, HEAD_SPLIT);
+  };
+  size_t mx = need(T_, C, d, 2);
+  if (grads) mx = std::max(mx, std::max(need(T_, d, C, 2), need(C, d, Tp, 1)));
+  return mx;
+}
+
+}  // namespace
+
+HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
+  HeadCarve c;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) / 256 * 256;
+    return o;
+  };
+  const size_t ob = bf16 ? 2 : 4, t = (size_t)T_;
+  c.Tp = (int)((t + 7) / 8 * 8);
+  int64_t C = piece > 0 ? piece : std::max<int64_t>(HEAD_PIECE_MIN, HEAD_PIECE_ELEMS / std::max(1, T_) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND);
+  C = (C + HEAD_PIECE_ROUND - 1) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND;
+  c.C = (int)std::min<int64_t>(C, V);
+  const size_t tp = (size_t)c.Tp, pc = tp * c.C, td = tp * d;
+  c.top = take(t * 4);
+  c.z = take(4 * t * 8);
+  c.ym = take(2 * t * 4);
+  c.f = take(4 * t * 8);
+  c.lm = take(pc * 4);
+  c.ld = take(pc * 4);
+  // (fp32 models: the gradient takes the place of the logits)
+  c.gm = grads && bf16 ? take(pc * ob) : c.lm;
+  c.gd = grads && bf16 ? take(pc * ob) : c.ld;
+  c.xm = take(grads ? td * ob : 0);
+  c.xd = take(grads ? td * ob : 0);
+  c.dm = take(grads && bf16 ? t * d * 4 : 0);
+  c.dd = take(grads && bf16 ? t * d * 4 : 0);
+  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, grads) : piece_split<float>(T_, c.Tp, c.C, d, grads);
+  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, grads) : piece_split<float>(T_, c.Tp, V % c.C, d, grads));
+  c.split_bytes = sp;
+  c.split = take(sp);
+  c.total = T_ > 0 ? at : 0;
+  return c;
+}
+
+// The products of a smaller batch may be cut into more parts: the split contractions' scratch is
+// the most that any number of rows takes (products over the rows have one plan for all of as many
+// 128-row tiles, those along them for all of as many slices of 32).  It lies behind the rest.
+size_t Engine::head_scratch_most(size_t tokens, int piece) const {
+  const int T_ = (int)std::min<size_t>(tokens, 16384);   // of one batch
+  if (T_ == 0) return 0;
+  std::lock_guard<std::mutex> lk(linear_mu);
+  if (T_ == most_tokens && piece == most_piece) return most_bytes;
+  const HeadCarve c = head_carve(T_, piece, true);
+  size_t mx = c.split_bytes;
+  for (int C : {c.C, V % c.C}) {
+    if (!C) continue;
+    for (int t = (T_ + 31) / 32 * 32; t > 0; t -= 32)
+      mx = std::max(mx, bf16 ? piece_split<bf16_t>(t, t, C, d, true) : piece_split<float>(t, t, C, d, true));
+  }
+  most_tokens = T_;
+  most_piece = piece;
+  most_bytes = c.total - (c.split_bytes + 255) / 256 * 256 + (mx + 255) / 256 * 256;
+  return most_bytes;
+}
+
+template <typename T>
+int Engine::head_run(const HeadCall& c) {
+  const HeadCarve k = head_carve(c.T, c.piece, c.grads);
+  hipStream_t st = stream;
+  char* ws = c.scratch;
+  const int T_ = c.T;
+  const int64_t t = T_;
+  HeadRows r;
+  r.top = (float*)(ws + k.top);
+  r.ym = (float*)(ws + k.ym);
+  r.yd = r.ym + t;
+  for (int q = 0; q < 4; ++q) {
+    r.z[q] = (double*)(ws + k.z) + q * t;
+    r.f[q] = (double*)(ws + k.f) + q * t;
+  }
+  float *lm = (float*)(ws + k.lm), *ld = (float*)(ws + k.ld);
+  const PairT<T> g{(T*)(ws + k.gm), (T*)(ws + k.gd)};
+  const T *wm = (const T*)c.w_m, *wd = (const T*)c.w_d;
+  const T *xm = (const T*)c.x_m, *xd = (const T*)c.x_d;
+  int64_t ldx = c.ldx;
+  auto product = [&](GemmArgs* a, int n) -> int {
+    for (int p = 0; p < n; ++p)
+      if (const char* msg = gemm_check<T>(a[p])) { err = msg; return FDH_ERR_UNSUPPORTED; }
+    const GemmScratch sc{(float*)(ws + k.split), HEAD_SPLIT, k.split_bytes};
+    int e0 = 0;
+    if (timing.on) CK(timing.begin(st, &e0));
+    CK(gemm<T>(a, n, sc, st));
+    if (timing.on) CK(timing.end(st, 0, e0, gemm_flops(a[0]) + (n > 1 ? gemm_flops(a[1]) : 0.0), 0.0));
+    return FDH_OK;
+  };
+  // logits of columns n0 .. n0 + C - 1 (the product of the two half differences, of second order in
+  // the step, is left out, as in every linear layer)
+  auto logits = [&](int n0, int C) -> int {
+    GemmArgs a[2];
+    for (GemmArgs& x : a) {
+      x.M = T_; x.N = C; x.K = d;
+      x.ldc = C;
+    }
+    a[0].npairs = 2;
+    a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(wm + (int64_t)n0 * d, d);
+    a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(wd + (int64_t)n0 * d, d);
+    a[0].C = ld;
+    a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(wm + (int64_t)n0 * d, d);
+    a[1].C = lm;
+    return product(a, 2);
+  };
+  if (c.grads && (c.copy_x || T_ != k.Tp)) {
+    const PairT<T> o{(T*)(ws + k.xm), (T*)(ws + k.xd)};
+    CK(launch_head_copy<T>(o, xm, xd, ldx, T_, k.Tp, d, c.tgt, st));
+    xm = o.m;
+    xd = o.d;
+    ldx = d;
+  }
+  for (int n0 = 0; n0 < V; n0 += k.C) {
+    const int C = std::min(k.C, V - n0);
+    const int rc = logits(n0, C);
+    if (rc != FDH_OK) return rc;
+    CK(launch_head_stats<T>(r, lm, ld, T_, C, n0, c.tgt, n0 == 0, st));
+  }
+  CK(launch_head_rows(r, c.tgt, T_, V, c.scale, c.loss_m, c.loss_d, c.rowloss, st));
+  if (!c.grads) return FDH_OK;
+  // the gradient of x is added up over the pieces in fp32
+  const bool round = !c.out_f32 && k.C < V;
+  const bool op_out = !c.out_f32 && !round;
+  void* dxm = round ? (void*)(ws + k.dm) : c.dx_m;
+  void* dxd = round ? (void*)(ws + k.dd) : c.dx_d;
+  const int64_t lddx = round ? d : c.lddx;
+  const size_t ob = c.out_f32 ? 4 : sizeof(T);
+  for (int n0 = 0; n0 < V; n0 += k.C) {
+    const int C = std::min(k.C, V - n0);
+    int rc = k.C < V ? logits(n0, C) : FDH_OK;
+    if (rc != FDH_OK) return rc;
+    CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, c.scale, st));
+    GemmArgs a[2];
+    for (GemmArgs& x : a) {
+      x.M = T_; x.N = d; x.K = C;
+      x.ldc = lddx;
+      x.out_type = op_out ? OUT_OP : OUT_F32;
+      x.beta = n0 > 0 ? 1.f : 0.f;
+    }
+    a[0].npairs = 2;
+    a[0].A[0] = kmaj(g.d, C); a[0].B[0] = mnmaj(wm + (int64_t)n0 * d, d);
+    a[0].A[1] = kmaj(g.m, C); a[0].B[1] = mnmaj(wd + (int64_t)n0 * d, d);
+    a[0].C = dxd;
+    a[1].A[0] = kmaj(g.m, C); a[1].B[0] = mnmaj(wm + (int64_t)n0 * d, d);
+    a[1].C = dxm;
+    rc = product(a, 2);
+    if (rc != FDH_OK) return rc;
+    GemmArgs w;
+    w.M = C; w.N = d; w.K = k.Tp; w.npairs = 2;
+    w.A[0] = mnmaj(g.m, C); w.B[0] = mnmaj(xd, ldx);
+    w.A[1] = mnmaj(g.d, C); w.B[1] = mnmaj(xm, ldx);
+    w.C = (char*)c.dw + (size_t)n0 * d * ob;
+    w.ldc = d;
+    w.out_type = c.out_f32 ? OUT_F32 : OUT_OP;
+    w.alpha = c.inv_eps;
+    w.beta = c.acc ? 1.f : 0.f;
+    rc = product(&w, 1);
+    if (rc != FDH_OK) return rc;
+  }
+  if (round) {
+    const PairT<bf16_t> o{(bf16_t*)c.dx_m, (bf16_t*)c.dx_d};
+    CK(launch_head_round(o, c.lddx, (const float*)dxm, (const float*)dxd, T_, d, st));
+  }
+  return FDH_OK;
+}
+template int Engine::head_run<float>(const HeadCall&);
+template int Engine::head_run<bf16_t>(const HeadCall&);
+
+int Engine::head_check(const fdh_head_inputs* in, bool grads, size_t scratch_bytes, const void* scratch, HeadCall* c) {
+  if (quad) { err = "needs a language-model context"; return FDH_ERR_UNSUPPORTED; }
+  if (!in) { err = "null inputs"; return FDH_ERR_INVALID_ARG; }
+  if (in->T < 0 || in->piece < 0 || in->reserved != 0) { err = "T and piece must not be negative, reserved 0"; return FDH_ERR_INVALID_ARG; }
+  if (in->T > HEAD_MAX_ROWS || d > HEAD_MAX_WIDTH) { err = "T must be <= 2^20 and d_model <= 2^16"; return FDH_ERR_UNSUPPORTED; }
+  const int ob = bf16 ? 2 : 4;
+  if (in->T > 0) {
+    if (bad_rows(in->x_m, in->ldx, d, ob) || bad_rows(in->x_d, in->ldx, d, ob) || in->ldx > HEAD_MAX_LD) {
+      err = "x: 16-byte aligned rows, d_model to 2^20 elements apart";
+      return FDH_ERR_INVALID_ARG;
+    }
+    if (bad_rows(in->w_m, d, d, ob) || bad_rows(in->w_d, d, d, ob)) { err = "w: null or not 16-byte aligned"; return FDH_ERR_INVALID_ARG; }
+    if (!in->targets || (uintptr_t)in->targets % 4) { err = "targets: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
+    const size_t need = head_carve(in->T, in->piece, grads).total;
+    if (!scratch || scratch_bytes < need) { err = "scratch smaller than fdh_head_scratch_bytes"; return FDH_ERR_WORKSPACE; }
+    if ((uintptr_t)scratch % 256) { err = "scratch must be 256-byte aligned"; return FDH_ERR_WORKSPACE; }
+  }
+  c->x_m = in->x_m; c->x_d = in->x_d; c->ldx = in->ldx;
+  c->w_m = in->w_m; c->w_d = in->w_d;
+  c->tgt = in->targets;
+  c->T = in->T; c->piece = in->piece;
+  c->scratch = (char*)scratch;
+  return FDH_OK;
+}
+
+int Engine::head_loss(const fdh_head_inputs* in, float* loss_m, float* loss_d, void* scratch, size_t scratch_bytes) {
+  HeadCall c;
+  const int rc = head_check(in, false, scratch_bytes, scratch, &c);
+  if (rc != FDH_OK) return rc;
+  if (c.T == 0) return FDH_OK;
+  if (!loss_m || !loss_d || (uintptr_t)loss_m % 4 || (uintptr_t)loss_d % 4) { err = "loss: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
+  const int64_t ob = bf16 ? 2 : 4, T_ = c.T, wd = (int64_t)d * ob;
+  const Region o[3] = {flat(loss_m, 4 * T_), flat(loss_d, 4 * T_), flat(scratch, (int64_t)head_carve(c.T, c.piece, false).total)};
+  const Region r[5] = {{(const char*)c.x_m, T_, c.ldx * ob, wd}, {(const char*)c.x_d, T_, c.ldx * ob, wd}, flat(c.w_m, V * wd),
+                       flat(c.w_d, V * wd), flat(c.tgt, 4 * T_)};
+  if (any_overlap(o, 3, r, 5)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }
+  c.loss_m = loss_m; c.loss_d = loss_d;
+  return bf16 ? head_run<bf16_t>(c) : head_run<float>(c);
+}
+
+int Engine::head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, const fdh_head_grads* g, void* scratch,
+                      size_t scratch_bytes) {
+  HeadCall c;
+  const int rc = head_check(in, true, scratch_bytes, scratch, &c);
+  if (rc != FDH_OK) return rc;
+  if (!g) { err = "null gradients"; return FDH_ERR_INVALID_ARG; }
+  if ((loss_m == nullptr) != (loss_d == nullptr) || (uintptr_t)loss_m % 4 || (uintptr_t)loss_d % 4) {
+    err = "loss: both or neither, 4-byte aligned";
+    return FDH_ERR_INVALID_ARG;
+  }
+  if (!(g->eps > 0.0) || !std::isfinite(g->eps) || !std::isfinite(g->scale)) {
+    err = "eps must be positive and finite, scale finite";
+    return FDH_ERR_INVALID_ARG;
+  }
+  if (g->dtype != FDH_F32 && g->dtype != cfg.dtype) { err = "gradients are float32 or of the context's dtype"; return FDH_ERR_INVALID_ARG; }
+  if (g->accumulate && g->dtype != FDH_F32) { err = "accumulate needs float32 gradients"; return FDH_ERR_INVALID_ARG; }
+  const int64_t ob = bf16 ? 2 : 4, T_ = c.T, wd = (int64_t)d * ob, gb = g->dtype == FDH_F32 ? 4 : 2, gw = (int64_t)d * gb;
+  if (!g->dw || (uintptr_t)g->dw % 16) { err = "dw: null or not 16-byte aligned"; return FDH_ERR_INVALID_ARG; }
+  if (T_ > 0 && (bad_rows(g->dx_m, g->lddx, d, (int)gb) || bad_rows(g->dx_d, g->lddx, d, (int)gb))) {
+    err = "dx: 16-byte aligned rows, at least d_model elements apart";
+    return FDH_ERR_INVALID_ARG;
+  }
+  if (T_ == 0) {
+    if (!g->accumulate) CK(launch_fill_f32((float*)g->dw, V * gw / 4, 0.f, stream));
+    return FDH_OK;
+  }
+  const Region o[6] = {flat(loss_m, 4 * T_), flat(loss_d, 4 * T_), {(const char*)g->dx_m, T_, g->lddx * gb, gw},
+                       {(const char*)g->dx_d, T_, g->lddx * gb, gw}, flat(g->dw, V * gw),
+                       flat(scratch, (int64_t)head_carve(c.T, c.piece, true).total)};
+  const Region r[5] = {{(const char*)c.x_m, T_, c.ldx * ob, wd}, {(const char*)c.x_d, T_, c.ldx * ob, wd}, flat(c.w_m, V * wd),
+                       flat(c.w_d, V * wd), flat(c.tgt, 4 * T_)};
+  if (any_overlap(o, 6, r, 5)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }
+  c.loss_m = loss_m; c.loss_d = loss_d;
+  c.grads = true;
+  c.scale = g->scale;
+  c.inv_eps = (float)(1.0 / g->eps);
+  c.dx_m = g->dx_m; c.dx_d = g->dx_d; c.lddx = g->lddx;
+  c.dw = g->dw;
+  c.out_f32 = g->dtype == FDH_F32;
+  c.acc = g->accumulate != 0;
+  return bf16 ? head_run<bf16_t>(c) : head_run<float>(c);
 }
 
 }  // namespace fdh

@@ -76,6 +76,7 @@ struct WsLayout {
   Span dqkv_m, dqkv_d, dqkvo_m, dqkvo_d, gqa_m, gqa_d, dl, da_m, da_d, emb, rope, cdf, gpartial, bpart, bout;
   Span tcount;  // two int64 counters of fdh_bind_dataset
   Span nfflag;  // non-finite flags of the input direction and the product (two int32)
+  Span tgt, head_ws;   // targets and scratch of the head in pieces
   Span wsplit;  // split-K partial products of the weight-gradient GEMMs
   Span lz_w, lz_q, lz_qp, lz_basis, lz_alpha, lz_beta, lz_coef, lz_gram, lz_partial, lz_flag, lz_maxabs;
   int64_t lz_ldq = 0;   // basis row stride (elements, multiple of 8)
@@ -87,10 +88,37 @@ struct WsLayout {
   // other spans of every layer alias one shared set, which the backward refills
   // by running that layer's forward again (x_in -> z) just before its backward
   bool rc = false;
+  int vp = 0;   // columns of the vocabulary per piece of the head (0: whole logits)
   int planB = 0, planS = 0, planM = 0;
   fdh_lanczos_opts planO{};
   size_t total = 0;     // bytes the carve needs
 };
+
+// The loss over the vocabulary in pieces (ends.hip): one call, and the carve of its scratch.
+struct HeadCall {
+  const void *x_m = nullptr, *x_d = nullptr;   // [T][ldx], operand type
+  int64_t ldx = 0;
+  const void *w_m = nullptr, *w_d = nullptr;   // [V][d], operand type
+  const int32_t* tgt = nullptr;                // [T]
+  int T = 0, piece = 0;                        // columns per piece (0: chosen)
+  float *loss_m = nullptr, *loss_d = nullptr;  // [T] or null
+  double* rowloss = nullptr;                   // scale times the losses at the two points, [2][T], or null
+  double scale = 1.0;
+  bool grads = false;
+  float inv_eps = 1.f;
+  void *dx_m = nullptr, *dx_d = nullptr;       // [T][lddx]
+  int64_t lddx = 0;
+  void* dw = nullptr;                          // [V][d]
+  bool out_f32 = true, acc = false;            // outputs fp32 (acc: added to dw), else the operand type
+  bool copy_x = true;                          // rows without a target may hold anything
+  char* scratch = nullptr;
+};
+struct HeadCarve {
+  int C = 0, Tp = 0;        // columns of a piece; rows of the logits' gradient (multiple of 8)
+  size_t top, z, ym, f, lm, ld, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
+};
+
+double gemm_flops(const GemmArgs& g);   // executed by a product, causal tails clipped
 
 class Engine : public WsLayout {
  public:
@@ -167,6 +195,15 @@ class Engine : public WsLayout {
   int embed_forward(const fdh_embed_tables* w, const int32_t* tok, int B, int S, float* x_m, float* x_d, int64_t ldx);
   int embed_backward(const int32_t* tok, int B, int S, const float* dx_d, int64_t lddx, double eps, float* hv_e, float* hv_p,
                      bool acc, void* scratch, size_t scratch_bytes);
+  // the loss over the vocabulary in pieces (fdh_head_loss, fdh_head_grad; the HVP's head with
+  // vocab_piece > 0)
+  int vocab_piece = 0;   // plan (and run) the head in pieces of so many columns; 0: whole logits
+  HeadCarve head_carve(int T_, int piece, bool grads) const;
+  size_t head_scratch_most(size_t tokens, int piece) const;   // of batches of up to so many tokens, with gradients
+  template <typename T> int head_run(const HeadCall& c);
+  int head_check(const fdh_head_inputs* in, bool grads, size_t scratch_bytes, const void* scratch, HeadCall* c);
+  int head_loss(const fdh_head_inputs* in, float* loss_m, float* loss_d, void* scratch, size_t scratch_bytes);
+  int head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, const fdh_head_grads* g, void* scratch, size_t scratch_bytes);
   std::vector<int64_t> layer_ranges() const;
 
  private:
@@ -174,6 +211,8 @@ class Engine : public WsLayout {
   mutable std::mutex linear_mu;      // linear_scratch(linear_tokens) = linear_bytes
   mutable int linear_tokens = -1;
   mutable size_t linear_bytes = 0;
+  mutable int most_tokens = -1, most_piece = 0;   // (linear_mu) head_scratch_most of these = most_bytes
+  mutable size_t most_bytes = 0;
   int check_batch(const int32_t* tok, int B, int S);
   int finish_checked(const float* hv);
   template <typename T>

@@ -303,8 +303,12 @@ size_t Engine::plan(int B, int S, int m, const fdh_lanczos_opts* o, WsLayout* ou
     take(W.f_m, td * ob); take(W.f_d, td * ob);
     take(W.lo, (size_t)P * ob);
     take(W.sc_m, pp * 4); take(W.sc_d, pp * 4);
-    take(W.log_m, T_ * V * 4); take(W.log_d, T_ * V * 4);
-    take(W.dlog_m, T_ * V * ob); take(W.dlog_d, T_ * V * ob);
+    W.vp = vocab_piece;
+    const size_t tv = W.vp ? 0 : T_ * V;   // (the head in pieces keeps no logits)
+    take(W.log_m, tv * 4); take(W.log_d, tv * 4);
+    take(W.dlog_m, tv * ob); take(W.dlog_d, tv * ob);
+    take(W.tgt, W.vp ? T_ * 4 : 0);
+    take(W.head_ws, W.vp ? head_scratch_most(T_, W.vp) : 0);
     take(W.rowloss, 2 * T_ * 8);
     take(W.losses, 2 * 8);
     take(W.tcount, 3 * 8);
@@ -418,12 +422,13 @@ uint64_t Engine::layout_digest() const {
                         &db_m, &db_d, &gpart, &do_m, &do_d, &dS_m, &dS_d, &dqkv_m, &dqkv_d, &dqkvo_m, &dqkvo_d, &gqa_m,
                         &gqa_d, &dl, &da_m, &da_d, &emb, &rope, &cdf, &gpartial, &bpart, &bout, &tcount,
                         &nfflag, &wsplit, &lz_w, &lz_q, &lz_qp, &lz_basis, &lz_alpha, &lz_beta, &lz_coef, &lz_gram,
-                        &lz_partial, &lz_flag, &lz_maxabs})
+                        &lz_partial, &lz_flag, &lz_maxabs, &tgt, &head_ws})
     sp(*x);
   mix((uint64_t)lz_ldq);
   mix((uint64_t)lz_dev_rows);
   mix(fused ? 1 : 0);
   mix(rc ? 1 : 0);
+  mix((uint64_t)vp);
   mix((uint64_t)planB);
   mix((uint64_t)planS);
   mix((uint64_t)planM);
@@ -483,7 +488,7 @@ Timing::~Timing() {
 }
 
 // executed (tile-exact, tails clipped) FLOPs of one GEMM call
-static double gemm_flops(const GemmArgs& g) {
+double gemm_flops(const GemmArgs& g) {
   const int BMt = 128;
   double f = 0.0;
   for (int m0 = 0; m0 < g.M; m0 += BMt) {
@@ -864,15 +869,37 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
   // final norm + head + cross-entropy
   CK(launch_norm_fwd<T>(PairT<T>{OP(f_m), OP(f_d)}, F32(xL_m), F32(xL_d), T_, d, ln, th + nfg.off, v + nfg.off,
                         ln ? th + nfb.off : nullptr, ln ? v + nfb.off : nullptr, eps, neps, st));
-  RC(lin_fwd(OP(f_m), OP(f_d), d, head, ParamRef{}, F32(log_m), F32(log_d), nullptr, nullptr, V, OUT_F32));
-  CK(launch_ce<T>(PairT<T>{OP(dlog_m), OP(dlog_d)}, (double*)(ws + rowloss.off), F32(log_m), F32(log_d), tok, lab, T_,
-                  S, V, inv_n, st));
+  if (vp) {
+    // a piece of the vocabulary at a time, both gradients with it
+    CK(launch_head_targets((int32_t*)(ws + tgt.off), tok, lab, T_, S, V, st));
+    HeadCall c;
+    c.x_m = OP(f_m); c.x_d = OP(f_d); c.ldx = d;
+    c.w_m = th + head.off; c.w_d = lo + head.off;
+    c.tgt = (const int32_t*)(ws + tgt.off);
+    c.T = T_; c.piece = vp;
+    c.rowloss = (double*)(ws + rowloss.off);
+    c.scale = inv_n;
+    c.grads = true;
+    c.inv_eps = inv_eps;
+    c.dx_m = F32(db_m); c.dx_d = F32(db_d); c.lddx = d;
+    c.dw = hv + head.off;
+    c.acc = acc;
+    c.copy_x = false;   // (no row is masked on its way here)
+    c.scratch = ws + head_ws.off;
+    RC(head_run<T>(c));
+  } else {
+    RC(lin_fwd(OP(f_m), OP(f_d), d, head, ParamRef{}, F32(log_m), F32(log_d), nullptr, nullptr, V, OUT_F32));
+    CK(launch_ce<T>(PairT<T>{OP(dlog_m), OP(dlog_d)}, (double*)(ws + rowloss.off), F32(log_m), F32(log_d), tok, lab, T_,
+                    S, V, inv_n, st));
+  }
   CK(launch_loss_sum((double*)(ws + losses.off), (const double*)(ws + rowloss.off), T_, acc, st));
 
   // ================= backward =================
   // head
-  RC(lin_wgrad(OP(dlog_m), OP(dlog_d), V, OP(f_m), OP(f_d), d, head));
-  RC(lin_dgrad(OP(dlog_m), OP(dlog_d), V, head, d, F32(db_m), F32(db_d), OUT_F32));
+  if (!vp) {
+    RC(lin_wgrad(OP(dlog_m), OP(dlog_d), V, OP(f_m), OP(f_d), d, head));
+    RC(lin_dgrad(OP(dlog_m), OP(dlog_d), V, head, d, F32(db_m), F32(db_d), OUT_F32));
+  }
   float* dxm = F32(dx0_m);
   float* dxd = F32(dx0_d);
   float* dym = F32(dx1_m);

@@ -308,4 +308,31 @@ hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, i
 hipError_t launch_pos_bwd(float* hv_p, const float* dxd, int64_t ld, int B, int S, int dm, double inv_eps, int64_t rows, bool acc,
                           hipStream_t s);
 
+// ---- head.hip: the loss over the vocabulary, a piece of it at a time ------------------
+constexpr int HEAD_MAX_ROWS = 1 << 20, HEAD_MAX_WIDTH = 1 << 16, HEAD_MAX_LD = 1 << 20;
+struct HeadRows {        // per row of the batch: reference, four sums, target logits, gradient factors
+  float* top;
+  double* z[4];
+  float *ym, *yd;
+  double* f[4];
+};
+// targets of the rows of a [B, S] batch (IGNORE_LABEL: none)
+hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* lab, int T_, int S, int V, hipStream_t s);
+// joins the logits [T][C] of columns n0 .. n0 + C - 1 to the rows' statistics (first: there are none)
+template <typename T>
+hipError_t launch_head_stats(const HeadRows& r, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt, bool first,
+                             hipStream_t s);
+// losses (float32 pair, or null) and scale times the losses at the two points (fp64 [2][T], or
+// null) from the statistics of all columns, and the factors of the gradients
+hipError_t launch_head_rows(const HeadRows& r, const int32_t* tgt, int T_, int V, double scale, float* loss_m, float* loss_d,
+                            double* rowloss, hipStream_t s);
+// o [Tp][C] = scale times the gradient of the losses with respect to these logits (o may be they)
+template <typename T>
+hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
+                               const int32_t* tgt, double scale, hipStream_t s);
+// o [Tp][dm] = the rows of x that have a target, zeros elsewhere
+template <typename T>
+hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
+hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const float* d, int T_, int dm, hipStream_t s);
+
 }  // namespace fdh

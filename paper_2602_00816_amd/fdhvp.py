@@ -54,6 +54,16 @@ class EmbedTables(C.Structure):
     _fields_ = [("e", C.c_void_p), ("v_e", C.c_void_p), ("p", C.c_void_p), ("v_p", C.c_void_p), ("eps", C.c_double)]
 
 
+class HeadInputs(C.Structure):
+    _fields_ = [("x_m", C.c_void_p), ("x_d", C.c_void_p), ("ldx", C.c_int64), ("w_m", C.c_void_p), ("w_d", C.c_void_p),
+                ("targets", C.c_void_p), ("T", C.c_int32), ("piece", C.c_int32), ("reserved", C.c_int32)]
+
+
+class HeadGrads(C.Structure):
+    _fields_ = [("dx_m", C.c_void_p), ("dx_d", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("scale", C.c_double),
+                ("eps", C.c_double), ("dtype", C.c_int32), ("accumulate", C.c_int32)]
+
+
 class LanczosOpts(C.Structure):
     _fields_ = [("reorth", C.c_int32), ("window", C.c_int32), ("basis_dtype", C.c_int32),
                 ("breakdown_tol", C.c_float)]
@@ -92,6 +102,7 @@ def lib():
         "fdh_workspace_bytes": (i32, [vp, i32, i32, i32, C.POINTER(LanczosOpts), C.POINTER(C.c_size_t)]),
         "fdh_set_workspace": (i32, [vp, vp, C.c_size_t, i32, i32, i32, C.POINTER(LanczosOpts)]),
         "fdh_set_recompute": (i32, [vp, i32]),
+        "fdh_set_vocab_piece": (i32, [vp, i32]),
         "fdh_init_params": (i32, [vp, vp, u64]),
         "fdh_make_tokens": (i32, [vp, vp, i32, i32, u64, i32]),
         "fdh_random_vector": (i32, [vp, vp, u64, i32]),
@@ -109,6 +120,9 @@ def lib():
         "fdh_embed_scratch_bytes": (i32, [vp, i32, i32, C.POINTER(C.c_size_t)]),
         "fdh_embed_forward": (i32, [vp, C.POINTER(EmbedTables), vp, i32, i32, vp, vp, i64]),
         "fdh_embed_backward": (i32, [vp, vp, i32, i32, vp, i64, f64, vp, vp, i32, vp, C.c_size_t]),
+        "fdh_head_scratch_bytes": (i32, [vp, i32, i32, i32, C.POINTER(C.c_size_t)]),
+        "fdh_head_loss": (i32, [vp, C.POINTER(HeadInputs), vp, vp, vp, C.c_size_t]),
+        "fdh_head_grad": (i32, [vp, C.POINTER(HeadInputs), vp, vp, C.POINTER(HeadGrads), vp, C.c_size_t]),
         "fdh_hvp_bound": (i32, [vp, vp, vp]),
         "fdh_set_basis_offload": (i32, [vp, i32, vp, C.c_size_t]),
         "fdh_lanczos": (i32, [vp, i32, u64, C.POINTER(LanczosOpts), pd, pd, pi]),
@@ -301,6 +315,11 @@ class Model:
         set_workspace: keep only each layer's input pair and rerun the layer's
         forward before its backward (same results, less memory)."""
         self._check(self._L.fdh_set_recompute(self._h, 1 if on else 0), "fdh_set_recompute")
+
+    def set_vocab_piece(self, columns: int):
+        """Run the HVP's head `columns` of the vocabulary at a time from the next workspace_bytes /
+        set_workspace on, without logits that stay (0: whole logits)."""
+        self._check(self._L.fdh_set_vocab_piece(self._h, int(columns)), "fdh_set_vocab_piece")
 
     def set_embed_scale(self, scale: float):
         """Factor of the token embedding in every following call (1 by default)."""
@@ -666,6 +685,80 @@ class Model:
         if st < 0:
             self._check(st, "fdh_embed_backward")
         return (out, out_positions) if gpt2 else out
+
+    def head_scratch(self, T: int, piece: int = 0, grads: bool = True):
+        """A device buffer for head_grad (or, without grads, head_loss) on T rows (None where
+        it needs none)."""
+        import torch
+        n = C.c_size_t()
+        self._check(self._L.fdh_head_scratch_bytes(self._h, T, piece, int(grads), C.byref(n)), "fdh_head_scratch_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device="cuda") if n.value else None
+
+    def _head_inputs(self, x, w, targets, piece):
+        import torch
+        dev = self._call_device(targets)
+        T, d, dt = targets.numel(), self._d, self._qk_dtype
+        xm, xd, ldx = self._row_pair(x, "x", dt, T, d, dev)
+        wm, wd = (self._whole(t, "w", dt, self._vocab * d, dev) for t in w)
+        tg = self._whole(targets, "targets", torch.int32, T, dev)
+        return dev, T, HeadInputs(xm, xd, ldx, wm, wd, tg, T, piece, 0)
+
+    def _head_loss_out(self, loss, T, dev):
+        import torch
+        return tuple(self._whole(t, "loss", torch.float32, T, dev) for t in loss)
+
+    def head_loss(self, x, w, targets, piece: int = 0, out=None, scratch=None):
+        """Softmax cross-entropy of every row of the pair x ([T, d_model] of the model's dtype, rows
+        of any stride) times the pair w ([vocab, d_model]; (theta, eps v) in the model's dtype)
+        against targets (int32 [T], -100: none): the float32 pair [T] of its mean and half
+        difference over the two points.  The logits are formed `piece` columns of the vocabulary at a
+        time (0: chosen) and not kept.  scratch: head_scratch(T, piece, grads=False), made here if
+        None.  Enqueued on the model's stream, which must be the current one."""
+        import torch
+        dev, T, inp = self._head_inputs(x, w, targets, piece)
+        if out is None:
+            out = tuple(torch.empty(T, device=targets.device) for _ in range(2))
+        lm, ld = self._head_loss_out(out, T, dev)
+        if scratch is None:
+            scratch = self.head_scratch(T, piece, grads=False)
+        ps, ns = self._scratch_arg(scratch, dev)
+        st = self._L.fdh_head_loss(self._h, C.byref(inp), lm, ld, ps, ns)
+        if st < 0:
+            self._check(st, "fdh_head_loss")
+        return out
+
+    def head_grad(self, x, w, targets, scale: float = 1.0, eps: float = 1.0, piece: int = 0, loss=None, dx=None, dw=None,
+                  accumulate: bool = False, scratch=None):
+        """head_loss with the gradients of scale * sum(loss): (loss, dx, dw), dx a pair like x and dw
+        [vocab, d_model] the half difference of w's gradient over eps (its entries of Hv).  dx and
+        dw are of the model's dtype, or float32 where they are given so; with accumulate dw is added
+        to what it holds (float32).  scratch: head_scratch(T, piece)."""
+        import torch
+        dev, T, inp = self._head_inputs(x, w, targets, piece)
+        d, dt, f32 = self._d, self._qk_dtype, torch.float32
+        if accumulate and dw is None:
+            raise ValueError("accumulate needs dw")
+        given = dw if dw is not None else dx[0] if dx is not None else None
+        gt = dt if given is None else given.dtype
+        if gt is not dt and gt is not f32:
+            raise ValueError(f"gradients must have dtype {dt} or {f32}")
+        if loss is None:
+            loss = tuple(torch.empty(T, device=targets.device) for _ in range(2))
+        if dx is None:
+            dx = tuple(torch.empty((T, d), dtype=gt, device=targets.device) for _ in range(2))
+        if dw is None:
+            dw = torch.empty((self._vocab, d), dtype=gt, device=targets.device)
+        lm, ld = self._head_loss_out(loss, T, dev)
+        dm, dd, lddx = self._row_pair(dx, "dx", gt, T, d, dev)
+        pw = self._whole(dw, "dw", gt, self._vocab * d, dev)
+        if scratch is None:
+            scratch = self.head_scratch(T, piece)
+        ps, ns = self._scratch_arg(scratch, dev)
+        g = HeadGrads(dm, dd, lddx, pw, scale, eps, DTYPE["f32"] if gt is f32 else self.cfg.dtype, int(accumulate))
+        st = self._L.fdh_head_grad(self._h, C.byref(inp), lm, ld, C.byref(g), ps, ns)
+        if st < 0:
+            self._check(st, "fdh_head_grad")
+        return loss, dx, dw
 
     def hvp_bound(self, v, out=None):
         """H v of the bound operator (float32 [P]); enqueued on the context stream."""

@@ -3,6 +3,7 @@
     python -m paper_2602_00816_amd.slq --workload llama-1.3b-bf16 [--probes N] [--m M]
                                        [--eps E] [--block-diagonal] [--out FILE.json]
                                        [--qk-norm] [--rope-sections T,H,W] [--rope-interleaved] [--grid H,W]
+                                       [--embed-scale S] [--vocab-piece N]
 
 Runs the SLQ estimate of section 4 with the workload's own settings (probe
 count, Lanczos length, reorthogonalisation mode and window, basis precision,
@@ -25,6 +26,9 @@ A Llama workload can be given a per-head norm of queries and keys (--qk-norm) an
 rotation over several position axes (--rope-sections: rotated pairs per axis, time
 first).  With --grid H,W the tokens of a row stand for frames of H x W patches and
 rotate at their (time, row, column); without it they are text, at 0 .. S - 1 on every axis.
+
+--embed-scale multiplies the token embedding (sqrt(d_model) in some models).  --vocab-piece runs the
+head N columns of the vocabulary at a time: a smaller workspace, the logits formed twice.
 """
 from __future__ import annotations
 
@@ -85,6 +89,8 @@ def main(argv=None):
     ap.add_argument("--rope-sections", type=_numbers(1, 3, 0), help="rotated pairs per position axis (Llama): time, height, width")
     ap.add_argument("--rope-interleaved", action="store_true", help="deal the axes' pairs in turn")
     ap.add_argument("--grid", type=_numbers(2, 2, 1), help="H,W: frames of H x W patches give the positions")
+    ap.add_argument("--embed-scale", type=float, default=1.0, help="factor of the token embedding")
+    ap.add_argument("--vocab-piece", type=int, default=0, help="columns of the vocabulary per piece of the head (0: whole logits)")
     ap.add_argument("--out", default="", help="write the results as JSON")
     args = ap.parse_args(argv)
 
@@ -93,10 +99,15 @@ def main(argv=None):
         ap.error("--qk-norm, --rope-sections, --rope-interleaved and --grid need a Llama workload")
     if (args.grid or args.rope_interleaved) and not args.rope_sections:
         ap.error("--grid and --rope-interleaved need --rope-sections")
+    if not 0.0 < args.embed_scale < float("inf"):
+        ap.error("--embed-scale must be positive and finite")
+    if args.vocab_piece < 0:
+        ap.error("--vocab-piece must not be negative")
     half = w["d_model"] // w["n_heads"] // 2
     if args.rope_sections and sum(args.rope_sections) != half:
         ap.error(f"--rope-sections must add up to {half} pairs")
-    w.update(qk_norm=args.qk_norm, rope_sections=args.rope_sections, rope_interleaved=args.rope_interleaved)
+    w.update(qk_norm=args.qk_norm, rope_sections=args.rope_sections, rope_interleaved=args.rope_interleaved,
+             embed_scale=args.embed_scale)
 
     import torch
     from paper_2602_00816_amd import fdhvp as fd
@@ -112,6 +123,7 @@ def main(argv=None):
     torch.cuda.empty_cache()
     mod = fd.Model.from_workload(w)
     mod.set_recompute(w.get("recompute", False))
+    mod.set_vocab_piece(args.vocab_piece)
     ws = mod.set_workspace(B, S, m, o)
     params = mod.init_params(SEED_PARAMS)
     tok = mod.make_tokens(B, S, SEED_TOKENS, w["token_dist"])
@@ -145,6 +157,7 @@ def main(argv=None):
     out = dict(workload=args.workload, params=mod.num_params, batch=B, seq=S, eps=eps, probes=probes, m=m,
                reorth=w["reorth"], window=w["window"], basis=w["basis"], qk_norm=args.qk_norm,
                rope_sections=args.rope_sections, rope_interleaved=args.rope_interleaved, grid=args.grid,
+               embed_scale=args.embed_scale, vocab_piece=args.vocab_piece,
                seconds=t, lanczos_steps=n_hvp,
                iters_per_min=60.0 * n_hvp / t, trace_estimate=trace, status=st, per_probe=per_probe,
                nodes=[nodes[p, :steps[p]].tolist() for p in range(probes)],
