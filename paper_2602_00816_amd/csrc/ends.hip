@@ -93,6 +93,8 @@ namespace {
 
 // elements of one channel of a piece's logits that are aimed at
 constexpr int64_t HEAD_PIECE_ELEMS = (int64_t)64 << 20;
+// bytes of statistics of column groups that are aimed at where no gradient takes more
+constexpr size_t HEAD_PART = (size_t)64 << 20;
 constexpr int HEAD_PIECE_ROUND = 256, HEAD_PIECE_MIN = 1024;
 // scratch that the plan of a split contraction may take
 constexpr size_t HEAD_SPLIT = (size_t)512 << 20;
@@ -115,6 +117,7 @@ GemmOperand mnmaj(const void* p, int64_t ld) {
 // the products of a piece of C columns: shapes for the plans of split contractions
 template <typename T>
 size_t piece_split(int T_, int Tp, int C, int d, bool grads) {
+  constexpr bool fused = sizeof(T) == 2;   // bf16 models form their logits in a kernel of its own
   GemmArgs g[2];
   auto need = [&](int M, int N, int K, int n) {
     for (int p = 0; p < 2; ++p) {
@@ -126,7 +129,7 @@ size_t piece_split(int T_, int Tp, int C, int d, bool grads) {
     }
     return gemm_scratch<T>(g, n, HEAD_SPLIT);
   };
-  size_t mx = need(T_, C, d, 2);
+  size_t mx = fused ? 0 : need(T_, C, d, 2);
   if (grads) mx = std::max(mx, std::max(need(T_, d, C, 2), need(C, d, Tp, 1)));
   return mx;
 }
@@ -151,11 +154,22 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   c.z = take(4 * t * 8);
   c.ym = take(2 * t * 4);
   c.f = take(4 * t * 8);
-  c.lm = take(pc * 4);
-  c.ld = take(pc * 4);
-  // (fp32 models: the gradient takes the place of the logits)
-  c.gm = grads && bf16 ? take(pc * ob) : c.lm;
-  c.gd = grads && bf16 ? take(pc * ob) : c.ld;
+  // fp32 models: a piece's logits, which their gradient replaces.  bf16 models: the gradient of a
+  // piece, in the first pass the statistics of column groups: of as many columns as fit there,
+  // alone of up to HEAD_PART bytes
+  c.C1 = c.C;
+  size_t part = 0;
+  if (bf16) {
+    const HeadTile tile = head_tile(T_, c.C);
+    const size_t col = std::max<size_t>(1, t * 20 / tile.group), room = std::max<size_t>(grads ? pc * 4 : 0, piece > 0 ? 0 : HEAD_PART);
+    c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, room / col / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
+    part = (size_t)ceil_div(c.C1, tile.group) * 20 * t;
+  }
+  const size_t gb = bf16 ? (grads ? pc * 2 : 0) : pc * 4;
+  c.gm = take(gb);
+  c.gd = take(gb);
+  c.part = c.gm;
+  if (part > at - c.gm) take(part - (at - c.gm));
   c.xm = take(grads ? td * ob : 0);
   c.xd = take(grads ? td * ob : 0);
   c.dm = take(grads && bf16 ? t * d * 4 : 0);
@@ -204,7 +218,6 @@ int Engine::head_run(const HeadCall& c) {
     r.z[q] = (double*)(ws + k.z) + q * t;
     r.f[q] = (double*)(ws + k.f) + q * t;
   }
-  float *lm = (float*)(ws + k.lm), *ld = (float*)(ws + k.ld);
   const PairT<T> g{(T*)(ws + k.gm), (T*)(ws + k.gd)};
   const T *wm = (const T*)c.w_m, *wd = (const T*)c.w_d;
   const T *xm = (const T*)c.x_m, *xd = (const T*)c.x_d;
@@ -220,20 +233,38 @@ int Engine::head_run(const HeadCall& c) {
     return FDH_OK;
   };
   // logits of columns n0 .. n0 + C - 1 (the product of the two half differences, of second order in
-  // the step, is left out, as in every linear layer)
-  auto logits = [&](int n0, int C) -> int {
-    GemmArgs a[2];
-    for (GemmArgs& x : a) {
-      x.M = T_; x.N = C; x.K = d;
-      x.ldc = C;
+  // the step, is left out, as in every linear layer): fp32 models in g, bf16 models statistics or
+  // gradient
+  auto logits = [&](int n0, int C, bool grad) -> int {
+    const T *pm = wm + (int64_t)n0 * d, *pd = wd + (int64_t)n0 * d;
+    if constexpr (sizeof(T) == 2) {
+      HeadLogits h{};
+      h.xm = xm; h.xd = xd; h.ldx = ldx;
+      h.wm = pm; h.wd = pd;
+      h.T = T_; h.Tp = k.Tp; h.C = C; h.d = d; h.n0 = n0;
+      h.tgt = c.tgt;
+      h.part = (float*)(ws + k.part);
+      h.gm = g.m; h.gd = g.d;
+      h.scale = (float)c.scale;
+      int e0 = 0;
+      if (timing.on) CK(timing.begin(st, &e0));
+      CK(launch_head_logits(h, r, grad, st));
+      if (timing.on) CK(timing.end(st, 0, e0, 6.0 * T_ * C * d, 0.0));
+      return FDH_OK;
+    } else {
+      GemmArgs a[2];
+      for (GemmArgs& x : a) {
+        x.M = T_; x.N = C; x.K = d;
+        x.ldc = C;
+      }
+      a[0].npairs = 2;
+      a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(pm, d);
+      a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(pd, d);
+      a[0].C = g.d;
+      a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(pm, d);
+      a[1].C = g.m;
+      return product(a, 2);
     }
-    a[0].npairs = 2;
-    a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(wm + (int64_t)n0 * d, d);
-    a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(wd + (int64_t)n0 * d, d);
-    a[0].C = ld;
-    a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(wm + (int64_t)n0 * d, d);
-    a[1].C = lm;
-    return product(a, 2);
   };
   if (c.grads && (c.copy_x || T_ != k.Tp)) {
     const PairT<T> o{(T*)(ws + k.xm), (T*)(ws + k.xd)};
@@ -242,11 +273,14 @@ int Engine::head_run(const HeadCall& c) {
     xd = o.d;
     ldx = d;
   }
-  for (int n0 = 0; n0 < V; n0 += k.C) {
-    const int C = std::min(k.C, V - n0);
-    const int rc = logits(n0, C);
+  for (int n0 = 0; n0 < V; n0 += k.C1) {
+    const int C = std::min(k.C1, V - n0);
+    const int rc = logits(n0, C, false);
     if (rc != FDH_OK) return rc;
-    CK(launch_head_stats<T>(r, lm, ld, T_, C, n0, c.tgt, n0 == 0, st));
+    if constexpr (sizeof(T) == 2)
+      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, head_tile(T_, C).group), T_, c.tgt, n0 == 0, st));
+    else
+      CK(launch_head_stats(r, g.m, g.d, T_, C, n0, c.tgt, n0 == 0, st));
   }
   CK(launch_head_rows(r, c.tgt, T_, V, c.scale, c.loss_m, c.loss_d, c.rowloss, st));
   if (!c.grads) return FDH_OK;
@@ -259,9 +293,10 @@ int Engine::head_run(const HeadCall& c) {
   const size_t ob = c.out_f32 ? 4 : sizeof(T);
   for (int n0 = 0; n0 < V; n0 += k.C) {
     const int C = std::min(k.C, V - n0);
-    int rc = k.C < V ? logits(n0, C) : FDH_OK;
+    // (fp32 models with one piece still have its logits)
+    int rc = sizeof(T) == 2 || k.C < V ? logits(n0, C, true) : FDH_OK;
     if (rc != FDH_OK) return rc;
-    CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, c.scale, st));
+    if constexpr (sizeof(T) == 4) CK(launch_head_dlogits(r, g.m, g.d, T_, k.Tp, C, n0, c.tgt, c.scale, st));
     GemmArgs a[2];
     for (GemmArgs& x : a) {
       x.M = T_; x.N = d; x.K = C;

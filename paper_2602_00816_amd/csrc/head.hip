@@ -11,6 +11,7 @@
 // A first pass over the pieces leaves c, the four sums and the target's logits of every row, a
 // second one forms the logits again and gives their gradient to the products: nothing of the
 // size of the logits stays.
+#include "head_dev.h"
 #include "kernels.h"
 
 namespace fdh {
@@ -18,46 +19,6 @@ namespace fdh {
 namespace {
 
 constexpr int NT = 256;
-
-constexpr float FAR_APART = 0.5f;   // from this |ld| on: p and q in the place of a and s
-
-// a and s (or p and q) of one logit.  bf16 models: fp32 (the exponential is common to both
-// points); fp32 models: fp64.  The series' first omitted terms are below 1e-10 (|ld| < 1/16) and
-// 1e-8 (1/2) of the sum, in fp64 2^-40 / 10!.
-__device__ inline void pair_exp(float lm, float ld, float c, float& a, float& s) {
-  const float x = lm - c, b = fabsf(ld);
-  if (b < 0.0625f) {
-    const float e = __expf(x), b2 = ld * ld;
-    a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24)));
-    s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120)));
-  } else if (b < FAR_APART) {
-    const float e = __expf(x), b2 = ld * ld;
-    a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24 + b2 * (1.f / 720 + b2 * (1.f / 40320)))));
-    s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120 + b2 * (1.f / 5040))));
-  } else {
-    a = __expf(x + ld);
-    s = __expf(x - ld);
-  }
-}
-__device__ inline void pair_exp(float lm, float ld, float c, double& a, double& s) {
-  const double x = (double)lm - (double)c, b = ld;
-  if (fabs(b) < 0.0625) {
-    const double e = exp(x), b2 = b * b;
-    a = e * (1.0 + b2 * (1.0 / 2 + b2 * (1.0 / 24 + b2 * (1.0 / 720 + b2 * (1.0 / 40320)))));
-    s = e * b * (1.0 + b2 * (1.0 / 6 + b2 * (1.0 / 120 + b2 * (1.0 / 5040 + b2 * (1.0 / 362880)))));
-  } else {
-    const double p = exp(x + b), q = exp(x - b);
-    const bool far = !(fabs(b) < FAR_APART);
-    a = far ? p : 0.5 * (p + q);
-    s = far ? q : 0.5 * (p - q);
-  }
-}
-__device__ inline bool far_apart(float ld) { return !(fabsf(ld) < FAR_APART); }
-
-template <typename T> struct Stat { typedef double type; };
-template <> struct Stat<bf16_t> { typedef float type; };
-
-__device__ inline float ref_of(float lm, float ld) { return lm + fabsf(ld); }
 
 // targets of a [B, S] batch, aligned with the rows that predict them (the next token or its
 // label; none for the last position); out of range: clamped, the batch's check reports it
@@ -69,12 +30,10 @@ __global__ void head_targets_kernel(int32_t* tgt, const int32_t* tok, const int3
 }
 
 // Statistics of one piece of the logits, columns n0 .. n0 + C - 1 of the vocabulary, joined to
-// those of the pieces before.  One workgroup per row; every thread keeps its sums relative to
-// its own maximum.
-template <typename T>
+// those of the pieces before (fp32 models).  One workgroup per row; every thread keeps its sums
+// relative to its own maximum.
 __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, const float* lm, const float* ld, int C, int n0,
                                                         const int32_t* tgt, bool first) {
-  typedef typename Stat<T>::type F;
   __shared__ double sh[NT / 64];
   const int64_t t = blockIdx.x;
   const int y = tgt[t];
@@ -85,7 +44,7 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, const float*
   double z[4] = {0.0, 0.0, 0.0, 0.0};   // Sa, Ss, Sp, Sq
   for (int j = 4 * threadIdx.x; j < C; j += 4 * NT) {
     const float4 a = *reinterpret_cast<const float4*>(m + j), b = *reinterpret_cast<const float4*>(d + j);
-    const float top = fmaxf(fmaxf(ref_of(a.x, b.x), ref_of(a.y, b.y)), fmaxf(ref_of(a.z, b.z), ref_of(a.w, b.w)));
+    const float top = fmaxf(fmaxf(head_ref(a.x, b.x), head_ref(a.y, b.y)), fmaxf(head_ref(a.z, b.z), head_ref(a.w, b.w)));
     if (top > mt) {
       const double f = mt > -INFINITY ? exp((double)mt - (double)top) : 0.0;
 #pragma unroll
@@ -93,13 +52,13 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, const float*
       mt = top;
     }
     auto add = [&](float x, float y) {
-      F p, s;
+      double p, s;
       pair_exp(x, y, mt, p, s);
       const int k = far_apart(y) ? 2 : 0;
-      z[0] += k ? F(0) : p;
-      z[1] += k ? F(0) : s;
-      z[2] += k ? p : F(0);
-      z[3] += k ? s : F(0);
+      z[0] += k ? 0.0 : p;
+      z[1] += k ? 0.0 : s;
+      z[2] += k ? p : 0.0;
+      z[3] += k ? s : 0.0;
     };
     add(a.x, b.x);
     add(a.y, b.y);
@@ -162,32 +121,30 @@ __global__ void head_rows_kernel(HeadRows r, const int32_t* tgt, int T_, int V, 
   for (int k = 0; k < 4; ++k) r.f[k][t] = f[k];
 }
 
-// Gradient of one piece of the logits in the operand type, [Tp][C]; rows without a target and
-// rows behind the last are zeros.  fp32 models: in place of the logits.
-template <typename T>
-__global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r, const float* lm, const float* ld, int T_, int C,
-                                                          int n0, const int32_t* tgt, double scale) {
-  typedef typename Stat<T>::type F;
+// Gradient of one piece of the logits in their place, [Tp][C] (fp32 models); rows without a target
+// and rows behind the last are zeros.
+__global__ __launch_bounds__(NT) void head_dlogits_kernel(HeadRows r, float* lm, float* ld, int T_, int C, int n0,
+                                                          const int32_t* tgt, double scale) {
   const int64_t t = blockIdx.x;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
   const int64_t base = t * C;
   if (y == IGNORE_LABEL) {
     for (int j = threadIdx.x; j < C; j += NT) {
-      stf(o.m, base + j, 0.f);
-      stf(o.d, base + j, 0.f);
+      lm[base + j] = 0.f;
+      ld[base + j] = 0.f;
     }
     return;
   }
   const float c = r.top[t];
-  const F f0 = (F)r.f[0][t], f1 = (F)r.f[1][t], f2 = (F)r.f[2][t], f3 = (F)r.f[3][t];
+  const double f0 = r.f[0][t], f1 = r.f[1][t], f2 = r.f[2][t], f3 = r.f[3][t];
   for (int j = threadIdx.x; j < C; j += NT) {
-    F p, s;
+    double p, s;
     const float b = ld[base + j];
     pair_exp(lm[base + j], b, c, p, s);
     const bool far = far_apart(b);
-    const F m = far ? p * f2 + s * f3 : p * f0 - s * f1;
-    stf(o.m, base + j, (float)(m - (n0 + j == y ? (F)scale : F(0))));
-    stf(o.d, base + j, (float)(far ? p * f2 - s * f3 : s * f0 - p * f1));
+    const double m = far ? p * f2 + s * f3 : p * f0 - s * f1;
+    lm[base + j] = (float)(m - (n0 + j == y ? scale : 0.0));
+    ld[base + j] = (float)(far ? p * f2 - s * f3 : s * f0 - p * f1);
   }
 }
 
@@ -223,10 +180,9 @@ hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* 
   hipLaunchKernelGGL(head_targets_kernel, dim3(ceil_div(T_, NT)), dim3(NT), 0, s, tgt, tok, lab, T_, S, V);
   return hipGetLastError();
 }
-template <typename T>
 hipError_t launch_head_stats(const HeadRows& r, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt, bool first,
                              hipStream_t s) {
-  hipLaunchKernelGGL(head_stats_kernel<T>, dim3(T_), dim3(NT), 0, s, r, lm, ld, C, n0, tgt, first);
+  hipLaunchKernelGGL(head_stats_kernel, dim3(T_), dim3(NT), 0, s, r, lm, ld, C, n0, tgt, first);
   return hipGetLastError();
 }
 hipError_t launch_head_rows(const HeadRows& r, const int32_t* tgt, int T_, int V, double scale, float* loss_m, float* loss_d,
@@ -234,10 +190,9 @@ hipError_t launch_head_rows(const HeadRows& r, const int32_t* tgt, int T_, int V
   hipLaunchKernelGGL(head_rows_kernel, dim3(ceil_div(T_, NT)), dim3(NT), 0, s, r, tgt, T_, V, scale, loss_m, loss_d, rowloss);
   return hipGetLastError();
 }
-template <typename T>
-hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
-                               const int32_t* tgt, double scale, hipStream_t s) {
-  hipLaunchKernelGGL(head_dlogits_kernel<T>, dim3(Tp), dim3(NT), 0, s, o, r, lm, ld, T_, C, n0, tgt, scale);
+hipError_t launch_head_dlogits(const HeadRows& r, float* lm, float* ld, int T_, int Tp, int C, int n0, const int32_t* tgt,
+                               double scale, hipStream_t s) {
+  hipLaunchKernelGGL(head_dlogits_kernel, dim3(Tp), dim3(NT), 0, s, r, lm, ld, T_, C, n0, tgt, scale);
   return hipGetLastError();
 }
 template <typename T>
@@ -250,13 +205,8 @@ hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const
   return hipGetLastError();
 }
 
-#define INST(T)                                                                                                                    \
-  template hipError_t launch_head_stats<T>(const HeadRows&, const float*, const float*, int, int, int, const int32_t*, bool,       \
-                                           hipStream_t);                                                                           \
-  template hipError_t launch_head_dlogits<T>(PairT<T>, const HeadRows&, const float*, const float*, int, int, int, int,            \
-                                             const int32_t*, double, hipStream_t);                                                 \
-  template hipError_t launch_head_copy<T>(PairT<T>, const T*, const T*, int64_t, int, int, int, const int32_t*, hipStream_t);
-INST(float)
-INST(bf16_t)
+template hipError_t launch_head_copy<float>(PairT<float>, const float*, const float*, int64_t, int, int, int, const int32_t*, hipStream_t);
+template hipError_t launch_head_copy<bf16_t>(PairT<bf16_t>, const bf16_t*, const bf16_t*, int64_t, int, int, int, const int32_t*,
+                                             hipStream_t);
 
 }  // namespace fdh

@@ -1,0 +1,413 @@
+// The logits' pair of bf16 models without logits in memory: the product of a tile of rows and a
+// tile of the vocabulary, both channels at once, whose epilogue leaves either the rows'
+// statistics over the tile's columns or the logits' gradient in bf16.
+//
+// lm = xm wm^T and ld = xd wm^T + xm wd^T share their operands: a K slice of the four tiles (x and
+// w, mean and half difference) feeds three matrix operations per output block, as many bytes per
+// operation as a 256 x 256 tile of one product takes from two.  Slices of 32 k come by direct
+// loads to LDS into a ring of three stages, two slices ahead; a wavefront keeps two fragment
+// sets (half slices of 16 k) and reads one while the matrix operations run on the other.  A
+// stage is free as soon as every wavefront has the second half of its slice in registers, which
+// the wait before the slice's one barrier makes sure of.
+#include "gemm_dev.h"
+#include "head_dev.h"
+#include "kernels.h"
+
+#include <type_traits>
+
+namespace fdh {
+
+namespace {
+
+constexpr int KT = 32;                  // k per slice
+constexpr uint32_t OOB = 0x80000000u;   // byte offset at which the buffer resources end
+
+// element (row, 16-byte chunk c) of a [rows][32] tile: 16 lanes that read 16 consecutive rows hit 64 banks
+__device__ inline int tile_at(int row, int c) { return row * KT + ((c ^ ((row >> 2) & 3)) << 3); }
+__device__ inline bf16x8_t fragment(const bf16_t* t, int r0, int kk, int lane) {
+  return *reinterpret_cast<const bf16x8_t*>(t + tile_at(r0 + (lane & 31), (kk >> 3) + (lane >> 5)));
+}
+
+template <int BM, int BN, int WM, int WN, bool GRAD>
+__global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a, HeadRows r) {
+  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, IM = WTM / 32, JN = WTN / 32;
+  constexpr int STAGE = 2 * (BM + BN) * KT;          // elements: xm, xd, wm, wd
+  constexpr int NU = 2 * (BM + BN) / 16 / NW;        // 1 KB loads per wavefront and slice
+  constexpr int NF = 2 * (IM + JN);                  // fragments of a half slice
+  constexpr int NM = 3 * IM * JN;                    // matrix operations of a half slice
+  static_assert(2 * (BM + BN) / 16 % NW == 0 && BM % 16 == 0 && BN % 16 == 0, "whole loads per wavefront");
+  __shared__ __attribute__((aligned(1024))) bf16_t st0[STAGE];
+  __shared__ __attribute__((aligned(1024))) bf16_t st1[STAGE];
+  __shared__ __attribute__((aligned(1024))) bf16_t st2[STAGE];
+
+  const int gx = (a.C + BN - 1) / BN, gy = (a.T + BM - 1) / BM;
+  const int lin = xcd_order(blockIdx.x, gridDim.x);
+  // tiles run down 4 tile rows before the next column (an XCD's tiles share 4 row and 8 column blocks)
+  constexpr int GM = 4;
+  const int gsize = GM * gx, first_m = lin / gsize * GM, gm_rows = min(gy - first_m, GM);
+  const int tm = first_m + lin % gsize % gm_rows, tn = lin % gsize / gm_rows;
+  const int m0 = tm * BM, n0 = tn * BN;
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int total = (a.d + KT - 1) / KT;
+
+  // load q of a slice: 16 rows of one of the four tiles.  Rows past the end read the last one
+  // (their outputs are not used), lanes past the contraction's end nothing (zeros).
+  const int ck = (lane & 3) ^ ((lane >> 4) & 3);   // (row >> 2 is lane >> 4 modulo 4)
+  const bf16_t* base[NU];
+  uint32_t vo[NU];
+#pragma clang loop unroll(full)
+  for (int u = 0; u < NU; ++u) {
+    const int q = wave + u * NW;
+    const bool isx = q < 2 * BM / 16;
+    const int qx = isx ? q : q - 2 * BM / 16;
+    const int per = isx ? BM / 16 : BN / 16;
+    const bool half = qx >= per;
+    const int row = (half ? qx - per : qx) * 16 + (lane >> 2);
+    const int64_t ld = isx ? a.ldx : a.d;
+    const int first = isx ? m0 : n0, end = isx ? a.T : a.C;
+    const bf16_t* p = isx ? (half ? a.xd : a.xm) : (half ? a.wd : a.wm);
+    base[u] = p + first * ld;
+    vo[u] = 2u * (uint32_t)((min(first + row, end - 1) - first) * ld + 8 * ck);
+  }
+  auto stage = [&](auto s) -> bf16_t* {
+    constexpr int S = decltype(s)::value % 3;
+    if constexpr (S == 0) return st0;
+    else if constexpr (S == 1) return st1;
+    else return st2;
+  };
+  // load u of slice t (past the last: the last again, into a stage that nobody reads)
+  auto dma = [&](bf16_t* st, int t, int u) {
+    const int k0 = min(t, total - 1) * KT;
+    const uint64_t b = (uint64_t)(uintptr_t)(base[u] + k0);
+    const i32x4_t rs{(int)(uint32_t)b, (int)((b >> 32) & 0xffffu), (int)OOB, 0x00020000};
+    const uint32_t off = 8 * ck < a.d - k0 ? vo[u] : OOB;
+    const uint32_t ldsaddr = (uint32_t)(uintptr_t)(lds_void_t*)st + (uint32_t)((wave + u * NW) * 1024);
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds"
+        :
+        : "s"(ldsaddr), "v"(off), "s"(rs)
+        : "memory", "m0");
+  };
+
+  f32x16_t cm[IM][JN], cd[IM][JN];
+#pragma clang loop unroll(full)
+  for (int i = 0; i < IM; ++i)
+#pragma clang loop unroll(full)
+    for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+      for (int e = 0; e < 16; ++e) cm[i][j][e] = cd[i][j][e] = 0.f;
+
+  // fragments 0 .. IM - 1: xm, then JN of wm, IM of xd, JN of wd (the order in which they are used)
+  bf16x8_t f0[NF], f1[NF];
+  auto rd = [&](bf16x8_t& f, const bf16_t* st, int x, int kk) {
+    if (x < IM) f = fragment(st, wm * WTM + x * 32, kk, lane);
+    else if (x < IM + JN) f = fragment(st + 2 * BM * KT, wn * WTN + (x - IM) * 32, kk, lane);
+    else if (x < 2 * IM + JN) f = fragment(st + BM * KT, wm * WTM + (x - IM - JN) * 32, kk, lane);
+    else f = fragment(st + (2 * BM + BN) * KT, wn * WTN + (x - 2 * IM - JN) * 32, kk, lane);
+  };
+  auto mma = [&](const bf16x8_t (&f)[NF], int e) {
+    const int kind = e / (IM * JN), i = e % (IM * JN) / JN, j = e % JN;
+    const bf16x8_t *xm = f, *wmf = f + IM, *xd = f + IM + JN, *wdf = f + 2 * IM + JN;
+    if (kind == 0) cm[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xm[i], cm[i][j], 0, 0, 0);
+    else if (kind == 1) cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xd[i], cd[i][j], 0, 0, 0);
+    else cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xm[i], cd[i][j], 0, 0, 0);
+  };
+  auto step = [&](auto s, int t) {
+    constexpr int S = decltype(s)::value;
+    bf16_t* cur = stage(s);
+    const bf16_t* nxt = stage(std::integral_constant<int, S + 1>{});
+#pragma clang loop unroll(full)
+    for (int x = 0; x < NF; ++x) {
+      rd(f1[x], cur, x, 16);
+#pragma clang loop unroll(full)
+      for (int e = x * NM / NF; e < (x + 1) * NM / NF; ++e) mma(f0, e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // own loads of slice t + 1 are there (slice t + 2's may be on their way) and own reads of slice
+    // t are done: after the barrier everyone's are, and stage S is free
+    __builtin_amdgcn_s_waitcnt((NU & 15) | ((NU >> 4) << 14) | (7 << 4) | (0 << 8));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma clang loop unroll(full)
+    for (int x = 0; x < NF; ++x) {
+      if (x < NU) dma(cur, t + 3, x);
+      if (x == NF - 1) {
+#pragma clang loop unroll(full)
+        for (int u = NF; u < NU; ++u) dma(cur, t + 3, u);
+      }
+      rd(f0[x], nxt, x, 0);
+#pragma clang loop unroll(full)
+      for (int e = x * NM / NF; e < (x + 1) * NM / NF; ++e) mma(f1, e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // slices 0, 1 and 2; the first is waited for
+#pragma clang loop unroll(full)
+  for (int u = 0; u < NU; ++u) dma(st0, 0, u);
+#pragma clang loop unroll(full)
+  for (int u = 0; u < NU; ++u) dma(st1, 1, u);
+#pragma clang loop unroll(full)
+  for (int u = 0; u < NU; ++u) dma(st2, 2, u);
+  wait_vm<2 * NU>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma clang loop unroll(full)
+  for (int x = 0; x < NF; ++x) rd(f0[x], st0, x, 0);
+  for (int t = 0; t < total; t += 3) {
+    step(std::integral_constant<int, 0>{}, t);
+    if (t + 1 < total) step(std::integral_constant<int, 1>{}, t + 1);
+    if (t + 2 < total) step(std::integral_constant<int, 2>{}, t + 2);
+  }
+  wait_vm<0>();   // no load may land in LDS from here on
+
+  // A block holds its part of the logits' transpose: lane l has row l & 31 and, for g = 0 .. 3, the
+  // columns 8 g + 4 (l >> 5) + 0 .. 3.  Lanes l and l + 32 share a row.
+  const int h = lane >> 5;
+  const int c0 = n0 + wn * WTN, live = a.C - c0;   // the wavefront's first column and how many there are
+  if constexpr (!GRAD) {
+    if (live <= 0) return;
+    if (live < WTN) {
+#pragma clang loop unroll(full)
+      for (int i = 0; i < IM; ++i)
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e)
+            if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 >= live) {
+              cm[i][j][e] = -INFINITY;
+              cd[i][j][e] = 0.f;
+            }
+    }
+#pragma clang loop unroll(full)
+    for (int i = 0; i < IM; ++i) {
+      const int row = m0 + wm * WTM + i * 32 + (lane & 31);
+      float mx = -INFINITY, far = 0.f;
+#pragma clang loop unroll(full)
+      for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+        for (int e = 0; e < 16; ++e) {
+          mx = fmaxf(mx, head_ref(cm[i][j][e], cd[i][j][e]));
+          far = fmaxf(far, fabsf(cd[i][j][e]));
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      float z[4] = {0.f, 0.f, 0.f, 0.f};
+      if (!__any(!(far < HEAD_NEAR))) {   // (NaN: a half difference that is NaN makes the sums NaN either way)
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e) {
+            float p, s;
+            pair_exp_near(cm[i][j][e], cd[i][j][e], mx, p, s);
+            z[0] += p;
+            z[1] += s;
+          }
+      } else {
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e) {
+            float p, s;
+            pair_exp(cm[i][j][e], cd[i][j][e], mx, p, s);
+            const bool apart = far_apart(cd[i][j][e]);
+            z[0] += apart ? 0.f : p;
+            z[1] += apart ? 0.f : s;
+            z[2] += apart ? p : 0.f;
+            z[3] += apart ? s : 0.f;
+          }
+      }
+#pragma clang loop unroll(full)
+      for (int k = 0; k < 4; ++k) z[k] += __shfl_xor(z[k], 32, 64);
+      if (row >= a.T) continue;
+      if (h == 0) {
+        float* o = a.part + (int64_t)(c0 / WTN) * 5 * a.T + row;
+        o[0] = mx;
+#pragma clang loop unroll(full)
+        for (int k = 0; k < 4; ++k) o[(int64_t)(k + 1) * a.T] = z[k];
+      }
+      const int y = a.tgt[row] - a.n0 - c0;   // (a row without a target has a negative one)
+      if (y >= 0 && y < min(live, WTN) && ((y >> 2) & 1) == h) {
+        float ym = 0.f, yd = 0.f;
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e)
+            if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 == y) {
+              ym = cm[i][j][e];
+              yd = cd[i][j][e];
+            }
+        r.ym[row] = ym;
+        r.yd[row] = yd;
+      }
+    }
+  } else {
+    // through LDS, so that a store covers 8 rows of 64 columns (JN = 2) or 16 of 32; a wavefront's
+    // own area, 32 rows of WTN columns for each channel in turn
+    constexpr int LD = WTN + 4;      // elements: 8-byte rows, lanes of 32 rows on distinct banks
+    static_assert(NW * 32 * LD <= STAGE, "staging areas exceed a stage");
+    __syncthreads();                 // every wavefront is done with the ring
+    bf16_t* stg = st0 + wave * 32 * LD;
+    constexpr int LPR = WTN / 8, RPS = 64 / LPR;   // lanes per row of a store, rows per store
+#pragma clang loop unroll(full)
+    for (int i = 0; i < IM; ++i) {
+      const int rb = m0 + wm * WTM + i * 32;
+      const int row = rb + (lane & 31);
+      const int t = min(row, a.T - 1);
+      const int y = row < a.T ? a.tgt[t] : IGNORE_LABEL;
+      const bool none = y == IGNORE_LABEL;
+      const float top = r.top[t];
+      const float w0 = (float)r.f[0][t], w1 = (float)r.f[1][t], w2 = (float)r.f[2][t], w3 = (float)r.f[3][t];
+      const int yc = y - a.n0 - c0;
+      float far = 0.f;
+#pragma clang loop unroll(full)
+      for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+        for (int e = 0; e < 16; ++e) far = fmaxf(far, fabsf(cd[i][j][e]));
+      if (!__any(!(far < HEAD_NEAR))) {
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e) {
+            float p, s;
+            pair_exp_near(cm[i][j][e], cd[i][j][e], top, p, s);
+            cm[i][j][e] = p * w0 - s * w1;
+            cd[i][j][e] = s * w0 - p * w1;
+          }
+      } else {
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e) {
+            float p, s;
+            const bool apart = far_apart(cd[i][j][e]);
+            pair_exp(cm[i][j][e], cd[i][j][e], top, p, s);
+            cm[i][j][e] = apart ? p * w2 + s * w3 : p * w0 - s * w1;
+            cd[i][j][e] = apart ? p * w2 - s * w3 : s * w0 - p * w1;
+          }
+      }
+      if (yc >= 0 && yc < WTN) {
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int e = 0; e < 16; ++e)
+            if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 == yc) cm[i][j][e] -= a.scale;
+      }
+#pragma clang loop unroll(full)
+      for (int ch = 0; ch < 2; ++ch) {
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int g = 0; g < 4; ++g) {
+            const f32x16_t& v = ch ? cd[i][j] : cm[i][j];
+            auto two = [&](int e) {
+              return (uint32_t)f32_to_bf16(none ? 0.f : v[e]) | ((uint32_t)f32_to_bf16(none ? 0.f : v[e + 1]) << 16);
+            };
+            *reinterpret_cast<uint2*>(stg + (lane & 31) * LD + j * 32 + 8 * g + 4 * h) = make_uint2(two(4 * g), two(4 * g + 2));
+          }
+        wave_lds_order();
+        bf16_t* o = ch ? a.gd : a.gm;
+#pragma clang loop unroll(full)
+        for (int k = 0; k < 32 / RPS; ++k) {
+          const int lr = k * RPS + lane / LPR, lc = 8 * (lane % LPR);
+          const uint2* p = reinterpret_cast<const uint2*>(stg + lr * LD + lc);
+          const uint2 u = p[0], v = p[1];
+          if (rb + lr < a.Tp && lc < live)   // (C is a multiple of 8)
+            *reinterpret_cast<uint4*>(o + (int64_t)(rb + lr) * a.C + c0 + lc) = make_uint4(u.x, u.y, v.x, v.y);
+        }
+        wave_lds_order();   // the next writes come after these reads
+      }
+    }
+  }
+}
+
+// Joins the tiles' statistics of the rows to those of the pieces before: 256 / R threads per
+// row take every 256 / R-th column group.
+template <int R>
+__global__ __launch_bounds__(256) void head_join_kernel(HeadRows r, const float* part, int groups, int T_, const int32_t* tgt, bool first) {
+  constexpr int L = 256 / R;
+  __shared__ double sh[5][L][R];
+  const int lr = threadIdx.x % R, l = threadIdx.x / R;
+  const int64_t t = (int64_t)blockIdx.x * R + lr;
+  const bool on = t < T_ && tgt[min(t, (int64_t)T_ - 1)] != IGNORE_LABEL;
+  double top = -INFINITY, z[4] = {0.0, 0.0, 0.0, 0.0};
+  auto join = [&](double m, const double (&x)[4]) {
+    const double mx = fmax(top, m);
+    const double f = top == mx || top == -INFINITY ? 1.0 : exp(top - mx);
+    const double g = m == mx || m == -INFINITY ? 1.0 : exp(m - mx);   // (sums at no maximum are NaN or nothing)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] = z[k] * f + x[k] * g;
+    top = mx;
+  };
+  if (on) {
+    constexpr int U = 4;
+    for (int g0 = l; g0 < groups; g0 += U * L) {
+      float v[U][5];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < 5; ++k) v[u][k] = part[((int64_t)min(g0 + u * L, groups - 1) * 5 + k) * T_ + t];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g0 + u * L < groups) join(v[u][0], {v[u][1], v[u][2], v[u][3], v[u][4]});
+    }
+  }
+  sh[0][l][lr] = top;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
+  __syncthreads();
+  // halves joined until one is left (a fixed order)
+  for (int n = L / 2; n > 0; n /= 2) {
+    if (l < n) {
+      join(sh[0][l + n][lr], {sh[1][l + n][lr], sh[2][l + n][lr], sh[3][l + n][lr], sh[4][l + n][lr]});
+      sh[0][l][lr] = top;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
+    }
+    __syncthreads();
+  }
+  if (l != 0 || !on) return;
+  if (!first) join(r.top[t], {r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]});
+  r.top[t] = (float)top;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) r.z[k][t] = z[k];
+}
+
+template <int BM, int BN, int WM, int WN>
+void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
+  const int rows = grad ? a.Tp : a.T;   // (Tp - T < 8 rows never add a tile: T is their only source)
+  (void)rows;
+  const dim3 grid(ceil_div(a.C, BN) * ceil_div(a.T, BM)), block(64 * WM * WN);
+  if (grad) hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, true>), grid, block, 0, s, a, r);
+  else hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, false>), grid, block, 0, s, a, r);
+}
+
+}  // namespace
+
+HeadTile head_tile(int T_, int C) {
+  (void)C;
+  if (T_ <= 32) return {32, 128, 32};
+  if (T_ <= 128) return {64, 64, 32};
+  return {256, 128, 64};
+}
+
+hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
+  const HeadTile t = head_tile(a.T, a.C);
+  if (t.BM == 32) launch_tile<32, 128, 1, 4>(a, r, grad, s);
+  else if (t.BM == 64) launch_tile<64, 64, 2, 2>(a, r, grad, s);
+  else launch_tile<256, 128, 4, 2>(a, r, grad, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_join(const HeadRows& r, const float* part, int groups, int T_, const int32_t* tgt, bool first, hipStream_t s) {
+  if (T_ >= 1024) hipLaunchKernelGGL(head_join_kernel<16>, dim3(ceil_div(T_, 16)), dim3(256), 0, s, r, part, groups, T_, tgt, first);
+  else hipLaunchKernelGGL(head_join_kernel<1>, dim3(T_), dim3(256), 0, s, r, part, groups, T_, tgt, first);
+  return hipGetLastError();
+}
+
+}  // namespace fdh
