@@ -218,6 +218,7 @@ int Engine::head_run(const HeadCall& c) {
     r.z[q] = (double*)(ws + k.z) + q * t;
     r.f[q] = (double*)(ws + k.f) + q * t;
   }
+  const HeadTile tile = head_tile(T_, k.C);
   const PairT<T> g{(T*)(ws + k.gm), (T*)(ws + k.gd)};
   const T *wm = (const T*)c.w_m, *wd = (const T*)c.w_d;
   const T *xm = (const T*)c.x_m, *xd = (const T*)c.x_d;
@@ -246,6 +247,7 @@ int Engine::head_run(const HeadCall& c) {
       h.part = (float*)(ws + k.part);
       h.gm = g.m; h.gd = g.d;
       h.scale = (float)c.scale;
+      h.tile = tile;
       int e0 = 0;
       if (timing.on) CK(timing.begin(st, &e0));
       CK(launch_head_logits(h, r, grad, st));
@@ -278,7 +280,7 @@ int Engine::head_run(const HeadCall& c) {
     const int rc = logits(n0, C, false);
     if (rc != FDH_OK) return rc;
     if constexpr (sizeof(T) == 2)
-      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, head_tile(T_, C).group), T_, c.tgt, n0 == 0, st));
+      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, tile.group), T_, c.tgt, n0 == 0, st));
     else
       CK(launch_head_stats(r, g.m, g.d, T_, C, n0, c.tgt, n0 == 0, st));
   }

@@ -380,8 +380,6 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadRows r, const float*
 
 template <int BM, int BN, int WM, int WN>
 void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
-  const int rows = grad ? a.Tp : a.T;   // (Tp - T < 8 rows never add a tile: T is their only source)
-  (void)rows;
   const dim3 grid(ceil_div(a.C, BN) * ceil_div(a.T, BM)), block(64 * WM * WN);
   if (grad) hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, true>), grid, block, 0, s, a, r);
   else hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, false>), grid, block, 0, s, a, r);
@@ -389,18 +387,32 @@ void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t 
 
 }  // namespace
 
+// The largest tile that the rows fill and that gives most compute units a workgroup.  Loss alone, us,
+// by tile (rows x columns):          256x128  128x128  64x128  64x64  32x128
+//   32 x 32000 x 2048                     84       60      53     54      53
+//   64 x 32000 x 2048                     85       63      56     65      70
+//   128 x 32000 x 2048                    87       73      87    100     116
+//   512 x 32000 x 2048                   193      233     295    345     415
+//   256 x 4096 x 512                      29       23      19     18      20
+//   512 x 4096 x 512                      30       26      24     26      29
+//   1024 x 4096 x 512                     31       28      32     34      40
+// (256 x 128 on four wavefronts of 128 x 64, and 128 x 256, are 1 to 5% slower than eight of 64 x 64
+// at 8192 x 32000 x 2048.)
 HeadTile head_tile(int T_, int C) {
-  (void)C;
-  if (T_ <= 32) return {32, 128, 32};
-  if (T_ <= 128) return {64, 64, 32};
-  return {256, 128, 64};
+  auto fills = [&](int bm, int bn) { return T_ > bm / 2 && (int64_t)ceil_div(T_, bm) * ceil_div(C, bn) >= 192; };
+  if (fills(256, 128)) return {256, 128, 64};
+  if (fills(128, 128)) return {128, 128, 32};
+  if (fills(64, 128)) return {64, 128, 32};
+  if (T_ > 32) return {64, 64, 32};
+  return {32, 128, 32};
 }
 
 hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
-  const HeadTile t = head_tile(a.T, a.C);
-  if (t.BM == 32) launch_tile<32, 128, 1, 4>(a, r, grad, s);
-  else if (t.BM == 64) launch_tile<64, 64, 2, 2>(a, r, grad, s);
-  else launch_tile<256, 128, 4, 2>(a, r, grad, s);
+  if (a.tile.BM == 256) launch_tile<256, 128, 4, 2>(a, r, grad, s);
+  else if (a.tile.BM == 128) launch_tile<128, 128, 2, 4>(a, r, grad, s);
+  else if (a.tile.BM == 64 && a.tile.BN == 128) launch_tile<64, 128, 2, 4>(a, r, grad, s);
+  else if (a.tile.BM == 64) launch_tile<64, 64, 2, 2>(a, r, grad, s);
+  else launch_tile<32, 128, 1, 4>(a, r, grad, s);
   return hipGetLastError();
 }
 

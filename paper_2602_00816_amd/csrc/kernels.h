@@ -334,6 +334,9 @@ template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
 // bf16 models (head_gemm.hip): the product that forms columns n0 .. n0 + C - 1 of the logits, and
 // what its epilogue makes of them
+struct HeadTile {
+  int BM, BN, group;       // rows and columns of a workgroup's tile, columns of a statistics group
+};
 struct HeadLogits {
   const bf16_t *xm, *xd;   // [T][ldx]
   int64_t ldx;
@@ -343,9 +346,7 @@ struct HeadLogits {
   float* part;             // statistics: [groups][5][T] (maximum and four sums), a group of HeadTile::group columns
   bf16_t *gm, *gd;         // gradient: [Tp][C]
   float scale;
-};
-struct HeadTile {
-  int BM, BN, group;
+  HeadTile tile;           // head_tile
 };
 HeadTile head_tile(int T_, int C);
 // grad: scale times the gradient of the losses, zeros in rows without a target and from T on; else
