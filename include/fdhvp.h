@@ -219,9 +219,10 @@ fdh_status fdh_set_recompute(fdh_ctx* ctx, int32_t on);
 
 /* The head of the HVP in pieces of the vocabulary: with columns > 0 the logits are formed
  * `columns` (rounded up to 256) at a time by the kernels of fdh_head_grad and never kept, so the
- * workspace holds 12 bytes (bf16) or 8 (fp32) per token and column of one piece in place of 12 or
+ * workspace holds 4 bytes (bf16) or 8 (fp32) per token and column of one piece in place of 12 or
  * 16 per token and word of the vocabulary; the logits are formed twice (3 more products of the
- * head's size, where it has 8).  0 keeps whole logits (the default).  Results agree to the rounding
+ * head's size, where it has 8), unless one piece holds the vocabulary (bf16: 12 bytes then).  0 keeps
+ * whole logits (the default).  Results agree to the rounding
  * of the context's dtype.  Takes effect for the following fdh_workspace_bytes / fdh_set_workspace;
  * the carve in use keeps its mode until then. */
 fdh_status fdh_set_vocab_piece(fdh_ctx* ctx, int32_t columns);
@@ -360,8 +361,8 @@ fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, siz
  *   loss[t] = log sum_j e^(l_tj) - l_ty as a float32 pair: _m the mean, _d the half difference of
  *   its values at the two points, not scaled; 0 for a row without a target.
  * fdh_head_grad also gives the gradients of scale * sum_t loss[t] (the loss pointers may be
- * NULL).  It forms the logits twice (once where one piece holds the vocabulary) and rounds
- * their gradient to the context's dtype, as the HVP's products do; sums and statistics are
+ * NULL).  It forms the logits twice (once where one piece holds the vocabulary: of up to 2^26
+ * logits that is chosen) and rounds their gradient to the context's dtype, as the HVP's products do; sums and statistics are
  * fp32 or wider, the order of the additions is fixed (the same bits in every call).  The
  * logits' mean leaves out x_d w_d^T, of second order in the step, as the HVP does.
  * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude.

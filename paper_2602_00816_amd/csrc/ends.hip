@@ -146,30 +146,36 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   };
   const size_t ob = bf16 ? 2 : 4, t = (size_t)T_;
   c.Tp = (int)((t + 7) / 8 * 8);
+  const bool whole = piece > 0 ? piece >= V : (int64_t)T_ * V <= HEAD_PIECE_ELEMS;
   int64_t C = piece > 0 ? piece : std::max<int64_t>(HEAD_PIECE_MIN, HEAD_PIECE_ELEMS / std::max(1, T_) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND);
   C = (C + HEAD_PIECE_ROUND - 1) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND;
-  c.C = (int)std::min<int64_t>(C, V);
+  c.C = (int)(whole ? V : std::min<int64_t>(C, V));
+  c.keep = c.C == V && (!bf16 || grads);   // the logits of the one piece are formed once
   const size_t tp = (size_t)c.Tp, pc = tp * c.C, td = tp * d;
   c.top = take(t * 4);
   c.z = take(4 * t * 8);
   c.ym = take(2 * t * 4);
   c.f = take(4 * t * 8);
   // fp32 models: a piece's logits, which their gradient replaces.  bf16 models: the gradient of a
-  // piece, in the first pass the statistics of column groups: of as many columns as fit there,
-  // alone of up to HEAD_PART bytes
+  // piece (and its logits where they are kept).  Statistics of column groups: bf16 models, in the
+  // first pass, in the gradient's place, of as many columns as fit there, alone of up to HEAD_PART bytes.
   c.C1 = c.C;
-  size_t part = 0;
+  c.lm = take(pc * (bf16 ? (c.keep ? 4 : 0) : 4));
+  c.ld = take(pc * (bf16 ? (c.keep ? 4 : 0) : 4));
   if (bf16) {
     const HeadTile tile = head_tile(T_, c.C);
     const size_t col = std::max<size_t>(1, t * 20 / tile.group), room = std::max<size_t>(grads ? pc * 4 : 0, piece > 0 ? 0 : HEAD_PART);
     c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, room / col / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
-    part = (size_t)ceil_div(c.C1, tile.group) * 20 * t;
+    const size_t part = (size_t)ceil_div(c.C1, tile.group) * 20 * t;
+    c.gm = take(grads ? pc * 2 : 0);
+    c.gd = take(grads ? pc * 2 : 0);
+    c.part = c.gm;
+    if (part > at - c.gm) take(part - (at - c.gm));
+  } else {
+    c.gm = c.lm;
+    c.gd = c.ld;
+    c.part = take((size_t)ceil_div(c.C, HEAD_CHUNK) * 40 * t);
   }
-  const size_t gb = bf16 ? (grads ? pc * 2 : 0) : pc * 4;
-  c.gm = take(gb);
-  c.gd = take(gb);
-  c.part = c.gm;
-  if (part > at - c.gm) take(part - (at - c.gm));
   c.xm = take(grads ? td * ob : 0);
   c.xd = take(grads ? td * ob : 0);
   c.dm = take(grads && bf16 ? t * d * 4 : 0);
@@ -218,6 +224,7 @@ int Engine::head_run(const HeadCall& c) {
     r.z[q] = (double*)(ws + k.z) + q * t;
     r.f[q] = (double*)(ws + k.f) + q * t;
   }
+  float *lm = (float*)(ws + k.lm), *ld = (float*)(ws + k.ld);
   const HeadTile tile = head_tile(T_, k.C);
   const PairT<T> g{(T*)(ws + k.gm), (T*)(ws + k.gd)};
   const T *wm = (const T*)c.w_m, *wd = (const T*)c.w_d;
@@ -234,8 +241,8 @@ int Engine::head_run(const HeadCall& c) {
     return FDH_OK;
   };
   // logits of columns n0 .. n0 + C - 1 (the product of the two half differences, of second order in
-  // the step, is left out, as in every linear layer): fp32 models in g, bf16 models statistics or
-  // gradient
+  // the step, is left out, as in every linear layer): fp32 models in lm and ld, bf16 models statistics
+  // (and, if kept, the logits) or gradient
   auto logits = [&](int n0, int C, bool grad) -> int {
     const T *pm = wm + (int64_t)n0 * d, *pd = wd + (int64_t)n0 * d;
     if constexpr (sizeof(T) == 2) {
@@ -246,6 +253,9 @@ int Engine::head_run(const HeadCall& c) {
       h.tgt = c.tgt;
       h.part = (float*)(ws + k.part);
       h.gm = g.m; h.gd = g.d;
+      if (k.keep) {
+        h.lm = lm; h.ld = ld;
+      }
       h.scale = (float)c.scale;
       h.tile = tile;
       int e0 = 0;
@@ -262,9 +272,9 @@ int Engine::head_run(const HeadCall& c) {
       a[0].npairs = 2;
       a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(pm, d);
       a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(pd, d);
-      a[0].C = g.d;
+      a[0].C = ld;
       a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(pm, d);
-      a[1].C = g.m;
+      a[1].C = lm;
       return product(a, 2);
     }
   };
@@ -275,16 +285,20 @@ int Engine::head_run(const HeadCall& c) {
     xd = o.d;
     ldx = d;
   }
+  const HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss};
   for (int n0 = 0; n0 < V; n0 += k.C1) {
     const int C = std::min(k.C1, V - n0);
     const int rc = logits(n0, C, false);
     if (rc != FDH_OK) return rc;
-    if constexpr (sizeof(T) == 2)
-      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, tile.group), T_, c.tgt, n0 == 0, st));
-    else
-      CK(launch_head_stats(r, g.m, g.d, T_, C, n0, c.tgt, n0 == 0, st));
+    const bool last = n0 + C == V;
+    if constexpr (sizeof(T) == 2) {
+      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, tile.group), T_, c.tgt, n0 == 0, last, out, st));
+    } else {
+      double* part = (double*)(ws + k.part);
+      CK(launch_head_stats(r, part, lm, ld, T_, C, n0, c.tgt, st));
+      CK(launch_head_join(r, (const double*)part, (int)ceil_div(C, HEAD_CHUNK), T_, c.tgt, n0 == 0, last, out, st));
+    }
   }
-  CK(launch_head_rows(r, c.tgt, T_, V, c.scale, c.loss_m, c.loss_d, c.rowloss, st));
   if (!c.grads) return FDH_OK;
   // the gradient of x is added up over the pieces in fp32
   const bool round = !c.out_f32 && k.C < V;
@@ -295,10 +309,9 @@ int Engine::head_run(const HeadCall& c) {
   const size_t ob = c.out_f32 ? 4 : sizeof(T);
   for (int n0 = 0; n0 < V; n0 += k.C) {
     const int C = std::min(k.C, V - n0);
-    // (fp32 models with one piece still have its logits)
-    int rc = sizeof(T) == 2 || k.C < V ? logits(n0, C, true) : FDH_OK;
+    int rc = k.keep ? FDH_OK : logits(n0, C, true);
     if (rc != FDH_OK) return rc;
-    if constexpr (sizeof(T) == 4) CK(launch_head_dlogits(r, g.m, g.d, T_, k.Tp, C, n0, c.tgt, c.scale, st));
+    if (sizeof(T) == 4 || k.keep) CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, c.scale, st));
     GemmArgs a[2];
     for (GemmArgs& x : a) {
       x.M = T_; x.N = d; x.K = C;

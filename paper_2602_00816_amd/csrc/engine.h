@@ -115,7 +115,8 @@ struct HeadCall {
 };
 struct HeadCarve {
   int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
-  size_t top, z, ym, f, part, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
+  bool keep = false;           // one piece, whose logits are formed once
+  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
 };
 
 double gemm_flops(const GemmArgs& g);   // executed by a product, causal tails clipped

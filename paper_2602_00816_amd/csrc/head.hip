@@ -10,7 +10,7 @@
 // instead, their sums kept apart (Z+ = Sa + Ss + Sp, Z- = Sa - Ss + Sq) and P+- = p / Z+, q / Z-.
 // A first pass over the pieces leaves c, the four sums and the target's logits of every row, a
 // second one forms the logits again and gives their gradient to the products: nothing of the
-// size of the logits stays.
+// size of the logits stays.  Where one piece holds the vocabulary its logits are formed once.
 #include "head_dev.h"
 #include "kernels.h"
 
@@ -29,20 +29,22 @@ __global__ void head_targets_kernel(int32_t* tgt, const int32_t* tok, const int3
   tgt[t] = y == IGNORE_LABEL ? y : min(max(y, 0), V - 1);
 }
 
-// Statistics of one piece of the logits, columns n0 .. n0 + C - 1 of the vocabulary, joined to
-// those of the pieces before (fp32 models).  One workgroup per row; every thread keeps its sums
-// relative to its own maximum.
-__global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, const float* lm, const float* ld, int C, int n0,
-                                                        const int32_t* tgt, bool first) {
+// Statistics of one piece of the logits (fp32 models), part [chunks][5][T]: the maximum and the four
+// sums of a row's CHUNK columns, one workgroup each; every thread keeps its sums relative to its own
+// maximum.
+constexpr int CHUNK = HEAD_CHUNK;
+__global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, double* part, const float* lm, const float* ld, int T_, int C, int n0,
+                                                        const int32_t* tgt) {
   __shared__ double sh[NT / 64];
   const int64_t t = blockIdx.x;
   const int y = tgt[t];
   if (y == IGNORE_LABEL) return;
   const float* m = lm + t * C;
   const float* d = ld + t * C;
+  const int from = blockIdx.y * CHUNK, end = min(from + CHUNK, C);
   float mt = -INFINITY;
   double z[4] = {0.0, 0.0, 0.0, 0.0};   // Sa, Ss, Sp, Sq
-  for (int j = 4 * threadIdx.x; j < C; j += 4 * NT) {
+  for (int j = from + 4 * threadIdx.x; j < end; j += 4 * NT) {
     const float4 a = *reinterpret_cast<const float4*>(m + j), b = *reinterpret_cast<const float4*>(d + j);
     const float top = fmaxf(fmaxf(head_ref(a.x, b.x), head_ref(a.y, b.y)), fmaxf(head_ref(a.z, b.z), head_ref(a.w, b.w)));
     if (top > mt) {
@@ -54,97 +56,162 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, const float*
     auto add = [&](float x, float y) {
       double p, s;
       pair_exp(x, y, mt, p, s);
-      const int k = far_apart(y) ? 2 : 0;
-      z[0] += k ? 0.0 : p;
-      z[1] += k ? 0.0 : s;
-      z[2] += k ? p : 0.0;
-      z[3] += k ? s : 0.0;
+      const bool apart = far_apart(y);
+      z[0] += apart ? 0.0 : p;
+      z[1] += apart ? 0.0 : s;
+      z[2] += apart ? p : 0.0;
+      z[3] += apart ? s : 0.0;
     };
     add(a.x, b.x);
     add(a.y, b.y);
     add(a.z, b.z);
     add(a.w, b.w);
   }
-  const float old = first ? -INFINITY : r.top[t];
-  const float mx = (float)block_max<NT>(fmax((double)mt, (double)old), sh);
+  const float mx = (float)block_max<NT>((double)mt, sh);
   // (a thread that saw NaN alone has no maximum: its sums are NaN at any factor but none)
   const double f = mt > -INFINITY ? exp((double)mt - (double)mx) : 1.0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) z[k] = block_sum<NT>(z[k] * f, sh);
   if (threadIdx.x != 0) return;
-  if (!first) {
-    const double g = old > -INFINITY ? exp((double)old - (double)mx) : 1.0;
+  double* o = part + (int64_t)blockIdx.y * 5 * T_ + t;
+  o[0] = mx;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) z[k] += r.z[k][t] * g;
-  }
-  r.top[t] = mx;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) r.z[k][t] = z[k];
-  if (y >= n0 && y < n0 + C) {
+  for (int k = 0; k < 4; ++k) o[(int64_t)(k + 1) * T_] = z[k];
+  if (y >= n0 + from && y < n0 + end) {
     r.ym[t] = m[y - n0];
     r.yd[t] = d[y - n0];
   }
 }
 
-// Losses of the rows and the factors of their gradients.  A target outside the vocabulary makes
-// its row NaN; rows without a target have no loss and no gradient.
-__global__ void head_rows_kernel(HeadRows r, const int32_t* tgt, int T_, int V, double scale, float* loss_m, float* loss_d,
-                                 double* rowloss) {
-  const int t = blockIdx.x * NT + threadIdx.x;
-  if (t >= T_) return;
-  const int y = tgt[t];
-  double m = 0.0, d = 0.0, f[4] = {0.0, 0.0, 0.0, 0.0};
-  if (y != IGNORE_LABEL) {
-    if (y < 0 || y >= V) {
-      m = d = f[0] = f[1] = f[2] = f[3] = __builtin_nan("");
-    } else {
-      const double sa = r.z[0][t], ss = r.z[1][t], sp = r.z[2][t], sq = r.z[3][t];
-      const double zp = sa + ss + sp, zn = sa - ss + sq, zm = sa + 0.5 * (sp + sq), zd = ss + 0.5 * (sp - sq);
-      const double lp = log(zp), ln = log(zn);
-      m = (double)r.top[t] - (double)r.ym[t] + 0.5 * (lp + ln);
-      d = (fabs(zd) < 0.5 * zm ? atanh(zd / zm) : 0.5 * (lp - ln)) - (double)r.yd[t];
-      f[0] = scale * (zm / (zp * zn));
-      f[1] = scale * (zd / (zp * zn));
-      f[2] = 0.5 * scale / zp;
-      f[3] = 0.5 * scale / zn;
+// Joins the groups' statistics of the rows to those of the pieces before: 256 / R threads per row
+// take every 256 / R-th group, then halves are joined until one is left.  After the last piece the
+// rows' losses and the factors of their gradients: a target outside the vocabulary makes its row
+// NaN, rows without a target have no loss and no gradient.
+template <int R, typename P>
+__global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part, int groups, int T_, const int32_t* tgt, bool first,
+                                                       bool last, HeadOut out) {
+  constexpr int L = NT / R;
+  __shared__ double sh[5][L][R];
+  const int lr = threadIdx.x % R, l = threadIdx.x / R;
+  const int64_t t = (int64_t)blockIdx.x * R + lr;
+  const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
+  const bool on = y != IGNORE_LABEL;
+  double top = -INFINITY, z[4] = {0.0, 0.0, 0.0, 0.0};
+  auto join = [&](double m, double x0, double x1, double x2, double x3) {
+    const double mx = fmax(top, m);
+    const double f = top == mx || top == -INFINITY ? 1.0 : exp(top - mx);
+    const double g = m == mx || m == -INFINITY ? 1.0 : exp(m - mx);   // (sums at no maximum are NaN or nothing)
+    z[0] = z[0] * f + x0 * g;
+    z[1] = z[1] * f + x1 * g;
+    z[2] = z[2] * f + x2 * g;
+    z[3] = z[3] * f + x3 * g;
+    top = mx;
+  };
+  if (on) {
+    constexpr int U = 4;
+    for (int g0 = l; g0 < groups; g0 += U * L) {
+      P v[U][5];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < 5; ++k) v[u][k] = part[((int64_t)min(g0 + u * L, groups - 1) * 5 + k) * T_ + t];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g0 + u * L < groups) join(v[u][0], v[u][1], v[u][2], v[u][3], v[u][4]);
     }
   }
-  if (loss_m) {
-    loss_m[t] = (float)m;
-    loss_d[t] = (float)d;
+  sh[0][l][lr] = top;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
+  __syncthreads();
+  for (int n = L / 2; n > 0; n /= 2) {
+    if (l < n) {
+      join(sh[0][l + n][lr], sh[1][l + n][lr], sh[2][l + n][lr], sh[3][l + n][lr], sh[4][l + n][lr]);
+      sh[0][l][lr] = top;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
+    }
+    __syncthreads();
   }
-  if (rowloss) {
-    rowloss[t] = (m + d) * scale;
-    rowloss[T_ + t] = (m - d) * scale;
+  if (l != 0 || t >= T_) return;
+  if (on) {
+    if (!first) join(r.top[t], r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]);
+    r.top[t] = (float)top;   // (a maximum of floats)
+  }
+  if (!last) {
+    if (on)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r.z[k][t] = z[k];
+    return;
+  }
+  double m = 0.0, d = 0.0, f[4] = {0.0, 0.0, 0.0, 0.0};
+  if (on && (y < 0 || y >= out.V)) {
+    m = d = f[0] = f[1] = f[2] = f[3] = __builtin_nan("");
+  } else if (on) {
+    const double sa = z[0], ss = z[1], sp = z[2], sq = z[3];
+    const double zp = sa + ss + sp, zn = sa - ss + sq, zm = sa + 0.5 * (sp + sq), zd = ss + 0.5 * (sp - sq);
+    const double lp = log(zp), ln = log(zn);
+    m = top - (double)r.ym[t] + 0.5 * (lp + ln);
+    d = (fabs(zd) < 0.5 * zm ? atanh(zd / zm) : 0.5 * (lp - ln)) - (double)r.yd[t];
+    f[0] = out.scale * (zm / (zp * zn));
+    f[1] = out.scale * (zd / (zp * zn));
+    f[2] = 0.5 * out.scale / zp;
+    f[3] = 0.5 * out.scale / zn;
+  }
+  if (out.loss_m) {
+    out.loss_m[t] = (float)m;
+    out.loss_d[t] = (float)d;
+  }
+  if (out.rowloss) {
+    out.rowloss[t] = (m + d) * out.scale;
+    out.rowloss[T_ + t] = (m - d) * out.scale;
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) r.f[k][t] = f[k];
 }
 
-// Gradient of one piece of the logits in their place, [Tp][C] (fp32 models); rows without a target
-// and rows behind the last are zeros.
-__global__ __launch_bounds__(NT) void head_dlogits_kernel(HeadRows r, float* lm, float* ld, int T_, int C, int n0,
+// Gradient of logits that are in memory (one piece holds the vocabulary, or an fp32 model) in the
+// operand type, [Tp][C]; rows without a target and rows behind the last are zeros.  o may be the
+// logits (fp32 models).
+template <typename T> struct Stat { typedef double type; };
+template <> struct Stat<bf16_t> { typedef float type; };
+__device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+__device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
+  auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16); };
+  *reinterpret_cast<uint2*>(p) = make_uint2(two(a, b), two(c, d));
+}
+template <typename T>
+__global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r, const float* lm, const float* ld, int T_, int C, int n0,
                                                           const int32_t* tgt, double scale) {
+  typedef typename Stat<T>::type F;
   const int64_t t = blockIdx.x;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
   const int64_t base = t * C;
+  const int from = blockIdx.y * CHUNK, end = min(from + CHUNK, C);
   if (y == IGNORE_LABEL) {
-    for (int j = threadIdx.x; j < C; j += NT) {
-      lm[base + j] = 0.f;
-      ld[base + j] = 0.f;
+    for (int j = from + 4 * threadIdx.x; j < end; j += 4 * NT) {
+      store4(o.m + base + j, 0.f, 0.f, 0.f, 0.f);
+      store4(o.d + base + j, 0.f, 0.f, 0.f, 0.f);
     }
     return;
   }
   const float c = r.top[t];
-  const double f0 = r.f[0][t], f1 = r.f[1][t], f2 = r.f[2][t], f3 = r.f[3][t];
-  for (int j = threadIdx.x; j < C; j += NT) {
-    double p, s;
-    const float b = ld[base + j];
-    pair_exp(lm[base + j], b, c, p, s);
-    const bool far = far_apart(b);
-    const double m = far ? p * f2 + s * f3 : p * f0 - s * f1;
-    lm[base + j] = (float)(m - (n0 + j == y ? scale : 0.0));
-    ld[base + j] = (float)(far ? p * f2 - s * f3 : s * f0 - p * f1);
+  const F f0 = (F)r.f[0][t], f1 = (F)r.f[1][t], f2 = (F)r.f[2][t], f3 = (F)r.f[3][t];
+  for (int j = from + 4 * threadIdx.x; j < end; j += 4 * NT) {
+    const float4 a4 = *reinterpret_cast<const float4*>(lm + base + j), b4 = *reinterpret_cast<const float4*>(ld + base + j);
+    const float a[4] = {a4.x, a4.y, a4.z, a4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
+    float gm[4], gd[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      F p, s;
+      pair_exp(a[e], b[e], c, p, s);
+      const bool apart = far_apart(b[e]);
+      const F m = apart ? p * f2 + s * f3 : p * f0 - s * f1;
+      gm[e] = (float)(m - (n0 + j + e == y ? (F)scale : F(0)));
+      gd[e] = (float)(apart ? p * f2 - s * f3 : s * f0 - p * f1);
+    }
+    store4(o.m + base + j, gm[0], gm[1], gm[2], gm[3]);
+    store4(o.d + base + j, gd[0], gd[1], gd[2], gd[3]);
   }
 }
 
@@ -180,21 +247,32 @@ hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* 
   hipLaunchKernelGGL(head_targets_kernel, dim3(ceil_div(T_, NT)), dim3(NT), 0, s, tgt, tok, lab, T_, S, V);
   return hipGetLastError();
 }
-hipError_t launch_head_stats(const HeadRows& r, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt, bool first,
+hipError_t launch_head_stats(const HeadRows& r, double* part, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt,
                              hipStream_t s) {
-  hipLaunchKernelGGL(head_stats_kernel, dim3(T_), dim3(NT), 0, s, r, lm, ld, C, n0, tgt, first);
+  hipLaunchKernelGGL(head_stats_kernel, dim3(T_, ceil_div(C, CHUNK)), dim3(NT), 0, s, r, part, lm, ld, T_, C, n0, tgt);
   return hipGetLastError();
 }
-hipError_t launch_head_rows(const HeadRows& r, const int32_t* tgt, int T_, int V, double scale, float* loss_m, float* loss_d,
-                            double* rowloss, hipStream_t s) {
-  hipLaunchKernelGGL(head_rows_kernel, dim3(ceil_div(T_, NT)), dim3(NT), 0, s, r, tgt, T_, V, scale, loss_m, loss_d, rowloss);
+// (16 rows per workgroup read 64 or 128 bytes at a time; where they would leave most of the chip idle
+// a workgroup takes one)
+template <typename P>
+hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_, const int32_t* tgt, bool first, bool last,
+                            const HeadOut& out, hipStream_t s) {
+  if (T_ >= 1024) hipLaunchKernelGGL((head_join_kernel<16, P>), dim3(ceil_div(T_, 16)), dim3(NT), 0, s, r, part, groups, T_, tgt, first, last, out);
+  else hipLaunchKernelGGL((head_join_kernel<1, P>), dim3(T_), dim3(NT), 0, s, r, part, groups, T_, tgt, first, last, out);
   return hipGetLastError();
 }
-hipError_t launch_head_dlogits(const HeadRows& r, float* lm, float* ld, int T_, int Tp, int C, int n0, const int32_t* tgt,
-                               double scale, hipStream_t s) {
-  hipLaunchKernelGGL(head_dlogits_kernel, dim3(Tp), dim3(NT), 0, s, r, lm, ld, T_, C, n0, tgt, scale);
+template hipError_t launch_head_join<float>(const HeadRows&, const float*, int, int, const int32_t*, bool, bool, const HeadOut&, hipStream_t);
+template hipError_t launch_head_join<double>(const HeadRows&, const double*, int, int, const int32_t*, bool, bool, const HeadOut&, hipStream_t);
+template <typename T>
+hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
+                               const int32_t* tgt, double scale, hipStream_t s) {
+  hipLaunchKernelGGL(head_dlogits_kernel<T>, dim3(Tp, ceil_div(C, CHUNK)), dim3(NT), 0, s, o, r, lm, ld, T_, C, n0, tgt, scale);
   return hipGetLastError();
 }
+template hipError_t launch_head_dlogits<float>(PairT<float>, const HeadRows&, const float*, const float*, int, int, int, int,
+                                               const int32_t*, double, hipStream_t);
+template hipError_t launch_head_dlogits<bf16_t>(PairT<bf16_t>, const HeadRows&, const float*, const float*, int, int, int, int,
+                                                const int32_t*, double, hipStream_t);
 template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s) {
   hipLaunchKernelGGL(head_copy_kernel<T>, dim3(Tp), dim3(NT), 0, s, o, xm, xd, ldx, T_, dm, tgt);

@@ -225,6 +225,19 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
       for (int k = 0; k < 4; ++k) z[k] += __shfl_xor(z[k], 32, 64);
       if (row >= a.T) continue;
+      if (a.lm) {   // (one piece: kept for its gradient)
+        const int64_t o = (int64_t)row * a.C + c0 + 4 * h;
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int g = 0; g < 4; ++g)
+            if (j * 32 + 8 * g < live) {   // (C is a multiple of 8)
+              *reinterpret_cast<float4*>(a.lm + o + j * 32 + 8 * g) =
+                  make_float4(cm[i][j][4 * g], cm[i][j][4 * g + 1], cm[i][j][4 * g + 2], cm[i][j][4 * g + 3]);
+              *reinterpret_cast<float4*>(a.ld + o + j * 32 + 8 * g) =
+                  make_float4(cd[i][j][4 * g], cd[i][j][4 * g + 1], cd[i][j][4 * g + 2], cd[i][j][4 * g + 3]);
+            }
+      }
       if (h == 0) {
         float* o = a.part + (int64_t)(c0 / WTN) * 5 * a.T + row;
         o[0] = mx;
@@ -326,58 +339,6 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   }
 }
 
-// Joins the tiles' statistics of the rows to those of the pieces before: 256 / R threads per
-// row take every 256 / R-th column group.
-template <int R>
-__global__ __launch_bounds__(256) void head_join_kernel(HeadRows r, const float* part, int groups, int T_, const int32_t* tgt, bool first) {
-  constexpr int L = 256 / R;
-  __shared__ double sh[5][L][R];
-  const int lr = threadIdx.x % R, l = threadIdx.x / R;
-  const int64_t t = (int64_t)blockIdx.x * R + lr;
-  const bool on = t < T_ && tgt[min(t, (int64_t)T_ - 1)] != IGNORE_LABEL;
-  double top = -INFINITY, z[4] = {0.0, 0.0, 0.0, 0.0};
-  auto join = [&](double m, const double (&x)[4]) {
-    const double mx = fmax(top, m);
-    const double f = top == mx || top == -INFINITY ? 1.0 : exp(top - mx);
-    const double g = m == mx || m == -INFINITY ? 1.0 : exp(m - mx);   // (sums at no maximum are NaN or nothing)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) z[k] = z[k] * f + x[k] * g;
-    top = mx;
-  };
-  if (on) {
-    constexpr int U = 4;
-    for (int g0 = l; g0 < groups; g0 += U * L) {
-      float v[U][5];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < 5; ++k) v[u][k] = part[((int64_t)min(g0 + u * L, groups - 1) * 5 + k) * T_ + t];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g0 + u * L < groups) join(v[u][0], {v[u][1], v[u][2], v[u][3], v[u][4]});
-    }
-  }
-  sh[0][l][lr] = top;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
-  __syncthreads();
-  // halves joined until one is left (a fixed order)
-  for (int n = L / 2; n > 0; n /= 2) {
-    if (l < n) {
-      join(sh[0][l + n][lr], {sh[1][l + n][lr], sh[2][l + n][lr], sh[3][l + n][lr], sh[4][l + n][lr]});
-      sh[0][l][lr] = top;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
-    }
-    __syncthreads();
-  }
-  if (l != 0 || !on) return;
-  if (!first) join(r.top[t], {r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]});
-  r.top[t] = (float)top;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) r.z[k][t] = z[k];
-}
-
 template <int BM, int BN, int WM, int WN>
 void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
   const dim3 grid(ceil_div(a.C, BN) * ceil_div(a.T, BM)), block(64 * WM * WN);
@@ -413,12 +374,6 @@ hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad,
   else if (a.tile.BM == 64 && a.tile.BN == 128) launch_tile<64, 128, 2, 4>(a, r, grad, s);
   else if (a.tile.BM == 64) launch_tile<64, 64, 2, 2>(a, r, grad, s);
   else launch_tile<32, 128, 1, 4>(a, r, grad, s);
-  return hipGetLastError();
-}
-
-hipError_t launch_head_join(const HeadRows& r, const float* part, int groups, int T_, const int32_t* tgt, bool first, hipStream_t s) {
-  if (T_ >= 1024) hipLaunchKernelGGL(head_join_kernel<16>, dim3(ceil_div(T_, 16)), dim3(256), 0, s, r, part, groups, T_, tgt, first);
-  else hipLaunchKernelGGL(head_join_kernel<1>, dim3(T_), dim3(256), 0, s, r, part, groups, T_, tgt, first);
   return hipGetLastError();
 }
 

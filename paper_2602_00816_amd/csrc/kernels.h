@@ -318,17 +318,28 @@ struct HeadRows {        // per row of the batch: reference, four sums, target l
 };
 // targets of the rows of a [B, S] batch (IGNORE_LABEL: none)
 hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* lab, int T_, int S, int V, hipStream_t s);
-// fp32 models: joins the logits [T][C] of columns n0 .. n0 + C - 1 to the rows' statistics (first:
-// there are none)
-hipError_t launch_head_stats(const HeadRows& r, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt, bool first,
+// fp32 models: statistics of the logits [T][C] of columns n0 .. n0 + C - 1, part [chunks][5][T] of
+// HEAD_CHUNK columns each, and the target logits of r
+constexpr int HEAD_CHUNK = 4096;
+hipError_t launch_head_stats(const HeadRows& r, double* part, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt,
                              hipStream_t s);
-// losses (float32 pair, or null) and scale times the losses at the two points (fp64 [2][T], or
-// null) from the statistics of all columns, and the factors of the gradients
-hipError_t launch_head_rows(const HeadRows& r, const int32_t* tgt, int T_, int V, double scale, float* loss_m, float* loss_d,
-                            double* rowloss, hipStream_t s);
-// fp32 models: lm, ld [Tp][C] = scale times the gradient of the losses with respect to them
-hipError_t launch_head_dlogits(const HeadRows& r, float* lm, float* ld, int T_, int Tp, int C, int n0, const int32_t* tgt,
-                               double scale, hipStream_t s);
+// what the rows' statistics over the whole vocabulary give: losses (float32 pair, or null), scale
+// times the losses at the two points (fp64 [2][T], or null), the factors of the gradients in r
+struct HeadOut {
+  int V;
+  double scale;
+  float *loss_m, *loss_d;
+  double* rowloss;
+};
+// joins the groups' statistics (part [groups][5][T]) to the rows' (first: there are none; last: nothing
+// comes behind, out is formed)
+template <typename P>
+hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_, const int32_t* tgt, bool first, bool last,
+                            const HeadOut& out, hipStream_t s);
+// o [Tp][C] = scale times the gradient of the losses with respect to the logits lm, ld (o may be they)
+template <typename T>
+hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
+                               const int32_t* tgt, double scale, hipStream_t s);
 // o [Tp][dm] = the rows of x that have a target, zeros elsewhere
 template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
@@ -344,6 +355,7 @@ struct HeadLogits {
   int T, Tp, C, d, n0;
   const int32_t* tgt;      // [T]
   float* part;             // statistics: [groups][5][T] (maximum and four sums), a group of HeadTile::group columns
+  float *lm, *ld;          // statistics: the logits too, [T][C], or null
   bf16_t *gm, *gd;         // gradient: [Tp][C]
   float scale;
   HeadTile tile;           // head_tile
@@ -352,8 +364,6 @@ HeadTile head_tile(int T_, int C);
 // grad: scale times the gradient of the losses, zeros in rows without a target and from T on; else
 // part, and the target logits of r
 hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s);
-// joins the groups' statistics to the rows' (first: there are none)
-hipError_t launch_head_join(const HeadRows& r, const float* part, int groups, int T_, const int32_t* tgt, bool first, hipStream_t s);
 hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const float* d, int T_, int dm, hipStream_t s);
 
 }  // namespace fdh
