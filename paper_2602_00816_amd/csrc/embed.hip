@@ -63,7 +63,7 @@ __global__ __launch_bounds__(NT) void embed_fwd_kernel(PairF x, int64_t ldx, con
 // all blocks and moves its keys there, 64 of a wavefront at a time in their order (the
 // lanes of equal digit found by one ballot per bit).  The table's rows that no token has are
 // zeros: blocks beyond the sort's write a part of the table in each launch, and so hide
-// the sort, which is bound by latency.
+// the sort, which is bound by latency; the rest is written beside the sums.
 constexpr int BITS = 9, BINS = 1 << BITS, SORT_BLOCKS = 64, WAVES = NT / 64;
 
 struct SortArgs {
@@ -173,6 +173,44 @@ __global__ __launch_bounds__(NT) void sort_move_kernel(SortArgs a) {
   }
 }
 
+// Position rows: the sum over the batch's rows, 16 of them in flight; rows S .. are set to zero.
+struct PosArgs {
+  float* hv;       // null: no positions
+  const float* dx;
+  int64_t ld;
+  int B, S, dm, acc;
+  double inv_eps;
+  int64_t n4;      // float4s of the table's rows
+};
+__device__ inline void pos_part(const PosArgs& a, int block, int blocks) {
+  const int n4 = a.dm / 4;
+  for (int64_t i = (int64_t)block * NT + threadIdx.x; i < a.n4; i += (int64_t)blocks * NT) {
+    const int64_t r = i / n4;
+    const int c = 4 * (int)(i - r * n4);
+    if (r >= a.S) {
+      put4(a.hv, 4 * i, 0.f, 0.f, 0.f, 0.f);
+      continue;
+    }
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    constexpr int U = 16;
+    for (int b0 = 0; b0 < a.B; b0 += U) {
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = row4(a.dx, ((int64_t)min(b0 + u, a.B - 1) * a.S + r) * a.ld + c);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (b0 + u < a.B) { s[0] += (double)x[u].x; s[1] += (double)x[u].y; s[2] += (double)x[u].z; s[3] += (double)x[u].w; }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] *= a.inv_eps;
+    if (a.acc) {
+      const float4 h = row4(a.hv, 4 * i);
+      s[0] += h.x; s[1] += h.y; s[2] += h.z; s[3] += h.w;
+    }
+    put4(a.hv, 4 * i, (float)s[0], (float)s[1], (float)s[2], (float)s[3]);
+  }
+}
+
 // ---- sums of the sorted rows -----------------------------------------------------------
 // A wavefront takes R consecutive sorted rows at 256 columns (four a lane), 16 rows in flight.
 // A token whose rows all lie in the chunk gets its sum at once.  One whose rows go beyond
@@ -190,7 +228,31 @@ struct SumArgs {
   double mul;      // scale / eps
   int acc;
   double* part;
+  int64_t chunks;  // chunks of R rows
+  int64_t blocks;  // workgroups that add; then pblocks that add positions (the same rows again, from the
+  int pblocks;     // caches), then those that set rows zfrom .. V - 1 that no token has to zero
+  int zfrom;
+  PosArgs posn;
 };
+
+// ZROWS rows per wavefront: whether a token has them is looked up in the sorted keys (a lane each)
+constexpr int ZROWS = 8;
+__device__ inline void zero_rows(const SumArgs& a, int64_t block) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r0 = a.zfrom + (block * WAVES + (threadIdx.x >> 6)) * ZROWS;
+  const uint32_t r = (uint32_t)min(r0 + lane % ZROWS, (int64_t)a.V - 1);
+  int64_t lo = 0, hi = a.T;   // first sorted position of a key >= r
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (a.key[mid] < r) lo = mid + 1;
+    else hi = mid;
+  }
+  const uint64_t there = __ballot(lo < a.T && a.key[min(lo, a.T - 1)] == r);
+  for (int i = 0; i < ZROWS; ++i) {
+    if (r0 + i >= a.V || (there >> i & 1)) continue;
+    for (int c = 4 * lane; c < a.dm; c += 256) put4(a.hv, (r0 + i) * a.dm + c, 0.f, 0.f, 0.f, 0.f);
+  }
+}
 
 __device__ inline void put_sum(const SumArgs& a, uint32_t tk, int c, const double (&s)[4]) {
   const int64_t o = (int64_t)tk * a.dm + c;
@@ -208,11 +270,17 @@ template <int R>
 __global__ __launch_bounds__(NT) void embed_sum_kernel(SumArgs a) {
   static_assert(R <= 64, "a lane for every row of a chunk");
   constexpr int U = 16;
-  const int64_t chunk = blockIdx.x, s0 = chunk * R;
+  if (blockIdx.x >= a.blocks) {
+    const int64_t b = blockIdx.x - a.blocks;
+    if (b < a.pblocks) pos_part(a.posn, (int)b, a.pblocks);
+    else zero_rows(a, b - a.pblocks);
+    return;
+  }
+  const int64_t chunk = blockIdx.x % a.chunks, s0 = chunk * R;
   const int n = (int)min((int64_t)R, a.T - s0);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c0 = ((int)blockIdx.y * WAVES + wave) * 256;
+  const int c0 = ((int)(blockIdx.x / a.chunks) * WAVES + wave) * 256;
   if (c0 >= a.dm) return;
   const int c = c0 + 4 * lane;
   const bool on = c < a.dm;
@@ -264,18 +332,21 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
   __shared__ double sh[WAVES][256];
   const int64_t chunk = blockIdx.x, s0 = chunk * R, s1 = s0 + R;
   if (s1 >= a.T) return;
-  const uint32_t tk = a.key[s1 - 1];
-  if (a.key[s1] != tk || tk >= (uint32_t)a.V) return;
-  if (s0 > 0 && a.key[s0] == tk && a.key[s0 - 1] == tk) return;   // it began before
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (all keys at once: each wait is some 1.5 us of the kernel's 5)
+  const uint32_t before = a.key[s0 > 0 ? s0 - 1 : 0], head = a.key[s0], tk = a.key[s1 - 1];
+  auto at = [&](int64_t m) { return a.key[min((chunk + 1 + m + lane) * R, a.T - 1)]; };
+  uint32_t after = at(0);
+  if ((uint32_t)__builtin_amdgcn_readfirstlane((int)after) != tk || tk >= (uint32_t)a.V) return;
+  if (s0 > 0 && head == tk && before == tk) return;   // it began before
   // chunks after this one whose first row is of this token
   int64_t m = 0;
   for (;;) {
-    const int64_t r = (chunk + 1 + m + lane) * R;
-    const uint64_t hit = __ballot(r < a.T && a.key[min(r, a.T - 1)] == tk);
+    const uint64_t hit = __ballot((chunk + 1 + m + lane) * R < a.T && after == tk);
     const int k = ~hit ? __ffsll((unsigned long long)~hit) - 1 : 64;
     m += k;
     if (k < 64) break;
+    after = at(m);
   }
   const int c = (int)blockIdx.y * 256 + 4 * lane;
   const bool on = c < a.dm;
@@ -283,7 +354,8 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
   const int64_t per = (m + WAVES - 1) / WAVES, lo = wave * per, hi = min(lo + per, m);
   double s[4] = {0.0, 0.0, 0.0, 0.0};
   const double* base = a.part + 2 * (chunk + 1) * a.dm + col;
-  constexpr int U = 8;
+  const double2 own0 = *reinterpret_cast<const double2*>(base - a.dm), own1 = *reinterpret_cast<const double2*>(base - a.dm + 2);
+  constexpr int U = 16;
   for (int64_t q = lo; q < hi; q += U) {
     double2 x[U], y[U];
 #pragma unroll
@@ -300,7 +372,7 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
   for (int e = 0; e < 4; ++e) sh[wave][4 * lane + e] = s[e];
   __syncthreads();
   if (wave != 0 || !on) return;
-  const double* own = a.part + (2 * chunk + 1) * a.dm + c;
+  const double own[4] = {own0.x, own0.y, own1.x, own1.y};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     s[e] = own[e];
@@ -308,39 +380,6 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
     for (int q = 0; q < WAVES; ++q) s[e] += sh[q][4 * lane + e];
   }
   put_sum(a, tk, c, s);
-}
-
-// Position rows: the sum over the batch's rows, four columns a thread and eight rows in
-// flight; rows S .. rows - 1 of the table are set to zero (left alone with acc).
-__global__ __launch_bounds__(NT) void pos_bwd_kernel(float* hv, const float* dx, int64_t ld, int B, int S, int dm, double inv_eps,
-                                                     int64_t rows, int acc) {
-  const int n4 = dm / 4;
-  const int64_t n = rows * n4;
-  for (int64_t i = blockIdx.x * (int64_t)NT + threadIdx.x; i < n; i += (int64_t)gridDim.x * NT) {
-    const int64_t r = i / n4;
-    const int c = 4 * (int)(i - r * n4);
-    if (r >= S) {
-      put4(hv, r * dm + c, 0.f, 0.f, 0.f, 0.f);
-      continue;
-    }
-    double s[4] = {0.0, 0.0, 0.0, 0.0};
-    constexpr int U = 8;
-    for (int b0 = 0; b0 < B; b0 += U) {
-      float4 x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = row4(dx, ((int64_t)min(b0 + u, B - 1) * S + r) * ld + c);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (b0 + u < B) { s[0] += (double)x[u].x; s[1] += (double)x[u].y; s[2] += (double)x[u].z; s[3] += (double)x[u].w; }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] *= inv_eps;
-    if (acc) {
-      const float4 h = row4(hv, r * dm + c);
-      s[0] += h.x; s[1] += h.y; s[2] += h.z; s[3] += h.w;
-    }
-    put4(hv, r * dm + c, (float)s[0], (float)s[1], (float)s[2], (float)s[3]);
-  }
 }
 
 // rows per chunk of the sums
@@ -385,12 +424,14 @@ template hipError_t launch_embed_fwd<bf16_t>(PairF, int64_t, const int32_t*, int
 
 size_t embed_scratch_bytes(int64_t T_, int dm) { return embed_carve(T_, dm).total; }
 
-hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, int64_t ld, int64_t T_, int dm, int V, double mul,
-                            bool acc, void* scratch, hipStream_t s) {
+hipError_t launch_embed_bwd(const EmbedGrad& o, const int32_t* tok, const float* dxd, int64_t ld, int B, int S, int dm, int V,
+                            void* scratch, hipStream_t s) {
+  const int64_t T_ = (int64_t)B * S;
+  const bool acc = o.acc;
   const int64_t zero4 = acc ? 0 : (int64_t)V * dm / 4;
   if (T_ == 0) {
-    if (acc) return hipSuccess;
-    return launch_fill_f32(hv_e, (int64_t)V * dm, 0.f, s);
+    const hipError_t r = acc ? hipSuccess : launch_fill_f32(o.e, (int64_t)V * dm, 0.f, s);
+    return r != hipSuccess || !o.p || o.acc_p ? r : launch_fill_f32(o.p, o.rows * dm, 0.f, s);
   }
   char* ws = (char*)scratch;
   const EmbedScratch sc = embed_carve(T_, dm);
@@ -401,22 +442,24 @@ hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, i
   a.per = (int64_t)ceil_div(T_, (int64_t)a.blocks * NT) * NT;
   a.blocks = (int)ceil_div(T_, a.per);
   a.count = (uint32_t*)(ws + sc.count);
-  a.zero = hv_e;
+  a.zero = o.e;
   a.zero4 = zero4;
   const int passes = V + 1 > BINS ? 2 : 1;
-  a.zpart = (zero4 + 2 * passes - 1) / (2 * passes);
-  const int zblocks = (int)std::min<int64_t>(1024, ceil_div(a.zpart, NT));
-  for (int p = 0; p < passes; ++p) {
-    a.tok = p == 0 ? tok : nullptr;
+  // an eighth of the table in each launch, in whole rows (8192 tokens, 32000 x 2048: about as long as
+  // the sort takes)
+  const int64_t zrows = zero4 ? V / 8 : 0;
+  a.zpart = zrows * (dm / 4);
+  const int zblocks = (int)std::min<int64_t>(512, ceil_div(a.zpart, NT));
+  for (int p = 0; p < 2 * passes; ++p) {
+    a.tok = p < 2 ? tok : nullptr;
     a.key = (const uint32_t*)(ws + sc.key[0]);
     a.pos = (const uint32_t*)(ws + sc.pos[0]);
-    a.okey = (uint32_t*)(ws + sc.key[p]);
-    a.opos = (uint32_t*)(ws + sc.pos[p]);
-    a.shift = p * BITS;
-    a.zfrom = 2 * p * a.zpart;
-    hipLaunchKernelGGL(sort_count_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
-    a.zfrom += a.zpart;
-    hipLaunchKernelGGL(sort_move_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
+    a.okey = (uint32_t*)(ws + sc.key[p / 2]);
+    a.opos = (uint32_t*)(ws + sc.pos[p / 2]);
+    a.shift = p / 2 * BITS;
+    a.zfrom = p * a.zpart;
+    if (p % 2 == 0) hipLaunchKernelGGL(sort_count_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
+    else hipLaunchKernelGGL(sort_move_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
   }
   SumArgs u{};
   u.key = a.okey;
@@ -426,13 +469,19 @@ hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, i
   u.T = T_;
   u.dm = dm;
   u.V = V;
-  u.hv = hv_e;
-  u.mul = mul;
+  u.hv = o.e;
+  u.mul = o.mul;
   u.acc = acc;
   u.part = (double*)(ws + sc.part);
   const int R = chunk_rows(T_);
   const unsigned chunks = ceil_div(T_, R), cols = ceil_div(dm, 256);
-  const dim3 gs(chunks, ceil_div(cols, WAVES)), gj(chunks, cols);
+  u.chunks = chunks;
+  u.blocks = (int64_t)chunks * ceil_div(cols, WAVES);
+  u.zfrom = (int)(2 * passes * zrows);
+  const int64_t pos4 = o.p ? (o.acc_p ? std::min<int64_t>(o.rows, S) : o.rows) * (dm / 4) : 0;
+  u.posn = PosArgs{o.p, dxd, ld, B, S, dm, o.acc_p, o.inv_eps, pos4};
+  u.pblocks = (int)std::min<int64_t>(65536, ceil_div(pos4, NT));
+  const dim3 gs((unsigned)(u.blocks + u.pblocks + (zero4 ? ceil_div(V - u.zfrom, ZROWS * WAVES) : 0))), gj(chunks, cols);
   if (R == 32) {
     hipLaunchKernelGGL(embed_sum_kernel<32>, gs, dim3(NT), 0, s, u);
     if (chunks > 1) hipLaunchKernelGGL(embed_join_kernel<32>, gj, dim3(NT), 0, s, u);
@@ -440,15 +489,6 @@ hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, i
     hipLaunchKernelGGL(embed_sum_kernel<64>, gs, dim3(NT), 0, s, u);
     hipLaunchKernelGGL(embed_join_kernel<64>, gj, dim3(NT), 0, s, u);
   }
-  return hipGetLastError();
-}
-
-hipError_t launch_pos_bwd(float* hv_p, const float* dxd, int64_t ld, int B, int S, int dm, double inv_eps, int64_t rows, bool acc,
-                          hipStream_t s) {
-  const int64_t live = acc ? std::min<int64_t>(rows, S) : rows;
-  if (live == 0 || (acc && B == 0)) return hipSuccess;
-  hipLaunchKernelGGL(pos_bwd_kernel, dim3((unsigned)std::min<int64_t>(65536, ceil_div(live * (dm / 4), NT))), dim3(NT), 0, s, hv_p, dxd,
-                     ld, B, S, dm, inv_eps, live, acc);
   return hipGetLastError();
 }
 

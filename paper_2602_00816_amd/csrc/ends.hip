@@ -81,8 +81,7 @@ int Engine::embed_backward(const int32_t* tok, int B, int S, const float* dx_d, 
   const Region o[3] = {flat(hv_e, (int64_t)V * d * 4), flat(hv_p, (int64_t)Smax * d * 4), need ? flat(scratch, (int64_t)need) : none};
   const Region r[2] = {T_ > 0 ? Region{(const char*)dx_d, T_, lddx * 4, (int64_t)d * 4} : none, flat(tok, 4 * T_)};
   if (any_overlap(o, 3, r, 2)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }
-  CK(launch_embed_bwd(hv_e, tok, dx_d, lddx, T_, d, V, embed_scale / eps, acc, scratch, stream));
-  if (gpt2) CK(launch_pos_bwd(hv_p, dx_d, lddx, B, S, d, 1.0 / eps, Smax, acc, stream));
+  CK(launch_embed_bwd(EmbedGrad{hv_e, hv_p, embed_scale / eps, 1.0 / eps, Smax, acc, acc}, tok, dx_d, lddx, B, S, d, V, scratch, stream));
   return FDH_OK;
 }
 

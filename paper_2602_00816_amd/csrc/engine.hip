@@ -1100,8 +1100,8 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
   }
   // embeddings (difference channel of the gradient w.r.t. the embedding output)
   // (GPT-2 ties the embedding to the head, whose gradient is already in hv)
-  CK(launch_embed_bwd(hv + wte.off, tok, dxd, d, T_, d, V, embed_scale / eps, gpt2 || acc, ws + emb.off, st));
-  if (gpt2) CK(launch_pos_bwd(hv + wpe.off, dxd, d, B, S, d, 1.0 / eps, Smax, acc, st));
+  CK(launch_embed_bwd(EmbedGrad{hv + wte.off, gpt2 ? hv + wpe.off : nullptr, embed_scale / eps, 1.0 / eps, Smax, gpt2 || acc, acc},
+                      tok, dxd, d, B, S, d, V, ws + emb.off, st));
   (void)dxm;
   return FDH_OK;
 #undef RC

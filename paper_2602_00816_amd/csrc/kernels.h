@@ -299,14 +299,18 @@ template <typename T>
 hipError_t launch_embed_fwd(PairF x, int64_t ldx, const int32_t* tok, int64_t T_, int S, int dm, int V, const EmbedTables& w,
                             int* bad_tok, hipStream_t s);
 size_t embed_scratch_bytes(int64_t T_, int dm);
-// hv_e[r] = mul * sum over positions t of token r of dxd[t] (zeros for the others), or with
-// acc added to the rows of the batch's tokens.  scratch: embed_scratch_bytes, 16-byte aligned
-hipError_t launch_embed_bwd(float* hv_e, const int32_t* tok, const float* dxd, int64_t ld, int64_t T_, int dm, int V, double mul,
-                            bool acc, void* scratch, hipStream_t s);
-// hv_p[s] = inv_eps * sum_b dxd[b S + s] for s < S and 0 for S <= s < rows, or with acc
-// added to the first min(S, rows) rows
-hipError_t launch_pos_bwd(float* hv_p, const float* dxd, int64_t ld, int B, int S, int dm, double inv_eps, int64_t rows, bool acc,
-                          hipStream_t s);
+// e[r] = mul * sum over positions t of token r of dxd[t] (zeros for the others) and, where p is not
+// null, p[s] = inv_eps * sum_b dxd[b S + s] for s < S and 0 for S <= s < rows, or with acc and acc_p
+// added to the rows of the batch's tokens and to the first min(S, rows) of p.  scratch: embed_scratch_bytes, 16-byte
+// aligned
+struct EmbedGrad {
+  float *e, *p;
+  double mul, inv_eps;
+  int64_t rows;
+  bool acc, acc_p;
+};
+hipError_t launch_embed_bwd(const EmbedGrad& o, const int32_t* tok, const float* dxd, int64_t ld, int B, int S, int dm, int V,
+                            void* scratch, hipStream_t s);
 
 // ---- head.hip: the loss over the vocabulary, a piece of it at a time ------------------
 constexpr int HEAD_MAX_ROWS = 1 << 20, HEAD_MAX_WIDTH = 1 << 16, HEAD_MAX_LD = 1 << 20;
