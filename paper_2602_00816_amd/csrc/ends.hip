@@ -210,7 +210,7 @@ size_t Engine::head_scratch_most(size_t tokens, int piece) const {
 
 template <typename T>
 int Engine::head_run(const HeadCall& c) {
-  const HeadCarve k = head_carve(c.T, c.piece, c.grads);
+  const HeadCarve& k = c.carve;
   hipStream_t st = stream;
   char* ws = c.scratch;
   const int T_ = c.T;
@@ -360,14 +360,14 @@ int Engine::head_check(const fdh_head_inputs* in, bool grads, size_t scratch_byt
     }
     if (bad_rows(in->w_m, d, d, ob) || bad_rows(in->w_d, d, d, ob)) { err = "w: null or not 16-byte aligned"; return FDH_ERR_INVALID_ARG; }
     if (!in->targets || (uintptr_t)in->targets % 4) { err = "targets: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
-    const size_t need = head_carve(in->T, in->piece, grads).total;
-    if (!scratch || scratch_bytes < need) { err = "scratch smaller than fdh_head_scratch_bytes"; return FDH_ERR_WORKSPACE; }
+    c->carve = head_carve(in->T, in->piece, grads);
+    if (!scratch || scratch_bytes < c->carve.total) { err = "scratch smaller than fdh_head_scratch_bytes"; return FDH_ERR_WORKSPACE; }
     if ((uintptr_t)scratch % 256) { err = "scratch must be 256-byte aligned"; return FDH_ERR_WORKSPACE; }
   }
   c->x_m = in->x_m; c->x_d = in->x_d; c->ldx = in->ldx;
   c->w_m = in->w_m; c->w_d = in->w_d;
   c->tgt = in->targets;
-  c->T = in->T; c->piece = in->piece;
+  c->T = in->T;
   c->scratch = (char*)scratch;
   return FDH_OK;
 }
@@ -379,7 +379,7 @@ int Engine::head_loss(const fdh_head_inputs* in, float* loss_m, float* loss_d, v
   if (c.T == 0) return FDH_OK;
   if (!loss_m || !loss_d || (uintptr_t)loss_m % 4 || (uintptr_t)loss_d % 4) { err = "loss: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
   const int64_t ob = bf16 ? 2 : 4, T_ = c.T, wd = (int64_t)d * ob;
-  const Region o[3] = {flat(loss_m, 4 * T_), flat(loss_d, 4 * T_), flat(scratch, (int64_t)head_carve(c.T, c.piece, false).total)};
+  const Region o[3] = {flat(loss_m, 4 * T_), flat(loss_d, 4 * T_), flat(scratch, (int64_t)c.carve.total)};
   const Region r[5] = {{(const char*)c.x_m, T_, c.ldx * ob, wd}, {(const char*)c.x_d, T_, c.ldx * ob, wd}, flat(c.w_m, V * wd),
                        flat(c.w_d, V * wd), flat(c.tgt, 4 * T_)};
   if (any_overlap(o, 3, r, 5)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }
@@ -415,7 +415,7 @@ int Engine::head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, c
   }
   const Region o[6] = {flat(loss_m, 4 * T_), flat(loss_d, 4 * T_), {(const char*)g->dx_m, T_, g->lddx * gb, gw},
                        {(const char*)g->dx_d, T_, g->lddx * gb, gw}, flat(g->dw, V * gw),
-                       flat(scratch, (int64_t)head_carve(c.T, c.piece, true).total)};
+                       flat(scratch, (int64_t)c.carve.total)};
   const Region r[5] = {{(const char*)c.x_m, T_, c.ldx * ob, wd}, {(const char*)c.x_d, T_, c.ldx * ob, wd}, flat(c.w_m, V * wd),
                        flat(c.w_d, V * wd), flat(c.tgt, 4 * T_)};
   if (any_overlap(o, 6, r, 5)) { err = "an output or the scratch overlaps an input or another output"; return FDH_ERR_INVALID_ARG; }

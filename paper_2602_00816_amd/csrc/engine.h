@@ -94,13 +94,19 @@ struct WsLayout {
   size_t total = 0;     // bytes the carve needs
 };
 
-// The loss over the vocabulary in pieces (ends.hip): one call, and the carve of its scratch.
+// The loss over the vocabulary in pieces (ends.hip): the carve of its scratch, and one call.
+struct HeadCarve {
+  int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
+  bool keep = false;           // one piece, whose logits are formed once
+  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
+};
 struct HeadCall {
   const void *x_m = nullptr, *x_d = nullptr;   // [T][ldx], operand type
   int64_t ldx = 0;
   const void *w_m = nullptr, *w_d = nullptr;   // [V][d], operand type
   const int32_t* tgt = nullptr;                // [T]
-  int T = 0, piece = 0;                        // columns per piece (0: chosen)
+  int T = 0;
+  HeadCarve carve;                             // head_carve of T, the piece and grads
   float *loss_m = nullptr, *loss_d = nullptr;  // [T] or null
   double* rowloss = nullptr;                   // scale times the losses at the two points, [2][T], or null
   double scale = 1.0;
@@ -113,12 +119,6 @@ struct HeadCall {
   bool copy_x = true;                          // rows without a target may hold anything
   char* scratch = nullptr;
 };
-struct HeadCarve {
-  int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
-  bool keep = false;           // one piece, whose logits are formed once
-  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
-};
-
 double gemm_flops(const GemmArgs& g);   // executed by a product, causal tails clipped
 
 class Engine : public WsLayout {

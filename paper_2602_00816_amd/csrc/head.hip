@@ -8,11 +8,14 @@
 // and the logits' gradient is w (P.m - [j = y]) and w P.d with the rows' weight w.  Where the two
 // points are far apart (|ld| >= 1/2) a - s would lose bits: there p = a + s and q = a - s are formed
 // instead, their sums kept apart (Z+ = Sa + Ss + Sp, Z- = Sa - Ss + Sq) and P+- = p / Z+, q / Z-.
+// Which of the two a logit takes may differ between the passes: only the sums' totals are used.
 // A first pass over the pieces leaves c, the four sums and the target's logits of every row, a
 // second one forms the logits again and gives their gradient to the products: nothing of the
 // size of the logits stays.  Where one piece holds the vocabulary its logits are formed once.
 #include "head_dev.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace fdh {
 
@@ -53,19 +56,24 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, double* part
       for (int k = 0; k < 4; ++k) z[k] *= f;
       mt = top;
     }
-    auto add = [&](float x, float y) {
-      double p, s;
-      pair_exp(x, y, mt, p, s);
-      const bool apart = far_apart(y);
-      z[0] += apart ? 0.0 : p;
-      z[1] += apart ? 0.0 : s;
-      z[2] += apart ? p : 0.0;
-      z[3] += apart ? s : 0.0;
-    };
-    add(a.x, b.x);
-    add(a.y, b.y);
-    add(a.z, b.z);
-    add(a.w, b.w);
+    const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    float sa = 0.f, ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (far_apart_fine(x[e], y[e], mt)) {
+        double p, q;
+        pair_exp_far(x[e], y[e], mt, p, q);
+        z[2] += p;
+        z[3] += q;
+      } else {
+        float p, s;
+        pair_exp<true>(x[e], y[e], mt, p, s);
+        sa += p;
+        ss += s;
+      }
+    }
+    z[0] += sa;
+    z[1] += ss;
   }
   const float mx = (float)block_max<NT>((double)mt, sh);
   // (a thread that saw NaN alone has no maximum: its sums are NaN at any factor but none)
@@ -173,8 +181,6 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
 // Gradient of logits that are in memory (one piece holds the vocabulary, or an fp32 model) in the
 // operand type, [Tp][C]; rows without a target and rows behind the last are zeros.  o may be the
 // logits (fp32 models).
-template <typename T> struct Stat { typedef double type; };
-template <> struct Stat<bf16_t> { typedef float type; };
 __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
   auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16); };
@@ -183,7 +189,8 @@ __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
 template <typename T>
 __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r, const float* lm, const float* ld, int T_, int C, int n0,
                                                           const int32_t* tgt, double scale) {
-  typedef typename Stat<T>::type F;
+  constexpr bool fine = sizeof(T) == 4;
+  typedef std::conditional_t<fine, double, float> F;   // of points far apart
   const int64_t t = blockIdx.x;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
   const int64_t base = t * C;
@@ -196,19 +203,26 @@ __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r
     return;
   }
   const float c = r.top[t];
-  const F f0 = (F)r.f[0][t], f1 = (F)r.f[1][t], f2 = (F)r.f[2][t], f3 = (F)r.f[3][t];
+  const float f0 = (float)r.f[0][t], f1 = (float)r.f[1][t], w = (float)scale;
+  const F f2 = (F)r.f[2][t], f3 = (F)r.f[3][t];
   for (int j = from + 4 * threadIdx.x; j < end; j += 4 * NT) {
     const float4 a4 = *reinterpret_cast<const float4*>(lm + base + j), b4 = *reinterpret_cast<const float4*>(ld + base + j);
     const float a[4] = {a4.x, a4.y, a4.z, a4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
     float gm[4], gd[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      F p, s;
-      pair_exp(a[e], b[e], c, p, s);
-      const bool apart = far_apart(b[e]);
-      const F m = apart ? p * f2 + s * f3 : p * f0 - s * f1;
-      gm[e] = (float)(m - (n0 + j + e == y ? (F)scale : F(0)));
-      gd[e] = (float)(apart ? p * f2 - s * f3 : s * f0 - p * f1);
+      if (fine ? far_apart_fine(a[e], b[e], c) : far_apart(b[e])) {
+        F p, q;
+        pair_exp_far(a[e], b[e], c, p, q);
+        gm[e] = (float)(p * f2 + q * f3);
+        gd[e] = (float)(p * f2 - q * f3);
+      } else {
+        float p, s;
+        pair_exp<fine>(a[e], b[e], c, p, s);
+        gm[e] = p * f0 - s * f1;
+        gd[e] = s * f0 - p * f1;
+      }
+      if (n0 + j + e == y) gm[e] -= w;
     }
     store4(o.m + base + j, gm[0], gm[1], gm[2], gm[3]);
     store4(o.d + base + j, gd[0], gd[1], gd[2], gd[3]);

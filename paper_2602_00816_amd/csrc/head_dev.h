@@ -10,40 +10,42 @@ constexpr float FAR_APART = 0.5f;      // from this |ld| on: p and q in the plac
 
 __device__ inline float head_ref(float lm, float ld) { return lm + fabsf(ld); }
 __device__ inline bool far_apart(float ld) { return !(fabsf(ld) < FAR_APART); }
+// fp32 models also take logits far below the reference in fp64: in a row whose two points are far
+// apart they may be all that one of them has
+__device__ inline bool far_apart_fine(float lm, float ld, float c) { return far_apart(ld) || lm - c < -60.f; }
 
-// a and s (or p and q) of one logit, see head.hip.  bf16 models: fp32 (the exponential is common to
-// both points); fp32 models: fp64.  The series' first omitted terms are below 1e-10 (|ld| < 1/16)
-// and 1e-8 (1/2) of the sum, in fp64 2^-40 / 10!.
-__device__ inline void pair_exp_near(float lm, float ld, float c, float& a, float& s) {
-  const float e = __expf(lm - c), b2 = ld * ld;
+// e^x, x >= -60, within two steps of fp32 (__expf is off by as many as |x| holds): the rounding of
+// x log2 e, and what log2 e lacks in fp32, put back to first order.
+__device__ inline float exp_fine(float x) {
+  const float hi = 1.4426950216f, lo = 1.9259630e-8f, p = x * hi;
+  const float r = fmaf(x, lo, fmaf(x, hi, -p)), e = __builtin_amdgcn_exp2f(p);
+  return fmaf(e, r * 0.69314718f, e);
+}
+
+// a and s of one logit, see head.hip; for |ld| < 1/2.  In fp32: the exponential is common to both
+// points, to the rounding of an fp32 model with FINE.  The series' first omitted terms are below
+// 1e-10 (|ld| < 1/16) and 1e-8 of the sum.
+template <bool FINE>
+__device__ inline void pair_exp_near(float lm, float ld, float c, float& a, float& s) {   // |ld| < 1/16
+  const float e = FINE ? exp_fine(lm - c) : __expf(lm - c), b2 = ld * ld;
   a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24)));
   s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120)));
 }
+template <bool FINE>
 __device__ inline void pair_exp(float lm, float ld, float c, float& a, float& s) {
-  const float x = lm - c, b = fabsf(ld);
-  if (b < HEAD_NEAR) {
-    pair_exp_near(lm, ld, c, a, s);
-  } else if (b < FAR_APART) {
-    const float e = __expf(x), b2 = ld * ld;
-    a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24 + b2 * (1.f / 720 + b2 * (1.f / 40320)))));
-    s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120 + b2 * (1.f / 5040))));
-  } else {
-    a = __expf(x + ld);
-    s = __expf(x - ld);
-  }
+  const float e = FINE ? exp_fine(lm - c) : __expf(lm - c), b2 = ld * ld;
+  a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24 + b2 * (1.f / 720 + b2 * (1.f / 40320)))));
+  s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120 + b2 * (1.f / 5040))));
 }
-__device__ inline void pair_exp(float lm, float ld, float c, double& a, double& s) {
-  const double x = (double)lm - (double)c, b = ld;
-  if (fabs(b) < HEAD_NEAR) {
-    const double e = exp(x), b2 = b * b;
-    a = e * (1.0 + b2 * (1.0 / 2 + b2 * (1.0 / 24 + b2 * (1.0 / 720 + b2 * (1.0 / 40320)))));
-    s = e * b * (1.0 + b2 * (1.0 / 6 + b2 * (1.0 / 120 + b2 * (1.0 / 5040 + b2 * (1.0 / 362880)))));
-  } else {
-    const double p = exp(x + b), q = exp(x - b);
-    const bool far = far_apart(ld);
-    a = far ? p : 0.5 * (p + q);
-    s = far ? q : 0.5 * (p - q);
-  }
+// p and q of one logit: fp32 (bf16 models) or fp64
+__device__ inline void pair_exp_far(float lm, float ld, float c, float& p, float& q) {
+  p = __expf(lm - c + ld);
+  q = __expf(lm - c - ld);
+}
+__device__ inline void pair_exp_far(float lm, float ld, float c, double& p, double& q) {
+  const double x = (double)lm - (double)c;
+  p = exp(x + (double)ld);
+  q = exp(x - (double)ld);
 }
 
 }  // namespace

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
             float p, s;
-            pair_exp_near(cm[i][j][e], cd[i][j][e], mx, p, s);
+            pair_exp_near<false>(cm[i][j][e], cd[i][j][e], mx, p, s);
             z[0] += p;
             z[1] += s;
           }
@@ -214,8 +214,9 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
             float p, s;
-            pair_exp(cm[i][j][e], cd[i][j][e], mx, p, s);
             const bool apart = far_apart(cd[i][j][e]);
+            if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], mx, p, s);
+            else pair_exp<false>(cm[i][j][e], cd[i][j][e], mx, p, s);
             z[0] += apart ? 0.f : p;
             z[1] += apart ? 0.f : s;
             z[2] += apart ? p : 0.f;
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
             float p, s;
-            pair_exp_near(cm[i][j][e], cd[i][j][e], top, p, s);
+            pair_exp_near<false>(cm[i][j][e], cd[i][j][e], top, p, s);
             cm[i][j][e] = p * w0 - s * w1;
             cd[i][j][e] = s * w0 - p * w1;
           }
@@ -299,7 +300,8 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
           for (int e = 0; e < 16; ++e) {
             float p, s;
             const bool apart = far_apart(cd[i][j][e]);
-            pair_exp(cm[i][j][e], cd[i][j][e], top, p, s);
+            if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], top, p, s);
+            else pair_exp<false>(cm[i][j][e], cd[i][j][e], top, p, s);
             cm[i][j][e] = apart ? p * w2 + s * w3 : p * w0 - s * w1;
             cd[i][j][e] = apart ? p * w2 - s * w3 : s * w0 - p * w1;
           }
