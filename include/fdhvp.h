@@ -168,7 +168,7 @@ typedef struct fdh_head_grads {
   void *dx_m, *dx_d;        /* [T] rows of d_model elements, lddx apart: the gradient of x, a pair */
   int64_t lddx;
   void* dw;                 /* [vocab][d_model]: the half difference of the gradient of w over eps (Hv's entries) */
-  double scale;             /* weight of every row's loss, e.g. 1 / targets; finite */
+  double scale;             /* weight of every row's loss, e.g. 1 / targets; it and scale / eps finite in float32 */
   double eps;               /* positive, finite */
   int32_t dtype;            /* of dx and dw: FDH_F32 or the context's dtype */
   int32_t accumulate;       /* != 0: dw is added to what is there (FDH_F32) */
@@ -361,10 +361,10 @@ fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, siz
  *   loss[t] = log sum_j e^(l_tj) - l_ty as a float32 pair: _m the mean, _d the half difference of
  *   its values at the two points, not scaled; 0 for a row without a target.
  * fdh_head_grad also gives the gradients of scale * sum_t loss[t] (the loss pointers may be
- * NULL).  It forms the logits twice (once where one piece holds the vocabulary: of up to 2^26
- * logits that is chosen) and rounds their gradient to the context's dtype, as the HVP's products do; sums and statistics are
- * fp32 or wider, the order of the additions is fixed (the same bits in every call).  The
- * logits' mean leaves out x_d w_d^T, of second order in the step, as the HVP does.
+ * NULL).  It forms the logits twice (once where one piece holds the vocabulary, which is chosen for
+ * up to 2^26 logits, and for up to 8 rows) and rounds their gradient to the context's dtype, as the
+ * HVP's products do (not for up to 8 rows); sums and statistics are fp32 or wider, the order of the
+ * additions is fixed (the same bits in every call).  The logits' mean may leave out x_d w_d^T, of second order in the step, as the HVP does.
  * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude.
  * Rows without a target may hold anything (NaN among it): their dx is 0 and they take no
  * part in dw.  A target outside [0, vocab) other than -100, or a NaN in its row, makes the row's

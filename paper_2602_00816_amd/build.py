@@ -22,8 +22,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(os.path.dirname(HERE), "include")]
 
-SOURCES = ["gemm.hip", "gemm_f32.hip", "gemm_split.hip", "attn.hip", "rng.hip", "vec.hip", "lm.hip", "qk.hip", "embed.hip", "head.hip", "head_gemm.hip", "engine.hip", "ends.hip",
-           "capi.hip"]
+SOURCES = ["gemm.hip", "gemm_f32.hip", "gemm_split.hip", "attn.hip", "rng.hip", "vec.hip", "lm.hip", "qk.hip", "embed.hip",
+           "head.hip", "head_gemm.hip", "head_thin.hip", "engine.hip", "ends.hip", "capi.hip"]
 # The fused attention kernels keep their MFMA accumulators in VGPRs: with the
 # default AGPR form the allocator moves the output accumulators through VGPRs
 # around every score product.

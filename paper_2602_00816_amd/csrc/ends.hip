@@ -145,7 +145,8 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   };
   const size_t ob = bf16 ? 2 : 4, t = (size_t)T_;
   c.Tp = (int)((t + 7) / 8 * 8);
-  const bool whole = piece > 0 ? piece >= V : (int64_t)T_ * V <= HEAD_PIECE_ELEMS;
+  c.thin = grads && T_ <= HEAD_THIN;   // (no more logits than w has rows 8 wide)
+  const bool whole = c.thin || (piece > 0 ? piece >= V : (int64_t)T_ * V <= HEAD_PIECE_ELEMS);
   int64_t C = piece > 0 ? piece : std::max<int64_t>(HEAD_PIECE_MIN, HEAD_PIECE_ELEMS / std::max(1, T_) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND);
   C = (C + HEAD_PIECE_ROUND - 1) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND;
   c.C = (int)(whole ? V : std::min<int64_t>(C, V));
@@ -166,8 +167,8 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
     const size_t col = std::max<size_t>(1, t * 20 / tile.group), room = std::max<size_t>(grads ? pc * 4 : 0, piece > 0 ? 0 : HEAD_PART);
     c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, room / col / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
     const size_t part = (size_t)ceil_div(c.C1, tile.group) * 20 * t;
-    c.gm = take(grads ? pc * 2 : 0);
-    c.gd = take(grads ? pc * 2 : 0);
+    c.gm = take(grads && !c.thin ? pc * 2 : 0);
+    c.gd = take(grads && !c.thin ? pc * 2 : 0);
     c.part = c.gm;
     if (part > at - c.gm) take(part - (at - c.gm));
   } else {
@@ -175,12 +176,14 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
     c.gd = c.ld;
     c.part = take((size_t)ceil_div(c.C, HEAD_CHUNK) * 40 * t);
   }
-  c.xm = take(grads ? td * ob : 0);
-  c.xd = take(grads ? td * ob : 0);
-  c.dm = take(grads && bf16 ? t * d * 4 : 0);
-  c.dd = take(grads && bf16 ? t * d * 4 : 0);
-  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, grads) : piece_split<float>(T_, c.Tp, c.C, d, grads);
-  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, grads) : piece_split<float>(T_, c.Tp, V % c.C, d, grads));
+  const bool products = grads && !c.thin;
+  c.xm = take(products ? td * ob : 0);
+  c.xd = take(products ? td * ob : 0);
+  c.dm = take(products && bf16 ? t * d * 4 : 0);
+  c.dd = take(products && bf16 ? t * d * 4 : 0);
+  c.runs = take(c.thin ? head_thin_part(T_, V, d) : 0);
+  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, products) : piece_split<float>(T_, c.Tp, c.C, d, products);
+  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, products) : piece_split<float>(T_, c.Tp, V % c.C, d, products));
   c.split_bytes = sp;
   c.split = take(sp);
   c.total = T_ > 0 ? at : 0;
@@ -189,7 +192,7 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
 
 // The products of a smaller batch may be cut into more parts: the split contractions' scratch is
 // the most that any number of rows takes (products over the rows have one plan for all of as many
-// 128-row tiles, those along them for all of as many slices of 32).  It lies behind the rest.
+// 128-row tiles, those along them for all of as many slices of 32).  It lies behind the rest.  A few rows have a carve of their own.
 size_t Engine::head_scratch_most(size_t tokens, int piece) const {
   const int T_ = (int)std::min<size_t>(tokens, 16384);   // of one batch
   if (T_ == 0) return 0;
@@ -205,6 +208,7 @@ size_t Engine::head_scratch_most(size_t tokens, int piece) const {
   most_tokens = T_;
   most_piece = piece;
   most_bytes = c.total - (c.split_bytes + 255) / 256 * 256 + (mx + 255) / 256 * 256;
+  for (int t = 1; t <= std::min(T_, HEAD_THIN); ++t) most_bytes = std::max(most_bytes, head_carve(t, piece, true).total);
   return most_bytes;
 }
 
@@ -255,7 +259,6 @@ int Engine::head_run(const HeadCall& c) {
       if (k.keep) {
         h.lm = lm; h.ld = ld;
       }
-      h.scale = (float)c.scale;
       h.tile = tile;
       int e0 = 0;
       if (timing.on) CK(timing.begin(st, &e0));
@@ -277,7 +280,7 @@ int Engine::head_run(const HeadCall& c) {
       return product(a, 2);
     }
   };
-  if (c.grads && (c.copy_x || T_ != k.Tp)) {
+  if (c.grads && !k.thin && (c.copy_x || T_ != k.Tp)) {
     const PairT<T> o{(T*)(ws + k.xm), (T*)(ws + k.xd)};
     CK(launch_head_copy<T>(o, xm, xd, ldx, T_, k.Tp, d, c.tgt, st));
     xm = o.m;
@@ -299,6 +302,22 @@ int Engine::head_run(const HeadCall& c) {
     }
   }
   if (!c.grads) return FDH_OK;
+  if (k.thin) {
+    HeadThin h{};
+    h.xm = xm; h.xd = xd; h.ldx = ldx;
+    h.wm = wm; h.wd = wd;
+    h.lm = lm; h.ld = ld;
+    h.tgt = c.tgt;
+    h.T = T_; h.V = V; h.d = d;
+    h.scale = (float)c.scale;
+    h.alpha_w = (float)(c.scale * c.inv_eps);
+    h.dxm = c.dx_m; h.dxd = c.dx_d; h.lddx = c.lddx;
+    h.dw = c.dw;
+    h.acc = c.acc;
+    h.part = (float*)(ws + k.runs);
+    CK(launch_head_thin<T>(h, r, c.out_f32, st));
+    return FDH_OK;
+  }
   // the gradient of x is added up over the pieces in fp32
   const bool round = !c.out_f32 && k.C < V;
   const bool op_out = !c.out_f32 && !round;
@@ -310,12 +329,13 @@ int Engine::head_run(const HeadCall& c) {
     const int C = std::min(k.C, V - n0);
     int rc = k.keep ? FDH_OK : logits(n0, C, true);
     if (rc != FDH_OK) return rc;
-    if (sizeof(T) == 4 || k.keep) CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, c.scale, st));
+    if (sizeof(T) == 4 || k.keep) CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, st));
     GemmArgs a[2];
     for (GemmArgs& x : a) {
       x.M = T_; x.N = d; x.K = C;
       x.ldc = lddx;
       x.out_type = op_out ? OUT_OP : OUT_F32;
+      x.alpha = (float)c.scale;
       x.beta = n0 > 0 ? 1.f : 0.f;
     }
     a[0].npairs = 2;
@@ -333,7 +353,7 @@ int Engine::head_run(const HeadCall& c) {
     w.C = (char*)c.dw + (size_t)n0 * d * ob;
     w.ldc = d;
     w.out_type = c.out_f32 ? OUT_F32 : OUT_OP;
-    w.alpha = c.inv_eps;
+    w.alpha = (float)(c.scale * c.inv_eps);
     w.beta = c.acc ? 1.f : 0.f;
     rc = product(&w, 1);
     if (rc != FDH_OK) return rc;
@@ -397,8 +417,8 @@ int Engine::head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, c
     err = "loss: both or neither, 4-byte aligned";
     return FDH_ERR_INVALID_ARG;
   }
-  if (!(g->eps > 0.0) || !std::isfinite(g->eps) || !std::isfinite(g->scale)) {
-    err = "eps must be positive and finite, scale finite";
+  if (!(g->eps > 0.0) || !std::isfinite(g->eps) || !std::isfinite((float)g->scale) || !std::isfinite((float)(g->scale / g->eps))) {
+    err = "eps must be positive and finite, scale and scale / eps finite in float32";
     return FDH_ERR_INVALID_ARG;
   }
   if (g->dtype != FDH_F32 && g->dtype != cfg.dtype) { err = "gradients are float32 or of the context's dtype"; return FDH_ERR_INVALID_ARG; }
@@ -422,7 +442,7 @@ int Engine::head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, c
   c.loss_m = loss_m; c.loss_d = loss_d;
   c.grads = true;
   c.scale = g->scale;
-  c.inv_eps = (float)(1.0 / g->eps);
+  c.inv_eps = 1.0 / g->eps;
   c.dx_m = g->dx_m; c.dx_d = g->dx_d; c.lddx = g->lddx;
   c.dw = g->dw;
   c.out_f32 = g->dtype == FDH_F32;

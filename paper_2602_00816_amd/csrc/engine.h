@@ -98,7 +98,8 @@ struct WsLayout {
 struct HeadCarve {
   int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
   bool keep = false;           // one piece, whose logits are formed once
-  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, split, split_bytes, total;
+  bool thin = false;           // both gradients in one pass over w
+  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, runs, split, split_bytes, total;
 };
 struct HeadCall {
   const void *x_m = nullptr, *x_d = nullptr;   // [T][ldx], operand type
@@ -111,7 +112,7 @@ struct HeadCall {
   double* rowloss = nullptr;                   // scale times the losses at the two points, [2][T], or null
   double scale = 1.0;
   bool grads = false;
-  float inv_eps = 1.f;
+  double inv_eps = 1.0;
   void *dx_m = nullptr, *dx_d = nullptr;       // [T][lddx]
   int64_t lddx = 0;
   void* dw = nullptr;                          // [V][d]

@@ -5,7 +5,8 @@
 // each with full relative precision however small ld is, and Zm = sum a, Zd = sum s.  Then
 //   loss.m = c + log(Z+ Z-) / 2 - lm_y,          loss.d = log(Z+ / Z-) / 2 - ld_y   (Z+- = Zm +- Zd),
 //   P.m = (a Zm - s Zd) / (Z+ Z-),               P.d = (s Zm - a Zd) / (Z+ Z-)
-// and the logits' gradient is w (P.m - [j = y]) and w P.d with the rows' weight w.  Where the two
+// and the logits' gradient is P.m - [j = y] and P.d (the rows' weight is the products' factor: in the
+// rounded gradient it would put one and the same error into every row).  Where the two
 // points are far apart (|ld| >= 1/2) a - s would lose bits: there p = a + s and q = a - s are formed
 // instead, their sums kept apart (Z+ = Sa + Ss + Sp, Z- = Sa - Ss + Sq) and P+- = p / Z+, q / Z-.
 // Which of the two a logit takes may differ between the passes: only the sums' totals are used.
@@ -14,8 +15,6 @@
 // size of the logits stays.  Where one piece holds the vocabulary its logits are formed once.
 #include "head_dev.h"
 #include "kernels.h"
-
-#include <type_traits>
 
 namespace fdh {
 
@@ -161,10 +160,10 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
     const double lp = log(zp), ln = log(zn);
     m = top - (double)r.ym[t] + 0.5 * (lp + ln);
     d = (fabs(zd) < 0.5 * zm ? atanh(zd / zm) : 0.5 * (lp - ln)) - (double)r.yd[t];
-    f[0] = out.scale * (zm / (zp * zn));
-    f[1] = out.scale * (zd / (zp * zn));
-    f[2] = 0.5 * out.scale / zp;
-    f[3] = 0.5 * out.scale / zn;
+    f[0] = zm / (zp * zn);
+    f[1] = zd / (zp * zn);
+    f[2] = 0.5 / zp;
+    f[3] = 0.5 / zn;
   }
   if (out.loss_m) {
     out.loss_m[t] = (float)m;
@@ -188,9 +187,7 @@ __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
 }
 template <typename T>
 __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r, const float* lm, const float* ld, int T_, int C, int n0,
-                                                          const int32_t* tgt, double scale) {
-  constexpr bool fine = sizeof(T) == 4;
-  typedef std::conditional_t<fine, double, float> F;   // of points far apart
+                                                          const int32_t* tgt) {
   const int64_t t = blockIdx.x;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
   const int64_t base = t * C;
@@ -203,26 +200,15 @@ __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r
     return;
   }
   const float c = r.top[t];
-  const float f0 = (float)r.f[0][t], f1 = (float)r.f[1][t], w = (float)scale;
-  const F f2 = (F)r.f[2][t], f3 = (F)r.f[3][t];
+  const double f0 = r.f[0][t], f1 = r.f[1][t], f2 = r.f[2][t], f3 = r.f[3][t];
   for (int j = from + 4 * threadIdx.x; j < end; j += 4 * NT) {
     const float4 a4 = *reinterpret_cast<const float4*>(lm + base + j), b4 = *reinterpret_cast<const float4*>(ld + base + j);
     const float a[4] = {a4.x, a4.y, a4.z, a4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
     float gm[4], gd[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (fine ? far_apart_fine(a[e], b[e], c) : far_apart(b[e])) {
-        F p, q;
-        pair_exp_far(a[e], b[e], c, p, q);
-        gm[e] = (float)(p * f2 + q * f3);
-        gd[e] = (float)(p * f2 - q * f3);
-      } else {
-        float p, s;
-        pair_exp<fine>(a[e], b[e], c, p, s);
-        gm[e] = p * f0 - s * f1;
-        gd[e] = s * f0 - p * f1;
-      }
-      if (n0 + j + e == y) gm[e] -= w;
+      logit_grad<sizeof(T) == 4>(a[e], b[e], c, f0, f1, f2, f3, gm[e], gd[e]);
+      if (n0 + j + e == y) gm[e] -= 1.f;
     }
     store4(o.m + base + j, gm[0], gm[1], gm[2], gm[3]);
     store4(o.d + base + j, gd[0], gd[1], gd[2], gd[3]);
@@ -279,14 +265,14 @@ template hipError_t launch_head_join<float>(const HeadRows&, const float*, int, 
 template hipError_t launch_head_join<double>(const HeadRows&, const double*, int, int, const int32_t*, bool, bool, const HeadOut&, hipStream_t);
 template <typename T>
 hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
-                               const int32_t* tgt, double scale, hipStream_t s) {
-  hipLaunchKernelGGL(head_dlogits_kernel<T>, dim3(Tp, ceil_div(C, CHUNK)), dim3(NT), 0, s, o, r, lm, ld, T_, C, n0, tgt, scale);
+                               const int32_t* tgt, hipStream_t s) {
+  hipLaunchKernelGGL(head_dlogits_kernel<T>, dim3(Tp, ceil_div(C, CHUNK)), dim3(NT), 0, s, o, r, lm, ld, T_, C, n0, tgt);
   return hipGetLastError();
 }
 template hipError_t launch_head_dlogits<float>(PairT<float>, const HeadRows&, const float*, const float*, int, int, int, int,
-                                               const int32_t*, double, hipStream_t);
+                                               const int32_t*, hipStream_t);
 template hipError_t launch_head_dlogits<bf16_t>(PairT<bf16_t>, const HeadRows&, const float*, const float*, int, int, int, int,
-                                                const int32_t*, double, hipStream_t);
+                                                const int32_t*, hipStream_t);
 template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s) {
   hipLaunchKernelGGL(head_copy_kernel<T>, dim3(Tp), dim3(NT), 0, s, o, xm, xd, ldx, T_, dm, tgt);

@@ -1,5 +1,7 @@
 // Device helpers of the loss over the vocabulary (head.hip, head_gemm.hip).
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 namespace fdh {
@@ -14,9 +16,10 @@ __device__ inline bool far_apart(float ld) { return !(fabsf(ld) < FAR_APART); }
 // apart they may be all that one of them has
 __device__ inline bool far_apart_fine(float lm, float ld, float c) { return far_apart(ld) || lm - c < -60.f; }
 
-// e^x, x >= -60, within two steps of fp32 (__expf is off by as many as |x| holds): the rounding of
+// e^x, x <= 0, within two steps of fp32 (__expf is off by as many as |x| holds): the rounding of
 // x log2 e, and what log2 e lacks in fp32, put back to first order.
 __device__ inline float exp_fine(float x) {
+  x = x < -200.f ? -200.f : x;   // (minus infinity, where no column is; NaN stays)
   const float hi = 1.4426950216f, lo = 1.9259630e-8f, p = x * hi;
   const float r = fmaf(x, lo, fmaf(x, hi, -p)), e = __builtin_amdgcn_exp2f(p);
   return fmaf(e, r * 0.69314718f, e);
@@ -46,6 +49,24 @@ __device__ inline void pair_exp_far(float lm, float ld, float c, double& p, doub
   const double x = (double)lm - (double)c;
   p = exp(x + (double)ld);
   q = exp(x - (double)ld);
+}
+
+// gradient of a row's loss with respect to one logit, but for the target's -1: c and f are the row's
+// reference and factors (HeadRows)
+template <bool FINE>
+__device__ inline void logit_grad(float lm, float ld, float c, double f0, double f1, double f2, double f3, float& gm, float& gd) {
+  if (FINE ? far_apart_fine(lm, ld, c) : far_apart(ld)) {
+    typedef std::conditional_t<FINE, double, float> F;
+    F p, q;
+    pair_exp_far(lm, ld, c, p, q);
+    gm = (float)(p * (F)f2 + q * (F)f3);
+    gd = (float)(p * (F)f2 - q * (F)f3);
+  } else {
+    float a, s;
+    pair_exp<FINE>(lm, ld, c, a, s);
+    gm = a * (float)f0 - s * (float)f1;
+    gd = s * (float)f0 - a * (float)f1;
+  }
 }
 
 }  // namespace

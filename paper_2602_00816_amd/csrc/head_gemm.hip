@@ -2,7 +2,7 @@
 // tile of the vocabulary, both channels at once, whose epilogue leaves either the rows'
 // statistics over the tile's columns or the logits' gradient in bf16.
 //
-// lm = xm wm^T and ld = xd wm^T + xm wd^T share their operands: a K slice of the four tiles (x and
+// lm = xm wm^T (+ xd wd^T) and ld = xd wm^T + xm wd^T share their operands: a K slice of the four tiles (x and
 // w, mean and half difference) feeds three matrix operations per output block, as many bytes per
 // operation as a 256 x 256 tile of one product takes from two.  Slices of 32 k come by direct
 // loads to LDS into a ring of three stages, two slices ahead; a wavefront keeps two fragment
@@ -34,7 +34,11 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   constexpr int STAGE = 2 * (BM + BN) * KT;          // elements: xm, xd, wm, wd
   constexpr int NU = 2 * (BM + BN) / 16 / NW;        // 1 KB loads per wavefront and slice
   constexpr int NF = 2 * (IM + JN);                  // fragments of a half slice
-  constexpr int NM = 3 * IM * JN;                    // matrix operations of a half slice
+  // few rows (the operands' bytes bound the tile): lm with xd wd^T too, and exponentials to the last
+  // bits.  What is otherwise left out or rounded is 1e-6 of a loss's half difference, which shows where
+  // that is small by chance and no other rows stand beside it.
+  constexpr bool FINE = BM == 32;
+  constexpr int NM = (FINE ? 4 : 3) * IM * JN;       // matrix operations of a half slice
   static_assert(2 * (BM + BN) / 16 % NW == 0 && BM % 16 == 0 && BN % 16 == 0, "whole loads per wavefront");
   __shared__ __attribute__((aligned(1024))) bf16_t st0[STAGE];
   __shared__ __attribute__((aligned(1024))) bf16_t st1[STAGE];
@@ -115,7 +119,8 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
     const bf16x8_t *xm = f, *wmf = f + IM, *xd = f + IM + JN, *wdf = f + 2 * IM + JN;
     if (kind == 0) cm[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xm[i], cm[i][j], 0, 0, 0);
     else if (kind == 1) cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xd[i], cd[i][j], 0, 0, 0);
-    else cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xm[i], cd[i][j], 0, 0, 0);
+    else if (kind == 2) cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xm[i], cd[i][j], 0, 0, 0);
+    else cm[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xd[i], cm[i][j], 0, 0, 0);
   };
   auto step = [&](auto s, int t) {
     constexpr int S = decltype(s)::value;
@@ -204,7 +209,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
             float p, s;
-            pair_exp_near<false>(cm[i][j][e], cd[i][j][e], mx, p, s);
+            pair_exp_near<FINE>(cm[i][j][e], cd[i][j][e], mx, p, s);
             z[0] += p;
             z[1] += s;
           }
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
             float p, s;
             const bool apart = far_apart(cd[i][j][e]);
             if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], mx, p, s);
-            else pair_exp<false>(cm[i][j][e], cd[i][j][e], mx, p, s);
+            else pair_exp<FINE>(cm[i][j][e], cd[i][j][e], mx, p, s);
             z[0] += apart ? 0.f : p;
             z[1] += apart ? 0.f : s;
             z[2] += apart ? p : 0.f;
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
             float p, s;
-            pair_exp_near<false>(cm[i][j][e], cd[i][j][e], top, p, s);
+            pair_exp_near<FINE>(cm[i][j][e], cd[i][j][e], top, p, s);
             cm[i][j][e] = p * w0 - s * w1;
             cd[i][j][e] = s * w0 - p * w1;
           }
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
             float p, s;
             const bool apart = far_apart(cd[i][j][e]);
             if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], top, p, s);
-            else pair_exp<false>(cm[i][j][e], cd[i][j][e], top, p, s);
+            else pair_exp<FINE>(cm[i][j][e], cd[i][j][e], top, p, s);
             cm[i][j][e] = apart ? p * w2 + s * w3 : p * w0 - s * w1;
             cd[i][j][e] = apart ? p * w2 - s * w3 : s * w0 - p * w1;
           }
@@ -311,7 +316,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
         for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e)
-            if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 == yc) cm[i][j][e] -= a.scale;
+            if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 == yc) cm[i][j][e] -= 1.f;
       }
 #pragma clang loop unroll(full)
       for (int ch = 0; ch < 2; ++ch) {

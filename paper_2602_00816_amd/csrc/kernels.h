@@ -340,10 +340,10 @@ struct HeadOut {
 template <typename P>
 hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_, const int32_t* tgt, bool first, bool last,
                             const HeadOut& out, hipStream_t s);
-// o [Tp][C] = scale times the gradient of the losses with respect to the logits lm, ld (o may be they)
+// o [Tp][C] = the gradient of the losses with respect to the logits lm, ld (o may be they)
 template <typename T>
 hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
-                               const int32_t* tgt, double scale, hipStream_t s);
+                               const int32_t* tgt, hipStream_t s);
 // o [Tp][dm] = the rows of x that have a target, zeros elsewhere
 template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
@@ -361,13 +361,33 @@ struct HeadLogits {
   float* part;             // statistics: [groups][5][T] (maximum and four sums), a group of HeadTile::group columns
   float *lm, *ld;          // statistics: the logits too, [T][C], or null
   bf16_t *gm, *gd;         // gradient: [Tp][C]
-  float scale;
   HeadTile tile;           // head_tile
 };
 HeadTile head_tile(int T_, int C);
-// grad: scale times the gradient of the losses, zeros in rows without a target and from T on; else
+// grad: the gradient of the losses, zeros in rows without a target and from T on; else
 // part, and the target logits of r
 hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s);
+// head_thin.hip: both gradients for up to HEAD_THIN rows whose logits lm, ld [T][V] are in memory, dw
+// (rows of d) alpha_w times the half difference of its gradient (added with acc, float outputs), dx
+// scale times its gradient; outputs float32 or of type T.  part: head_thin_part bytes
+constexpr int HEAD_THIN = 8;
+struct HeadThin {
+  const void *xm, *xd;     // [T][ldx]
+  int64_t ldx;
+  const void *wm, *wd;     // [V][d]
+  const float *lm, *ld;
+  const int32_t* tgt;
+  int T, V, d;
+  float scale, alpha_w;
+  void *dxm, *dxd;         // [T][lddx]
+  int64_t lddx;
+  void* dw;
+  bool acc;
+  float* part;
+};
+size_t head_thin_part(int T_, int V, int d);
+template <typename T>
+hipError_t launch_head_thin(const HeadThin& a, const HeadRows& r, bool out_f32, hipStream_t s);
 hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const float* d, int T_, int dm, hipStream_t s);
 
 }  // namespace fdh

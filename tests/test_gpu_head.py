@@ -37,8 +37,8 @@ def _case(torch, T, V, d, dtype, seed, pad=0, ignore=0.2, half=EPS, size=2.0):
 
 
 SHAPES = [  # T, V, d, pad, piece
-    (1, 8, 8, 0, 0), (1, 1000, 72, 0, 0), (1, 2056, 264, 8, 256), (2, 24, 16, 8, 0), (3, 264, 40, 0, 256), (7, 520, 64, 8, 0),
-    (8, 256, 136, 0, 0), (16, 2056, 520, 0, 0), (17, 1032, 328, 16, 512), (31, 1000, 40, 16, 512), (32, 4104, 64, 0, 0),
+    (1, 8, 8, 0, 0), (1, 1000, 72, 0, 0), (1, 2056, 264, 8, 256), (2, 24, 16, 8, 0), (3, 264, 40, 0, 256), (4, 5000, 1040, 0, 0),
+    (5, 4104, 2056, 8, 0), (7, 520, 64, 8, 0), (8, 256, 136, 0, 0), (9, 256, 136, 0, 0), (16, 2056, 520, 0, 0), (17, 1032, 328, 16, 512), (31, 1000, 40, 16, 512), (32, 4104, 64, 0, 0),
     (33, 2056, 72, 0, 300), (64, 1024, 256, 0, 256), (65, 640, 512, 0, 0), (130, 2056, 264, 8, 1024), (257, 5000, 128, 0, 0),
     (256, 776, 96, 0, 256), (300, 520, 1032, 0, 0), (600, 1304, 40, 8, 512)]
 
@@ -72,11 +72,12 @@ def test_loss_and_gradients(T, V, d, pad, piece, dtype):
             R.check_head(wide, x, w, tgt, scale, EPS, what + " in float32")
 
 
+@pytest.mark.parametrize("T", [77, 5])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_accumulate(dtype):
+def test_accumulate(dtype, T):
     torch = need_gpu()
     from paper_2602_00816_amd import fdhvp as fd
-    T, V, d = 77, 1032, 72
+    V, d = 1032, 72
     m = _model(fd, V, d, dtype)
     x, w, tgt = _case(torch, T, V, d, dtype, 5)
     for piece in (0, 256):
@@ -87,6 +88,24 @@ def test_accumulate(dtype):
         torch.cuda.synchronize()
         assert got[2] is dw
         R.check_head(got, x, w, tgt, 1.0, EPS, f"accumulate {dtype} {piece}", base=base)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_rows_without_a_target(dtype):
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    T, V, d = 7, 520, 40
+    m = _model(fd, V, d, dtype)
+    x, w, tgt = _case(torch, T, V, d, dtype, 6, ignore=0.0)
+    tgt[0], tgt[4] = R.IGNORE, R.IGNORE
+    dirty = tuple(t.clone() for t in x)
+    dirty[0][0], dirty[1][4] = float("nan"), float("inf")
+    got = m.head_grad(dirty, w, tgt, eps=EPS)
+    torch.cuda.synchronize()
+    R.check_head(got, x, w, tgt, 1.0, EPS, "few rows")
+    tgt.fill_(R.IGNORE)
+    loss, dx, dw = m.head_grad(dirty, w, tgt, eps=EPS)
+    assert all(float(t.float().abs().max()) == 0.0 for t in (*loss, *dx, dw))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -114,12 +133,13 @@ def test_rows_without_a_target(dtype):
         assert all(float(t.float().abs().max()) == 0.0 for t in (*loss, *dx, dw))
 
 
+@pytest.mark.parametrize("T", [40, 7])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_not_a_number(dtype):
+def test_not_a_number(dtype, T):
     """A bad target or a NaN in a row shows in that row's loss and gradient, and in dw."""
     torch = need_gpu()
     from paper_2602_00816_amd import fdhvp as fd
-    T, V, d = 40, 600, 64
+    V, d = 600, 64
     m = _model(fd, V, d, dtype)
     for kind in range(4):
         x, w, tgt = _case(torch, T, V, d, dtype, 7, ignore=0.0)
@@ -142,13 +162,14 @@ def test_not_a_number(dtype):
             assert all(torch.equal(a.isfinite(), b.isfinite()) for a, b in zip(only, loss))
 
 
+@pytest.mark.parametrize("T", [90, 6])
 @pytest.mark.parametrize("dtype,half", [("bf16", 0.05), ("bf16", 0.3), ("bf16", 1.0), ("f32", 0.05), ("f32", 0.3), ("f32", 3.0)])
-def test_points_far_apart(dtype, half):
+def test_points_far_apart(dtype, half, T):
     """Half differences of the logits from far below 1/16 to beyond the series (x's half difference
     alone: products of two half differences are left out)."""
     torch = need_gpu()
     from paper_2602_00816_amd import fdhvp as fd
-    T, V, d = 90, 1200, 48
+    V, d = 1200, 48
     m = _model(fd, V, d, dtype)
     x, w, tgt = _case(torch, T, V, d, dtype, 8, half=half)
     w = (w[0], torch.zeros_like(w[0]))
@@ -160,11 +181,12 @@ def test_points_far_apart(dtype, half):
         R.check_head(got, x, w, tgt, 1.0, 1.0, f"half {half} {dtype}")
 
 
+@pytest.mark.parametrize("T", [20, 8])
 @pytest.mark.parametrize("dtype,reach", [("bf16", 28.0), ("f32", 290.0)])
-def test_half_differences_at_the_end_of_their_range(dtype, reach):
+def test_half_differences_at_the_end_of_their_range(dtype, reach, T):
     torch = need_gpu()
     from paper_2602_00816_amd import fdhvp as fd
-    T, V, d = 20, 512, 32
+    V, d = 512, 32
     m = _model(fd, V, d, dtype)
     x, w, tgt = _case(torch, T, V, d, dtype, 9, half=1.0)
     w = (w[0], torch.zeros_like(w[0]))
