@@ -382,6 +382,70 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
   put_sum(a, tk, c, s);
 }
 
+// ---- a few tokens: one launch, no sort -----------------------------------------------------
+// A workgroup per position and 1024 columns: the first position of a token adds the rows of all of
+// them in their order (eight in flight), the others have nothing to do.  The rows that no token has
+// and the positions come behind, as above.  2 tokens, 11784 x 112: 23 -> 8 us.
+constexpr int FEW = 256;
+static_assert(FEW == NT, "a thread for every position");
+__global__ __launch_bounds__(NT) void embed_few_kernel(SumArgs a, const int32_t* tok) {
+  const int T_ = (int)a.T, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (blockIdx.x >= a.blocks) {
+    const int64_t b = blockIdx.x - a.blocks;
+    if (b < a.pblocks) return pos_part(a.posn, (int)b, a.pblocks);
+    const int64_t r0 = ((b - a.pblocks) * WAVES + w) * ZROWS;
+    int own[FEW / 64];
+#pragma unroll
+    for (int k = 0; k < FEW / 64; ++k) own[k] = tok[min(lane + 64 * k, T_ - 1)];
+    for (int i = 0; i < ZROWS && r0 + i < a.V; ++i) {
+      bool hit = false;
+#pragma unroll
+      for (int k = 0; k < FEW / 64; ++k) hit |= own[k] == (int)(r0 + i);
+      if (__ballot(hit)) continue;
+      for (int c = 4 * lane; c < a.dm; c += 256) put4(a.hv, (r0 + i) * a.dm + c, 0.f, 0.f, 0.f, 0.f);
+    }
+    return;
+  }
+  __shared__ uint64_t same[FEW / 64];
+  const int t = (int)(blockIdx.x % a.chunks), c = 4 * ((int)(blockIdx.x / a.chunks) * NT + (int)threadIdx.x);
+  const int tk = tok[t];
+  const uint64_t m = __ballot((int)threadIdx.x < T_ && tok[min((int)threadIdx.x, T_ - 1)] == tk);
+  if (lane == 0) same[w] = m;
+  __syncthreads();
+  uint64_t left[FEW / 64];
+#pragma unroll
+  for (int k = 0; k < FEW / 64; ++k) left[k] = same[k];
+  auto next = [&]() {   // the lowest position left, or -1
+    int p = -1;
+#pragma unroll
+    for (int k = FEW / 64 - 1; k >= 0; --k)
+      if (left[k]) p = 64 * k + __ffsll((unsigned long long)left[k]) - 1;
+#pragma unroll
+    for (int k = 0; k < FEW / 64; ++k)
+      if (p >> 6 == k) left[k] &= left[k] - 1;
+    return p;
+  };
+  int p = next();
+  if (p != t || tk < 0 || tk >= a.V || c >= a.dm) return;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  constexpr int U = 8;
+  while (p >= 0) {
+    float4 x[U];
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p < 0) continue;
+      x[u] = row4(a.dx, (int64_t)p * a.ld + c);
+      n = u + 1;
+      p = next();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < n) { s[0] += (double)x[u].x; s[1] += (double)x[u].y; s[2] += (double)x[u].z; s[3] += (double)x[u].w; }
+  }
+  put_sum(a, (uint32_t)tk, c, s);
+}
+
 // rows per chunk of the sums
 int chunk_rows(int64_t T_) { return T_ <= 16384 ? 32 : 64; }
 
@@ -403,7 +467,7 @@ EmbedScratch embed_carve(int64_t T_, int dm) {
   s.count = take((size_t)SORT_BLOCKS * BINS * 4);
   const size_t chunks = ((size_t)T_ + 31) / 32;   // (of 32 rows: as many or more than are used)
   s.part = take(chunks * 2 * dm * 8);
-  s.total = T_ > 0 ? at : 0;
+  s.total = T_ > FEW ? at : 0;
   return s;
 }
 
@@ -433,6 +497,25 @@ hipError_t launch_embed_bwd(const EmbedGrad& o, const int32_t* tok, const float*
     const hipError_t r = acc ? hipSuccess : launch_fill_f32(o.e, (int64_t)V * dm, 0.f, s);
     return r != hipSuccess || !o.p || o.acc_p ? r : launch_fill_f32(o.p, o.rows * dm, 0.f, s);
   }
+  SumArgs u{};
+  u.dx = dxd;
+  u.ld = ld;
+  u.T = T_;
+  u.dm = dm;
+  u.V = V;
+  u.hv = o.e;
+  u.mul = o.mul;
+  u.acc = acc;
+  const int64_t pos4 = o.p ? (o.acc_p ? std::min<int64_t>(o.rows, S) : o.rows) * (dm / 4) : 0;
+  u.posn = PosArgs{o.p, dxd, ld, B, S, dm, o.acc_p, o.inv_eps, pos4};
+  u.pblocks = (int)std::min<int64_t>(65536, ceil_div(pos4, NT));
+  if (T_ <= FEW) {
+    u.chunks = T_;
+    u.blocks = T_ * ceil_div(dm, 4 * NT);
+    const dim3 grid((unsigned)(u.blocks + u.pblocks + (acc ? 0 : ceil_div(V, ZROWS * WAVES))));
+    hipLaunchKernelGGL(embed_few_kernel, grid, dim3(NT), 0, s, u, tok);
+    return hipGetLastError();
+  }
   char* ws = (char*)scratch;
   const EmbedScratch sc = embed_carve(T_, dm);
   SortArgs a{};
@@ -461,26 +544,14 @@ hipError_t launch_embed_bwd(const EmbedGrad& o, const int32_t* tok, const float*
     if (p % 2 == 0) hipLaunchKernelGGL(sort_count_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
     else hipLaunchKernelGGL(sort_move_kernel, dim3(a.blocks + zblocks), dim3(NT), 0, s, a);
   }
-  SumArgs u{};
   u.key = a.okey;
   u.pos = a.opos;
-  u.dx = dxd;
-  u.ld = ld;
-  u.T = T_;
-  u.dm = dm;
-  u.V = V;
-  u.hv = o.e;
-  u.mul = o.mul;
-  u.acc = acc;
   u.part = (double*)(ws + sc.part);
   const int R = chunk_rows(T_);
   const unsigned chunks = ceil_div(T_, R), cols = ceil_div(dm, 256);
   u.chunks = chunks;
   u.blocks = (int64_t)chunks * ceil_div(cols, WAVES);
   u.zfrom = (int)(2 * passes * zrows);
-  const int64_t pos4 = o.p ? (o.acc_p ? std::min<int64_t>(o.rows, S) : o.rows) * (dm / 4) : 0;
-  u.posn = PosArgs{o.p, dxd, ld, B, S, dm, o.acc_p, o.inv_eps, pos4};
-  u.pblocks = (int)std::min<int64_t>(65536, ceil_div(pos4, NT));
   const dim3 gs((unsigned)(u.blocks + u.pblocks + (zero4 ? ceil_div(V - u.zfrom, ZROWS * WAVES) : 0))), gj(chunks, cols);
   if (R == 32) {
     hipLaunchKernelGGL(embed_sum_kernel<32>, gs, dim3(NT), 0, s, u);

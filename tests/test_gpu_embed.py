@@ -69,7 +69,9 @@ def test_forward(V, d, B, S, pad, scale, pos, dtype):
 
 
 @pytest.mark.parametrize("V,d,B,S,pad,kind,pos", [
-    (8, 8, 1, 1, 0, "uniform", False), (24, 16, 1, 31, 4, "zipf", True), (256, 64, 8, 64, 0, "uniform", False),
+    (8, 8, 1, 1, 0, "uniform", False), (24, 16, 1, 31, 4, "zipf", True), (40, 1032, 1, 2, 0, "one", False),
+    (520, 264, 2, 32, 4, "uniform", True), (64, 4104, 5, 13, 0, "zipf", False), (1000, 24, 4, 64, 0, "one", True),
+    (128256, 16, 1, 256, 0, "uniform", False), (1000, 24, 1, 257, 0, "zipf", True), (256, 64, 8, 64, 0, "uniform", False),
     (504, 72, 3, 11, 8, "one", True), (512, 264, 1, 32, 0, "uniform", False), (520, 264, 1, 33, 0, "one", False),
     (1000, 520, 2, 650, 12, "zipf", True), (8192, 1032, 9, 57, 0, "zipf", False), (32000, 256, 1, 8192, 0, "zipf", False),
     (128, 40, 70, 257, 0, "zipf", True), (128256, 32, 3, 5461, 0, "uniform", False), (262136, 8, 1, 70001, 0, "uniform", False),
