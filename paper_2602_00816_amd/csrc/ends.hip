@@ -2,6 +2,7 @@
 // fdh_embed_* and fdh_head_* (include/fdhvp.h), and the loop over the vocabulary's pieces.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "engine.h"
 #include "regions.h"
@@ -113,10 +114,9 @@ GemmOperand mnmaj(const void* p, int64_t ld) {
   return o;
 }
 
-// the products of a piece of C columns: shapes for the plans of split contractions
+// scratch of the products of a piece of C columns: those that its gradient goes to and, unless fused, its logits'
 template <typename T>
-size_t piece_split(int T_, int Tp, int C, int d, bool grads) {
-  constexpr bool fused = sizeof(T) == 2;   // bf16 models form their logits in a kernel of its own
+size_t piece_split(int T_, int Tp, int C, int d, bool grads, bool fused) {
   GemmArgs g[2];
   auto need = [&](int M, int N, int K, int n) {
     for (int p = 0; p < 2; ++p) {
@@ -150,31 +150,36 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   int64_t C = piece > 0 ? piece : std::max<int64_t>(HEAD_PIECE_MIN, HEAD_PIECE_ELEMS / std::max(1, T_) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND);
   C = (C + HEAD_PIECE_ROUND - 1) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND;
   c.C = (int)(whole ? V : std::min<int64_t>(C, V));
-  c.keep = c.C == V && (!bf16 || grads);   // the logits of the one piece are formed once
+  c.keep = grads && c.C == V;   // the logits of the one piece are formed once
   const size_t tp = (size_t)c.Tp, pc = tp * c.C, td = tp * d;
   c.top = take(t * 4);
   c.z = take(4 * t * 8);
   c.ym = take(2 * t * 4);
   c.f = take(4 * t * 8);
-  // fp32 models: a piece's logits, which their gradient replaces.  bf16 models: the gradient of a
-  // piece (and its logits where they are kept).  Statistics of column groups: bf16 models, in the
-  // first pass, in the gradient's place, of as many columns as fit there, alone of up to HEAD_PART bytes.
+  // The gradient of a piece and, where they are formed in memory, its logits (whose place the gradient
+  // takes in fp32 models).
+  // The first pass has the statistics of column groups in the gradient's place, of as many columns as
+  // fit there, alone of up to HEAD_PART bytes.
+  c.fused = bf16 || head_f32_fused(T_, c.C, d);
+  const bool whole_logits = c.keep || !c.fused, inplace = whole_logits && !bf16;
+  c.lm = take(whole_logits ? pc * 4 : 0);
+  c.ld = take(whole_logits ? pc * 4 : 0);
+  const size_t gb = grads && !c.thin && !inplace ? pc * ob : 0, pb = bf16 ? 20 : 40;
+  const HeadTile tile = head_tile(T_, c.C);
   c.C1 = c.C;
-  c.lm = take(pc * (bf16 ? (c.keep ? 4 : 0) : 4));
-  c.ld = take(pc * (bf16 ? (c.keep ? 4 : 0) : 4));
-  if (bf16) {
-    const HeadTile tile = head_tile(T_, c.C);
-    const size_t col = std::max<size_t>(1, t * 20 / tile.group), room = std::max<size_t>(grads ? pc * 4 : 0, piece > 0 ? 0 : HEAD_PART);
+  size_t part = (size_t)ceil_div(c.C, HEAD_CHUNK) * pb * t;
+  if (c.fused) {
+    const size_t col = std::max<size_t>(1, t * pb / tile.group), room = std::max<size_t>(2 * gb, piece > 0 ? 0 : HEAD_PART);
     c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, room / col / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
-    const size_t part = (size_t)ceil_div(c.C1, tile.group) * 20 * t;
-    c.gm = take(grads && !c.thin ? pc * 2 : 0);
-    c.gd = take(grads && !c.thin ? pc * 2 : 0);
-    c.part = c.gm;
-    if (part > at - c.gm) take(part - (at - c.gm));
-  } else {
+    part = (size_t)ceil_div(c.C1, tile.group) * pb * t;
+  }
+  c.gm = take(gb);
+  c.gd = take(gb);
+  c.part = c.gm;
+  if (part > at - c.gm) take(part - (at - c.gm));
+  if (inplace) {
     c.gm = c.lm;
     c.gd = c.ld;
-    c.part = take((size_t)ceil_div(c.C, HEAD_CHUNK) * 40 * t);
   }
   const bool products = grads && !c.thin;
   c.xm = take(products ? td * ob : 0);
@@ -182,33 +187,24 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   c.dm = take(products && bf16 ? t * d * 4 : 0);
   c.dd = take(products && bf16 ? t * d * 4 : 0);
   c.runs = take(c.thin ? head_thin_part(T_, V, d) : 0);
-  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, products) : piece_split<float>(T_, c.Tp, c.C, d, products);
-  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, products) : piece_split<float>(T_, c.Tp, V % c.C, d, products));
+  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, products, c.fused) : piece_split<float>(T_, c.Tp, c.C, d, products, c.fused);
+  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, products, c.fused) : piece_split<float>(T_, c.Tp, V % c.C, d, products, c.fused));
   c.split_bytes = sp;
   c.split = take(sp);
   c.total = T_ > 0 ? at : 0;
   return c;
 }
 
-// The products of a smaller batch may be cut into more parts: the split contractions' scratch is
-// the most that any number of rows takes (products over the rows have one plan for all of as many
-// 128-row tiles, those along them for all of as many slices of 32).  It lies behind the rest.  A few rows have a carve of their own.
+// Smaller batches may take more: contractions that are cut, other ways of the logits, a few rows.
+// (A batch has a multiple of 8 tokens.)
 size_t Engine::head_scratch_most(size_t tokens, int piece) const {
   const int T_ = (int)std::min<size_t>(tokens, 16384);   // of one batch
-  if (T_ == 0) return 0;
   std::lock_guard<std::mutex> lk(linear_mu);
   if (T_ == most_tokens && piece == most_piece) return most_bytes;
-  const HeadCarve c = head_carve(T_, piece, true);
-  size_t mx = c.split_bytes;
-  for (int C : {c.C, V % c.C}) {
-    if (!C) continue;
-    for (int t = (T_ + 31) / 32 * 32; t > 0; t -= 32)
-      mx = std::max(mx, bf16 ? piece_split<bf16_t>(t, t, C, d, true) : piece_split<float>(t, t, C, d, true));
-  }
   most_tokens = T_;
   most_piece = piece;
-  most_bytes = c.total - (c.split_bytes + 255) / 256 * 256 + (mx + 255) / 256 * 256;
-  for (int t = 1; t <= std::min(T_, HEAD_THIN); ++t) most_bytes = std::max(most_bytes, head_carve(t, piece, true).total);
+  most_bytes = head_carve(T_, piece, true).total;
+  for (int t = 8; t < T_; t += 8) most_bytes = std::max(most_bytes, head_carve(t, piece, true).total);
   return most_bytes;
 }
 
@@ -243,42 +239,39 @@ int Engine::head_run(const HeadCall& c) {
     if (timing.on) CK(timing.end(st, 0, e0, gemm_flops(a[0]) + (n > 1 ? gemm_flops(a[1]) : 0.0), 0.0));
     return FDH_OK;
   };
-  // logits of columns n0 .. n0 + C - 1 (the product of the two half differences, of second order in
-  // the step, is left out, as in every linear layer): fp32 models in lm and ld, bf16 models statistics
-  // (and, if kept, the logits) or gradient
+  // the product that forms columns n0 .. n0 + C - 1 of the logits, for their statistics (keeping them, if
+  // they are kept) or for their gradient
   auto logits = [&](int n0, int C, bool grad) -> int {
-    const T *pm = wm + (int64_t)n0 * d, *pd = wd + (int64_t)n0 * d;
-    if constexpr (sizeof(T) == 2) {
-      HeadLogits h{};
-      h.xm = xm; h.xd = xd; h.ldx = ldx;
-      h.wm = pm; h.wd = pd;
-      h.T = T_; h.Tp = k.Tp; h.C = C; h.d = d; h.n0 = n0;
-      h.tgt = c.tgt;
-      h.part = (float*)(ws + k.part);
-      h.gm = g.m; h.gd = g.d;
-      if (k.keep) {
-        h.lm = lm; h.ld = ld;
-      }
-      h.tile = tile;
-      int e0 = 0;
-      if (timing.on) CK(timing.begin(st, &e0));
-      CK(launch_head_logits(h, r, grad, st));
-      if (timing.on) CK(timing.end(st, 0, e0, 6.0 * T_ * C * d, 0.0));
-      return FDH_OK;
-    } else {
+    if (!k.fused) {
       GemmArgs a[2];
       for (GemmArgs& x : a) {
         x.M = T_; x.N = C; x.K = d;
         x.ldc = C;
       }
       a[0].npairs = 2;
-      a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(pm, d);
-      a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(pd, d);
+      a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(wm + (int64_t)n0 * d, d);
+      a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(wd + (int64_t)n0 * d, d);
       a[0].C = ld;
-      a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(pm, d);
+      a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(wm + (int64_t)n0 * d, d);
       a[1].C = lm;
       return product(a, 2);
     }
+    HeadLogits h{};
+    h.xm = xm; h.xd = xd; h.ldx = ldx;
+    h.wm = wm + (int64_t)n0 * d; h.wd = wd + (int64_t)n0 * d;
+    h.T = T_; h.Tp = k.Tp; h.C = C; h.d = d; h.n0 = n0;
+    h.tgt = c.tgt;
+    h.part = ws + k.part;
+    h.gm = g.m; h.gd = g.d;
+    if (k.keep) {
+      h.lm = lm; h.ld = ld;
+    }
+    h.tile = tile;
+    int e0 = 0;
+    if (timing.on) CK(timing.begin(st, &e0));
+    CK(launch_head_logits<T>(h, r, grad, st));
+    if (timing.on) CK(timing.end(st, 0, e0, 6.0 * T_ * C * d, 0.0));
+    return FDH_OK;
   };
   if (c.grads && !k.thin && (c.copy_x || T_ != k.Tp)) {
     const PairT<T> o{(T*)(ws + k.xm), (T*)(ws + k.xd)};
@@ -293,13 +286,9 @@ int Engine::head_run(const HeadCall& c) {
     const int rc = logits(n0, C, false);
     if (rc != FDH_OK) return rc;
     const bool last = n0 + C == V;
-    if constexpr (sizeof(T) == 2) {
-      CK(launch_head_join(r, (const float*)(ws + k.part), (int)ceil_div(C, tile.group), T_, c.tgt, n0 == 0, last, out, st));
-    } else {
-      double* part = (double*)(ws + k.part);
-      CK(launch_head_stats(r, part, lm, ld, T_, C, n0, c.tgt, st));
-      CK(launch_head_join(r, (const double*)part, (int)ceil_div(C, HEAD_CHUNK), T_, c.tgt, n0 == 0, last, out, st));
-    }
+    typedef std::conditional_t<sizeof(T) == 4, double, float> P;
+    if (!k.fused) CK(launch_head_stats(r, (double*)(ws + k.part), lm, ld, T_, C, n0, c.tgt, st));
+    CK(launch_head_join(r, (const P*)(ws + k.part), (int)ceil_div(C, k.fused ? tile.group : HEAD_CHUNK), T_, c.tgt, n0 == 0, last, out, st));
   }
   if (!c.grads) return FDH_OK;
   if (k.thin) {
@@ -329,7 +318,7 @@ int Engine::head_run(const HeadCall& c) {
     const int C = std::min(k.C, V - n0);
     int rc = k.keep ? FDH_OK : logits(n0, C, true);
     if (rc != FDH_OK) return rc;
-    if (sizeof(T) == 4 || k.keep) CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, st));
+    if (k.keep || !k.fused) CK(launch_head_dlogits<T>(g, r, lm, ld, T_, k.Tp, C, n0, c.tgt, st));
     GemmArgs a[2];
     for (GemmArgs& x : a) {
       x.M = T_; x.N = d; x.K = C;

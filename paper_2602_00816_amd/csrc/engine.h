@@ -99,6 +99,7 @@ struct HeadCarve {
   int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
   bool keep = false;           // one piece, whose logits are formed once
   bool thin = false;           // both gradients in one pass over w
+  bool fused = true;           // logits on head_gemm.hip, else on the GEMM (fp32 models, many rows)
   size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, runs, split, split_bytes, total;
 };
 struct HeadCall {

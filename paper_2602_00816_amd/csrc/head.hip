@@ -31,7 +31,7 @@ __global__ void head_targets_kernel(int32_t* tgt, const int32_t* tok, const int3
   tgt[t] = y == IGNORE_LABEL ? y : min(max(y, 0), V - 1);
 }
 
-// Statistics of one piece of the logits (fp32 models), part [chunks][5][T]: the maximum and the four
+// Statistics of one piece of the logits (fp32 models, many rows), part [chunks][5][T]: the maximum and the four
 // sums of a row's CHUNK columns, one workgroup each; every thread keeps its sums relative to its own
 // maximum.
 constexpr int CHUNK = HEAD_CHUNK;
@@ -177,8 +177,8 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
   for (int k = 0; k < 4; ++k) r.f[k][t] = f[k];
 }
 
-// Gradient of logits that are in memory (one piece holds the vocabulary, or an fp32 model) in the
-// operand type, [Tp][C]; rows without a target and rows behind the last are zeros.  o may be the
+// Gradient of logits that are in memory (one piece holds the vocabulary, or an fp32 model's many rows)
+// in the operand type, [Tp][C]; rows without a target and rows behind the last are zeros.  o may be the
 // logits (fp32 models).
 __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {

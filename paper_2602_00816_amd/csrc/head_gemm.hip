@@ -1,48 +1,71 @@
-// The logits' pair of bf16 models without logits in memory: the product of a tile of rows and a
-// tile of the vocabulary, both channels at once, whose epilogue leaves either the rows'
-// statistics over the tile's columns or the logits' gradient in bf16.
+// The logits' pair without logits in memory: the product of a tile of rows and a tile of the
+// vocabulary, both channels at once, whose epilogue leaves either the rows' statistics over the
+// tile's columns or the logits' gradient in the operand type.
 //
-// lm = xm wm^T (+ xd wd^T) and ld = xd wm^T + xm wd^T share their operands: a K slice of the four tiles (x and
-// w, mean and half difference) feeds three matrix operations per output block, as many bytes per
-// operation as a 256 x 256 tile of one product takes from two.  Slices of 32 k come by direct
-// loads to LDS into a ring of three stages, two slices ahead; a wavefront keeps two fragment
-// sets (half slices of 16 k) and reads one while the matrix operations run on the other.  A
-// stage is free as soon as every wavefront has the second half of its slice in registers, which
-// the wait before the slice's one barrier makes sure of.
+// lm = xm wm^T (+ xd wd^T) and ld = xd wm^T + xm wd^T share their operands: a K slice of the four
+// tiles (x and w, mean and half difference) feeds three matrix operations per output block, as many
+// bytes per operation as a 256 x 256 tile of one product takes from two.  Slices of 64 bytes a row
+// (32 k in bf16, 16 in fp32) come by direct loads to LDS into a ring of three stages, two slices
+// ahead; a wavefront keeps two fragment sets (half slices) and reads one while the matrix operations
+// run on the other.  A stage is free as soon as every wavefront has the second half of its slice in
+// registers, which the wait before the slice's one barrier makes sure of.
 #include "gemm_dev.h"
 #include "head_dev.h"
 #include "kernels.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace fdh {
 
 namespace {
 
-constexpr int KT = 32;                  // k per slice
 constexpr uint32_t OOB = 0x80000000u;   // byte offset at which the buffer resources end
+constexpr int ROW = 64;                 // bytes of a row's slice
 
-// element (row, 16-byte chunk c) of a [rows][32] tile: 16 lanes that read 16 consecutive rows hit 64 banks
-__device__ inline int tile_at(int row, int c) { return row * KT + ((c ^ ((row >> 2) & 3)) << 3); }
-__device__ inline bf16x8_t fragment(const bf16_t* t, int r0, int kk, int lane) {
-  return *reinterpret_cast<const bf16x8_t*>(t + tile_at(r0 + (lane & 31), (kk >> 3) + (lane >> 5)));
+// byte offset of 16-byte chunk c of a row of a tile: 16 lanes that read 16 consecutive rows hit 64 banks
+__device__ inline int tile_at(int row, int c) { return row * ROW + ((c ^ ((row >> 2) & 3)) << 4); }
+
+// A fragment holds a lane's 16 bytes of a row: chunk 2 half + (lane >> 5).  fp32: the four operations
+// that a pair of fragments feeds take one element each, k and k + 4 in the two halves of the wavefront.
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> {
+  typedef bf16x8_t type;
+  static constexpr int OPS = 1;
+  static __device__ inline f32x16_t mma(const type& w, const type& x, int, const f32x16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x, c, 0, 0, 0);
+  }
+};
+template <> struct Frag<float> {
+  typedef float type __attribute__((ext_vector_type(4)));
+  static constexpr int OPS = 4;
+  static __device__ inline f32x16_t mma(const type& w, const type& x, int e, const f32x16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(w[e], x[e], c, 0, 0, 0);
+  }
+};
+template <typename T>
+__device__ inline typename Frag<T>::type fragment(const char* t, int r0, int half, int lane) {
+  return *reinterpret_cast<const typename Frag<T>::type*>(t + tile_at(r0 + (lane & 31), 2 * half + (lane >> 5)));
 }
 
-template <int BM, int BN, int WM, int WN, bool GRAD>
+template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
 __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a, HeadRows r) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, IM = WTM / 32, JN = WTN / 32;
-  constexpr int STAGE = 2 * (BM + BN) * KT;          // elements: xm, xd, wm, wd
+  typedef typename Frag<T>::type F;
+  typedef std::conditional_t<sizeof(T) == 4, double, float> P;   // of the statistics and of points far apart
+  constexpr int KT = ROW / sizeof(T), CE = 16 / sizeof(T);   // k per slice and per 16 bytes
+  constexpr int STAGE = 2 * (BM + BN) * ROW;         // bytes: xm, xd, wm, wd
   constexpr int NU = 2 * (BM + BN) / 16 / NW;        // 1 KB loads per wavefront and slice
   constexpr int NF = 2 * (IM + JN);                  // fragments of a half slice
   // few rows (the operands' bytes bound the tile): lm with xd wd^T too, and exponentials to the last
-  // bits.  What is otherwise left out or rounded is 1e-6 of a loss's half difference, which shows where
-  // that is small by chance and no other rows stand beside it.
-  constexpr bool FINE = BM == 32;
-  constexpr int NM = (FINE ? 4 : 3) * IM * JN;       // matrix operations of a half slice
+  // bits, which fp32 models always take.  What is otherwise left out or rounded is 1e-6 of a loss's
+  // half difference, which shows where that is small by chance and no other rows stand beside it.
+  constexpr bool WHOLE = BM == 32, FINE = WHOLE || sizeof(T) == 4;
+  constexpr int NM = (WHOLE ? 4 : 3) * IM * JN * Frag<T>::OPS;       // matrix operations of a half slice
   static_assert(2 * (BM + BN) / 16 % NW == 0 && BM % 16 == 0 && BN % 16 == 0, "whole loads per wavefront");
-  __shared__ __attribute__((aligned(1024))) bf16_t st0[STAGE];
-  __shared__ __attribute__((aligned(1024))) bf16_t st1[STAGE];
-  __shared__ __attribute__((aligned(1024))) bf16_t st2[STAGE];
+  __shared__ __attribute__((aligned(1024))) char st0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char st1[STAGE];
+  __shared__ __attribute__((aligned(1024))) char st2[STAGE];
 
   const int gx = (a.C + BN - 1) / BN, gy = (a.T + BM - 1) / BM;
   const int lin = xcd_order(blockIdx.x, gridDim.x);
@@ -60,7 +83,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   // load q of a slice: 16 rows of one of the four tiles.  Rows past the end read the last one
   // (their outputs are not used), lanes past the contraction's end nothing (zeros).
   const int ck = (lane & 3) ^ ((lane >> 4) & 3);   // (row >> 2 is lane >> 4 modulo 4)
-  const bf16_t* base[NU];
+  const T* base[NU];
   uint32_t vo[NU];
 #pragma clang loop unroll(full)
   for (int u = 0; u < NU; ++u) {
@@ -72,22 +95,22 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
     const int row = (half ? qx - per : qx) * 16 + (lane >> 2);
     const int64_t ld = isx ? a.ldx : a.d;
     const int first = isx ? m0 : n0, end = isx ? a.T : a.C;
-    const bf16_t* p = isx ? (half ? a.xd : a.xm) : (half ? a.wd : a.wm);
+    const T* p = (const T*)(isx ? (half ? a.xd : a.xm) : (half ? a.wd : a.wm));
     base[u] = p + first * ld;
-    vo[u] = 2u * (uint32_t)((min(first + row, end - 1) - first) * ld + 8 * ck);
+    vo[u] = (uint32_t)sizeof(T) * (uint32_t)((min(first + row, end - 1) - first) * ld + CE * ck);
   }
-  auto stage = [&](auto s) -> bf16_t* {
+  auto stage = [&](auto s) -> char* {
     constexpr int S = decltype(s)::value % 3;
     if constexpr (S == 0) return st0;
     else if constexpr (S == 1) return st1;
     else return st2;
   };
   // load u of slice t (past the last: the last again, into a stage that nobody reads)
-  auto dma = [&](bf16_t* st, int t, int u) {
+  auto dma = [&](char* st, int t, int u) {
     const int k0 = min(t, total - 1) * KT;
     const uint64_t b = (uint64_t)(uintptr_t)(base[u] + k0);
     const i32x4_t rs{(int)(uint32_t)b, (int)((b >> 32) & 0xffffu), (int)OOB, 0x00020000};
-    const uint32_t off = 8 * ck < a.d - k0 ? vo[u] : OOB;
+    const uint32_t off = CE * ck < a.d - k0 ? vo[u] : OOB;
     const uint32_t ldsaddr = (uint32_t)(uintptr_t)(lds_void_t*)st + (uint32_t)((wave + u * NW) * 1024);
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
@@ -107,28 +130,29 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       for (int e = 0; e < 16; ++e) cm[i][j][e] = cd[i][j][e] = 0.f;
 
   // fragments 0 .. IM - 1: xm, then JN of wm, IM of xd, JN of wd (the order in which they are used)
-  bf16x8_t f0[NF], f1[NF];
-  auto rd = [&](bf16x8_t& f, const bf16_t* st, int x, int kk) {
-    if (x < IM) f = fragment(st, wm * WTM + x * 32, kk, lane);
-    else if (x < IM + JN) f = fragment(st + 2 * BM * KT, wn * WTN + (x - IM) * 32, kk, lane);
-    else if (x < 2 * IM + JN) f = fragment(st + BM * KT, wm * WTM + (x - IM - JN) * 32, kk, lane);
-    else f = fragment(st + (2 * BM + BN) * KT, wn * WTN + (x - 2 * IM - JN) * 32, kk, lane);
+  F f0[NF], f1[NF];
+  auto rd = [&](F& f, const char* st, int x, int half) {
+    if (x < IM) f = fragment<T>(st, wm * WTM + x * 32, half, lane);
+    else if (x < IM + JN) f = fragment<T>(st + 2 * BM * ROW, wn * WTN + (x - IM) * 32, half, lane);
+    else if (x < 2 * IM + JN) f = fragment<T>(st + BM * ROW, wm * WTM + (x - IM - JN) * 32, half, lane);
+    else f = fragment<T>(st + (2 * BM + BN) * ROW, wn * WTN + (x - 2 * IM - JN) * 32, half, lane);
   };
-  auto mma = [&](const bf16x8_t (&f)[NF], int e) {
-    const int kind = e / (IM * JN), i = e % (IM * JN) / JN, j = e % JN;
-    const bf16x8_t *xm = f, *wmf = f + IM, *xd = f + IM + JN, *wdf = f + 2 * IM + JN;
-    if (kind == 0) cm[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xm[i], cm[i][j], 0, 0, 0);
-    else if (kind == 1) cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wmf[j], xd[i], cd[i][j], 0, 0, 0);
-    else if (kind == 2) cd[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xm[i], cd[i][j], 0, 0, 0);
-    else cm[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wdf[j], xd[i], cm[i][j], 0, 0, 0);
+  auto mma = [&](const F (&f)[NF], int e) {
+    constexpr int NB = IM * JN;
+    const int kind = e / (NB * Frag<T>::OPS), k = e / NB % Frag<T>::OPS, i = e % NB / JN, j = e % JN;
+    const F *xm = f, *wmf = f + IM, *xd = f + IM + JN, *wdf = f + 2 * IM + JN;
+    if (kind == 0) cm[i][j] = Frag<T>::mma(wmf[j], xm[i], k, cm[i][j]);
+    else if (kind == 1) cd[i][j] = Frag<T>::mma(wmf[j], xd[i], k, cd[i][j]);
+    else if (kind == 2) cd[i][j] = Frag<T>::mma(wdf[j], xm[i], k, cd[i][j]);
+    else cm[i][j] = Frag<T>::mma(wdf[j], xd[i], k, cm[i][j]);
   };
   auto step = [&](auto s, int t) {
     constexpr int S = decltype(s)::value;
-    bf16_t* cur = stage(s);
-    const bf16_t* nxt = stage(std::integral_constant<int, S + 1>{});
+    char* cur = stage(s);
+    const char* nxt = stage(std::integral_constant<int, S + 1>{});
 #pragma clang loop unroll(full)
     for (int x = 0; x < NF; ++x) {
-      rd(f1[x], cur, x, 16);
+      rd(f1[x], cur, x, 1);
 #pragma clang loop unroll(full)
       for (int e = x * NM / NF; e < (x + 1) * NM / NF; ++e) mma(f0, e);
       __builtin_amdgcn_sched_barrier(0);
@@ -202,7 +226,8 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
           far = fmaxf(far, fabsf(cd[i][j][e]));
         }
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      float z[4] = {0.f, 0.f, 0.f, 0.f};
+      float za = 0.f, zs = 0.f;
+      P zp = 0, zq = 0;
       if (!__any(!(far < HEAD_NEAR))) {   // (NaN: a half difference that is NaN makes the sums NaN either way)
 #pragma clang loop unroll(full)
         for (int j = 0; j < JN; ++j)
@@ -210,24 +235,29 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
           for (int e = 0; e < 16; ++e) {
             float p, s;
             pair_exp_near<FINE>(cm[i][j][e], cd[i][j][e], mx, p, s);
-            z[0] += p;
-            z[1] += s;
+            za += p;
+            zs += s;
           }
       } else {
 #pragma clang loop unroll(full)
         for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
-            float p, s;
-            const bool apart = far_apart(cd[i][j][e]);
-            if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], mx, p, s);
-            else pair_exp<FINE>(cm[i][j][e], cd[i][j][e], mx, p, s);
-            z[0] += apart ? 0.f : p;
-            z[1] += apart ? 0.f : s;
-            z[2] += apart ? p : 0.f;
-            z[3] += apart ? s : 0.f;
+            const float m = cm[i][j][e], d = cd[i][j][e];
+            if (sizeof(T) == 4 ? far_apart_fine(m, d, mx) : far_apart(d)) {
+              P p, q;
+              pair_exp_far(m, d, mx, p, q);
+              zp += p;
+              zq += q;
+            } else {
+              float p, s;
+              pair_exp<FINE>(m, d, mx, p, s);
+              za += p;
+              zs += s;
+            }
           }
       }
+      P z[4] = {za, zs, zp, zq};
 #pragma clang loop unroll(full)
       for (int k = 0; k < 4; ++k) z[k] += __shfl_xor(z[k], 32, 64);
       if (row >= a.T) continue;
@@ -245,7 +275,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
             }
       }
       if (h == 0) {
-        float* o = a.part + (int64_t)(c0 / WTN) * 5 * a.T + row;
+        P* o = (P*)a.part + (int64_t)(c0 / WTN) * 5 * a.T + row;
         o[0] = mx;
 #pragma clang loop unroll(full)
         for (int k = 0; k < 4; ++k) o[(int64_t)(k + 1) * a.T] = z[k];
@@ -266,12 +296,12 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       }
     }
   } else {
-    // through LDS, so that a store covers 8 rows of 64 columns (JN = 2) or 16 of 32; a wavefront's
+    // bf16: through LDS, so that a store covers 8 rows of 64 columns (JN = 2) or 16 of 32; a wavefront's
     // own area, 32 rows of WTN columns for each channel in turn
     constexpr int LD = WTN + 4;      // elements: 8-byte rows, lanes of 32 rows on distinct banks
-    static_assert(NW * 32 * LD <= STAGE, "staging areas exceed a stage");
+    static_assert(sizeof(T) == 4 || NW * 32 * LD * 2 <= STAGE, "staging areas exceed a stage");
     __syncthreads();                 // every wavefront is done with the ring
-    bf16_t* stg = st0 + wave * 32 * LD;
+    bf16_t* stg = reinterpret_cast<bf16_t*>(st0) + wave * 32 * LD;
     constexpr int LPR = WTN / 8, RPS = 64 / LPR;   // lanes per row of a store, rows per store
 #pragma clang loop unroll(full)
     for (int i = 0; i < IM; ++i) {
@@ -281,14 +311,18 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       const int y = row < a.T ? a.tgt[t] : IGNORE_LABEL;
       const bool none = y == IGNORE_LABEL;
       const float top = r.top[t];
-      const float w0 = (float)r.f[0][t], w1 = (float)r.f[1][t], w2 = (float)r.f[2][t], w3 = (float)r.f[3][t];
+      const double e0 = r.f[0][t], e1 = r.f[1][t], e2 = r.f[2][t], e3 = r.f[3][t];
+      const float w0 = (float)e0, w1 = (float)e1;
       const int yc = y - a.n0 - c0;
-      float far = 0.f;
+      float far = 0.f, low = 0.f;
 #pragma clang loop unroll(full)
       for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
-        for (int e = 0; e < 16; ++e) far = fmaxf(far, fabsf(cd[i][j][e]));
-      if (!__any(!(far < HEAD_NEAR))) {
+        for (int e = 0; e < 16; ++e) {
+          far = fmaxf(far, fabsf(cd[i][j][e]));
+          if constexpr (sizeof(T) == 4) low = fminf(low, cm[i][j][e] - top);
+        }
+      if (!__any(!(far < HEAD_NEAR) || low < -60.f)) {
 #pragma clang loop unroll(full)
         for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
@@ -303,12 +337,10 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
         for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e) {
-            float p, s;
-            const bool apart = far_apart(cd[i][j][e]);
-            if (apart) pair_exp_far(cm[i][j][e], cd[i][j][e], top, p, s);
-            else pair_exp<FINE>(cm[i][j][e], cd[i][j][e], top, p, s);
-            cm[i][j][e] = apart ? p * w2 + s * w3 : p * w0 - s * w1;
-            cd[i][j][e] = apart ? p * w2 - s * w3 : s * w0 - p * w1;
+            float gm, gd;
+            logit_grad<sizeof(T) == 4>(cm[i][j][e], cd[i][j][e], top, e0, e1, e2, e3, gm, gd);
+            cm[i][j][e] = gm;
+            cd[i][j][e] = gd;
           }
       }
       if (yc >= 0 && yc < WTN) {
@@ -317,6 +349,22 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
           for (int e = 0; e < 16; ++e)
             if (j * 32 + 8 * (e / 4) + 4 * h + e % 4 == yc) cm[i][j][e] -= 1.f;
+      }
+      if constexpr (sizeof(T) == 4) {
+        if (row >= a.Tp) continue;
+        const int64_t o = (int64_t)row * a.C + c0 + 4 * h;
+#pragma clang loop unroll(full)
+        for (int j = 0; j < JN; ++j)
+#pragma clang loop unroll(full)
+          for (int g = 0; g < 4; ++g)
+            if (j * 32 + 8 * g < live) {   // (C is a multiple of 8)
+              auto four = [&](const f32x16_t& v) {
+                return none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+              };
+              *reinterpret_cast<float4*>((float*)a.gm + o + j * 32 + 8 * g) = four(cm[i][j]);
+              *reinterpret_cast<float4*>((float*)a.gd + o + j * 32 + 8 * g) = four(cd[i][j]);
+            }
+        continue;
       }
 #pragma clang loop unroll(full)
       for (int ch = 0; ch < 2; ++ch) {
@@ -331,7 +379,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
             *reinterpret_cast<uint2*>(stg + (lane & 31) * LD + j * 32 + 8 * g + 4 * h) = make_uint2(two(4 * g), two(4 * g + 2));
           }
         wave_lds_order();
-        bf16_t* o = ch ? a.gd : a.gm;
+        bf16_t* o = (bf16_t*)(ch ? a.gd : a.gm);
 #pragma clang loop unroll(full)
         for (int k = 0; k < 32 / RPS; ++k) {
           const int lr = k * RPS + lane / LPR, lc = 8 * (lane % LPR);
@@ -346,11 +394,11 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   }
 }
 
-template <int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN>
 void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
   const dim3 grid(ceil_div(a.C, BN) * ceil_div(a.T, BM)), block(64 * WM * WN);
-  if (grad) hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, true>), grid, block, 0, s, a, r);
-  else hipLaunchKernelGGL((head_logits_kernel<BM, BN, WM, WN, false>), grid, block, 0, s, a, r);
+  if (grad) hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, true>), grid, block, 0, s, a, r);
+  else hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, false>), grid, block, 0, s, a, r);
 }
 
 }  // namespace
@@ -375,13 +423,32 @@ HeadTile head_tile(int T_, int C) {
   return {32, 128, 32};
 }
 
+// fp32 models: this kernel takes the fp32 matrix instructions, the GEMM (gemm_f32.hip) products of
+// split operands, a tenth faster, on whole tiles of 128 rows, contractions cut where tiles are few; with it
+// the statistics are a launch more and the logits go through memory.  Estimates of both in us: the slices
+// of 16 k of the busiest compute unit at 613 GFLOP/s and a quarter for the rest, 8 for the joining launch;
+// 170 TFLOP/s and 24 for three launches.  Loss alone, us, here and there:
+//   1 x 32000 x 2048    158  300      64 x 32000 x 2048   235  292      128 x 32000 x 2048   413  301
+//   128 x 8192 x 512     39   51     256 x 8192 x 512      62   70      512 x 8192 x 512     111   94
+//   512 x 256 x 64       15   23       1 x 1024 x 1024     70   26     1024 x 1024 x 1024    63   73
+bool head_f32_fused(int T_, int C, int d) {
+  const HeadTile t = head_tile(T_, C);
+  const double wgs = (double)ceil_div(T_, t.BM) * ceil_div(C, t.BN), slice = (t.BM == 32 ? 4 : 3) * 2.0 * t.BM * t.BN * 16 / 613e3;
+  const double here = 1.25 * std::ceil(wgs / 256) * ceil_div(d, 16) * slice + 8;
+  const double there = 6.0 * ceil_div(T_, 128) * 128 * C * d / 170e6 + 24;
+  return here < there;
+}
+
+template <typename T>
 hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s) {
-  if (a.tile.BM == 256) launch_tile<256, 128, 4, 2>(a, r, grad, s);
-  else if (a.tile.BM == 128) launch_tile<128, 128, 2, 4>(a, r, grad, s);
-  else if (a.tile.BM == 64 && a.tile.BN == 128) launch_tile<64, 128, 2, 4>(a, r, grad, s);
-  else if (a.tile.BM == 64) launch_tile<64, 64, 2, 2>(a, r, grad, s);
-  else launch_tile<32, 128, 1, 4>(a, r, grad, s);
+  if (a.tile.BM == 256) launch_tile<T, 256, 128, 4, 2>(a, r, grad, s);
+  else if (a.tile.BM == 128) launch_tile<T, 128, 128, 2, 4>(a, r, grad, s);
+  else if (a.tile.BM == 64 && a.tile.BN == 128) launch_tile<T, 64, 128, 2, 4>(a, r, grad, s);
+  else if (a.tile.BM == 64) launch_tile<T, 64, 64, 2, 2>(a, r, grad, s);
+  else launch_tile<T, 32, 128, 1, 4>(a, r, grad, s);
   return hipGetLastError();
 }
+template hipError_t launch_head_logits<float>(const HeadLogits&, const HeadRows&, bool, hipStream_t);
+template hipError_t launch_head_logits<bf16_t>(const HeadLogits&, const HeadRows&, bool, hipStream_t);
 
 }  // namespace fdh

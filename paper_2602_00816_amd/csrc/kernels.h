@@ -322,8 +322,8 @@ struct HeadRows {        // per row of the batch: reference, four sums, target l
 };
 // targets of the rows of a [B, S] batch (IGNORE_LABEL: none)
 hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* lab, int T_, int S, int V, hipStream_t s);
-// fp32 models: statistics of the logits [T][C] of columns n0 .. n0 + C - 1, part [chunks][5][T] of
-// HEAD_CHUNK columns each, and the target logits of r
+// fp32 models with many rows: statistics of the logits [T][C] of columns n0 .. n0 + C - 1, part
+// [chunks][5][T] of HEAD_CHUNK columns each, and the target logits of r
 constexpr int HEAD_CHUNK = 4096;
 hipError_t launch_head_stats(const HeadRows& r, double* part, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt,
                              hipStream_t s);
@@ -347,25 +347,29 @@ hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, c
 // o [Tp][dm] = the rows of x that have a target, zeros elsewhere
 template <typename T>
 hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
-// bf16 models (head_gemm.hip): the product that forms columns n0 .. n0 + C - 1 of the logits, and
-// what its epilogue makes of them
+// head_gemm.hip: the product that forms columns n0 .. n0 + C - 1 of the logits, and what its epilogue
+// makes of them
 struct HeadTile {
   int BM, BN, group;       // rows and columns of a workgroup's tile, columns of a statistics group
 };
 struct HeadLogits {
-  const bf16_t *xm, *xd;   // [T][ldx]
+  const void *xm, *xd;     // [T][ldx], operand type
   int64_t ldx;
-  const bf16_t *wm, *wd;   // [C][d], the piece's rows
+  const void *wm, *wd;     // [C][d], the piece's rows
   int T, Tp, C, d, n0;
   const int32_t* tgt;      // [T]
-  float* part;             // statistics: [groups][5][T] (maximum and four sums), a group of HeadTile::group columns
+  void* part;              // statistics: [groups][5][T] (maximum and four sums), a group of HeadTile::group
+                           // columns, float32 (bf16 models) or float64
   float *lm, *ld;          // statistics: the logits too, [T][C], or null
-  bf16_t *gm, *gd;         // gradient: [Tp][C]
+  void *gm, *gd;           // gradient: [Tp][C], operand type
   HeadTile tile;           // head_tile
 };
 HeadTile head_tile(int T_, int C);
+// whether this product forms the logits of an fp32 model, or the GEMM
+bool head_f32_fused(int T_, int C, int d);
 // grad: the gradient of the losses, zeros in rows without a target and from T on; else
 // part, and the target logits of r
+template <typename T>
 hipError_t launch_head_logits(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t s);
 // head_thin.hip: both gradients for up to HEAD_THIN rows whose logits lm, ld [T][V] are in memory, dw
 // (rows of d) alpha_w times the half difference of its gradient (added with acc, float outputs), dx
