@@ -7,7 +7,7 @@
 namespace fdh {
 namespace {
 
-constexpr float HEAD_NEAR = 0.0625f;   // up to this |ld| the short series
+constexpr float HEAD_NEAR = 0.015625f;   // up to this |ld| the short series
 constexpr float FAR_APART = 0.5f;      // from this |ld| on: p and q in the place of a and s
 
 __device__ inline float head_ref(float lm, float ld) { return lm + fabsf(ld); }
@@ -27,12 +27,12 @@ __device__ inline float exp_fine(float x) {
 
 // a and s of one logit, see head.hip; for |ld| < 1/2.  In fp32: the exponential is common to both
 // points, to the rounding of an fp32 model with FINE.  The series' first omitted terms are below
-// 1e-10 (|ld| < 1/16) and 1e-8 of the sum.
+// 3e-9 (|ld| < 1/64) and 1e-8 of the sum.
 template <bool FINE>
-__device__ inline void pair_exp_near(float lm, float ld, float c, float& a, float& s) {   // |ld| < 1/16
+__device__ inline void pair_exp_near(float lm, float ld, float c, float& a, float& s) {   // |ld| < 1/64
   const float e = FINE ? exp_fine(lm - c) : __expf(lm - c), b2 = ld * ld;
-  a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24)));
-  s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120)));
+  a = fmaf(e, 0.5f * b2, e);
+  s = e * ld * fmaf(b2, 1.f / 6, 1.f);
 }
 template <bool FINE>
 __device__ inline void pair_exp(float lm, float ld, float c, float& a, float& s) {

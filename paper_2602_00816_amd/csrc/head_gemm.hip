@@ -222,9 +222,10 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       for (int j = 0; j < JN; ++j)
 #pragma clang loop unroll(full)
         for (int e = 0; e < 16; ++e) {
-          mx = fmaxf(mx, head_ref(cm[i][j][e], cd[i][j][e]));
+          mx = fmaxf(mx, cm[i][j][e]);
           far = fmaxf(far, fabsf(cd[i][j][e]));
         }
+      mx += far;   // (any reference that no logit of the row exceeds will do)
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       float za = 0.f, zs = 0.f;
       P zp = 0, zq = 0;
