@@ -158,6 +158,28 @@ def test_offsets_beyond_32_bits():
     assert float(hv[1:V - 2].abs().max()) == 0.0
 
 
+def test_a_batch_of_more_than_32_bits():
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    V, d, T = 24, 8200, 264000
+    m = _model(fd, "gpt2", V, d, "f32", max_seq=T)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    tok = torch.randint(0, V, (1, T), device="cuda", generator=g, dtype=torch.int32)
+    tok[0, -3:] = V - 1
+    dx = torch.randn(T, d, device="cuda", generator=g)
+    hv, pos = m.embed_backward(dx, tok)
+    assert torch.equal(pos[-5:], dx[-5:])
+    cols = torch.tensor([0, 1, 4095, 8199], device="cuda")
+    x = dx[:, cols].double().cpu()
+    want = torch.zeros(V, 4, dtype=torch.float64).index_add_(0, tok[0].cpu().long(), x)
+    size = torch.zeros(V, 4, dtype=torch.float64).index_add_(0, tok[0].cpu().long(), x.abs())
+    R.check(hv[:, cols], want, 2.0 ** -52 * T * size, "hv_e")
+    del hv, pos
+    e = torch.randn(V, d, device="cuda", generator=g)
+    y = m.embed_forward(tok, (e, None), positions=(dx, None))[0]
+    R.check(y[-4:], (e[tok[0, -4:].long()].double() + dx[-4:].double()).cpu(), torch.zeros(1, dtype=torch.float64), "x.m")
+
+
 def test_graph_and_stream():
     """Captured on a stream of its own and replayed over new inputs, with eager work between."""
     torch = need_gpu()

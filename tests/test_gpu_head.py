@@ -228,6 +228,42 @@ def test_no_rows():
     assert bool((dw == 1).all())
 
 
+@pytest.mark.parametrize("dtype,piece", [("bf16", 0), ("bf16", 131072), ("f32", 131072)])
+def test_offsets_beyond_32_bits(dtype, piece):
+    """More than 2^31 logits: the last rows and the last columns against the statement."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    T, V, d = 17000, 131072, 8
+    m = _model(fd, V, d, dtype)
+    x, w, tgt = _case(torch, T, V, d, dtype, 14, half=1e-2)
+    loss, dx, dw = m.head_grad(x, w, tgt, eps=EPS, piece=piece)
+    torch.cuda.synchronize()
+    # rows are independent of each other
+    rows = torch.cat([torch.arange(40), torch.arange(T - 90, T)]).cuda()
+    xs, ts = tuple(t[rows] for t in x), tgt[rows]
+    want, bound = R.head(xs, w, ts, 1.0, EPS), R.head_bound(xs, w, ts, 1.0, EPS)
+    for a, v, b, c in zip((*loss, *dx), (*want[0], *want[1]), (*bound[0], *bound[1]), ("loss.m", "loss.d", "dx.m", "dx.d")):
+        R.check(a[rows], v, b, c)
+    # the gradient of w at some of its rows, from the whole batch in float64 on the device
+    cols = torch.cat([torch.arange(30), torch.arange(V - 60, V)]).cuda()
+    live = (tgt != R.IGNORE).double()[:, None]
+    at = []
+    for sign in (1.0, -1.0):
+        xx, g = x[0].double() + sign * x[1].double(), torch.empty(T, len(cols), device="cuda", dtype=torch.float64)
+        ww = w[0].double() + sign * w[1].double()
+        for i in range(0, T, 2048):
+            g[i:i + 2048] = torch.softmax(xx[i:i + 2048] @ ww.T, -1)[:, cols]
+        g -= (tgt[:, None] == cols[None]).double()
+        at.append((g * live).T @ xx)
+    want = ((at[0] - at[1]) / (2 * EPS)).cpu()
+    got = R.f64(dw[cols])
+    # the product left out of the logits' mean (1e-2 of x times 1e-2 of w here) moves every probability
+    # by at most as much of itself
+    left = float((x[1].double() @ w[1][cols].double().T).abs().max())
+    assert left < 2e-3
+    assert float(torch.linalg.norm(got - want) / torch.linalg.norm(want)) <= 2 * R.half_step(x[0].dtype) + 1e-5 + left
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_graph_and_stream(dtype):
     torch = need_gpu()
