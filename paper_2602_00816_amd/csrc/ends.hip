@@ -239,6 +239,9 @@ int Engine::head_run(const HeadCall& c) {
     if (timing.on) CK(timing.end(st, 0, e0, gemm_flops(a[0]) + (n > 1 ? gemm_flops(a[1]) : 0.0), 0.0));
     return FDH_OK;
   };
+  const bool copy = c.grads && !k.thin && (c.copy_x || T_ != k.Tp);
+  HeadCopy cp{};
+  if (copy) cp = HeadCopy{ws + k.xm, ws + k.xd, xm, xd, ldx, T_, k.Tp, d, c.tgt};
   // the product that forms columns n0 .. n0 + C - 1 of the logits, for their statistics (keeping them, if
   // they are kept) or for their gradient
   auto logits = [&](int n0, int C, bool grad) -> int {
@@ -267,19 +270,14 @@ int Engine::head_run(const HeadCall& c) {
       h.lm = lm; h.ld = ld;
     }
     h.tile = tile;
+    if (n0 == 0 && !grad) h.copy = cp;
     int e0 = 0;
     if (timing.on) CK(timing.begin(st, &e0));
     CK(launch_head_logits<T>(h, r, grad, st));
     if (timing.on) CK(timing.end(st, 0, e0, 6.0 * T_ * C * d, 0.0));
     return FDH_OK;
   };
-  if (c.grads && !k.thin && (c.copy_x || T_ != k.Tp)) {
-    const PairT<T> o{(T*)(ws + k.xm), (T*)(ws + k.xd)};
-    CK(launch_head_copy<T>(o, xm, xd, ldx, T_, k.Tp, d, c.tgt, st));
-    xm = o.m;
-    xd = o.d;
-    ldx = d;
-  }
+  if (copy && !k.fused) CK(launch_head_copy<T>(cp, st));
   const HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss};
   for (int n0 = 0; n0 < V; n0 += k.C1) {
     const int C = std::min(k.C1, V - n0);
@@ -289,6 +287,11 @@ int Engine::head_run(const HeadCall& c) {
     typedef std::conditional_t<sizeof(T) == 4, double, float> P;
     if (!k.fused) CK(launch_head_stats(r, (double*)(ws + k.part), lm, ld, T_, C, n0, c.tgt, st));
     CK(launch_head_join(r, (const P*)(ws + k.part), (int)ceil_div(C, k.fused ? tile.group : HEAD_CHUNK), T_, c.tgt, n0 == 0, last, out, st));
+  }
+  if (copy) {   // (for the products: the statistics read x where it is)
+    xm = (const T*)cp.om;
+    xd = (const T*)cp.od;
+    ldx = d;
   }
   if (!c.grads) return FDH_OK;
   if (k.thin) {

@@ -13,8 +13,9 @@
 // A first pass over the pieces leaves c, the four sums and the target's logits of every row, a
 // second one forms the logits again and gives their gradient to the products: nothing of the
 // size of the logits stays.  Where one piece holds the vocabulary its logits are formed once.
+#include <algorithm>
+
 #include "head_dev.h"
-#include "kernels.h"
 
 namespace fdh {
 
@@ -91,23 +92,25 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, double* part
 }
 
 // Joins the groups' statistics of the rows to those of the pieces before: 256 / R threads per row
-// take every 256 / R-th group, then halves are joined until one is left.  After the last piece the
-// rows' losses and the factors of their gradients: a target outside the vocabulary makes its row
-// NaN, rows without a target have no loss and no gradient.
+// take every 256 / R-th group, each relative to its own maximum; then the row's maximum, and the sums
+// relative to it, across the wavefronts' lanes and the wavefronts (a fixed order).  After the last
+// piece the rows' losses and the factors of their gradients: a target outside the vocabulary makes
+// its row NaN, rows without a target have no loss and no gradient.
 template <int R, typename P>
 __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part, int groups, int T_, const int32_t* tgt, bool first,
                                                        bool last, HeadOut out) {
-  constexpr int L = NT / R;
-  __shared__ double sh[5][L][R];
-  const int lr = threadIdx.x % R, l = threadIdx.x / R;
+  constexpr int L = NT / R, W = NT / 64;
+  __shared__ double sh[W][R][5];
+  const int lr = threadIdx.x % R, l = threadIdx.x / R, w = threadIdx.x >> 6;
   const int64_t t = (int64_t)blockIdx.x * R + lr;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
   const bool on = y != IGNORE_LABEL;
   double top = -INFINITY, z[4] = {0.0, 0.0, 0.0, 0.0};
+  // sums at no maximum are NaN or nothing: their factor is 1
+  auto factor = [](double from, double to) { return from == to || from == -INFINITY ? 1.0 : exp(from - to); };
   auto join = [&](double m, double x0, double x1, double x2, double x3) {
     const double mx = fmax(top, m);
-    const double f = top == mx || top == -INFINITY ? 1.0 : exp(top - mx);
-    const double g = m == mx || m == -INFINITY ? 1.0 : exp(m - mx);   // (sums at no maximum are NaN or nothing)
+    const double f = factor(top, mx), g = factor(m, mx);
     z[0] = z[0] * f + x0 * g;
     z[1] = z[1] * f + x1 * g;
     z[2] = z[2] * f + x2 * g;
@@ -126,25 +129,33 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
       for (int u = 0; u < U; ++u)
         if (g0 + u * L < groups) join(v[u][0], v[u][1], v[u][2], v[u][3], v[u][4]);
     }
+    if (!first && l == 0) join(r.top[t], r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]);
   }
-  sh[0][l][lr] = top;
+  double mx = top;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
+  for (int o = R; o < 64; o <<= 1) mx = fmax(mx, __shfl_xor(mx, o, 64));
+  if (l % (64 / R) == 0) sh[w][lr][0] = mx;
   __syncthreads();
-  for (int n = L / 2; n > 0; n /= 2) {
-    if (l < n) {
-      join(sh[0][l + n][lr], sh[1][l + n][lr], sh[2][l + n][lr], sh[3][l + n][lr], sh[4][l + n][lr]);
-      sh[0][l][lr] = top;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sh[k + 1][l][lr] = z[k];
-    }
-    __syncthreads();
+  for (int q = 0; q < W; ++q) mx = fmax(mx, sh[q][lr][0]);
+  const double f0 = factor(top, mx);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    z[k] *= f0;
+#pragma unroll
+    for (int o = R; o < 64; o <<= 1) z[k] += __shfl_xor(z[k], o, 64);
+    if (l % (64 / R) == 0) sh[w][lr][k + 1] = z[k];
   }
+  __syncthreads();
   if (l != 0 || t >= T_) return;
-  if (on) {
-    if (!first) join(r.top[t], r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]);
-    r.top[t] = (float)top;   // (a maximum of floats)
+  top = mx;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    z[k] = sh[0][lr][k + 1];
+#pragma unroll
+    for (int q = 1; q < W; ++q) z[k] += sh[q][lr][k + 1];
   }
+  if (on) r.top[t] = (float)top;   // (a maximum of floats)
   if (!last) {
     if (on)
 #pragma unroll
@@ -215,19 +226,9 @@ __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r
   }
 }
 
-// x as the gradients' products read it: contiguous, with zeros in the rows that have no target
-// (whatever stands there) and in those behind the last
 template <typename T>
-__global__ __launch_bounds__(NT) void head_copy_kernel(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int dm,
-                                                       const int32_t* tgt) {
-  constexpr int VEC = 16 / sizeof(T);
-  const int64_t t = blockIdx.x;
-  const bool live = t < T_ && tgt[t] != IGNORE_LABEL;
-  for (int c = VEC * threadIdx.x; c < dm; c += VEC * NT) {
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    *reinterpret_cast<uint4*>(o.m + t * dm + c) = live ? *reinterpret_cast<const uint4*>(xm + t * ldx + c) : none;
-    *reinterpret_cast<uint4*>(o.d + t * dm + c) = live ? *reinterpret_cast<const uint4*>(xd + t * ldx + c) : none;
-  }
+__global__ __launch_bounds__(NT) void head_copy_kernel(HeadCopy c) {
+  copy_rows<T>(c, blockIdx.x, gridDim.x);
 }
 
 // bf16 copy of the fp32 pair [T][dm]
@@ -274,17 +275,15 @@ template hipError_t launch_head_dlogits<float>(PairT<float>, const HeadRows&, co
 template hipError_t launch_head_dlogits<bf16_t>(PairT<bf16_t>, const HeadRows&, const float*, const float*, int, int, int, int,
                                                 const int32_t*, hipStream_t);
 template <typename T>
-hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s) {
-  hipLaunchKernelGGL(head_copy_kernel<T>, dim3(Tp), dim3(NT), 0, s, o, xm, xd, ldx, T_, dm, tgt);
+hipError_t launch_head_copy(const HeadCopy& c, hipStream_t s) {
+  hipLaunchKernelGGL(head_copy_kernel<T>, dim3(std::min(c.Tp, 2048)), dim3(NT), 0, s, c);
   return hipGetLastError();
 }
+template hipError_t launch_head_copy<float>(const HeadCopy&, hipStream_t);
+template hipError_t launch_head_copy<bf16_t>(const HeadCopy&, hipStream_t);
 hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const float* d, int T_, int dm, hipStream_t s) {
   hipLaunchKernelGGL(head_round_kernel, dim3(T_), dim3(NT), 0, s, o, ldo, m, d, dm);
   return hipGetLastError();
 }
-
-template hipError_t launch_head_copy<float>(PairT<float>, const float*, const float*, int64_t, int, int, int, const int32_t*, hipStream_t);
-template hipError_t launch_head_copy<bf16_t>(PairT<bf16_t>, const bf16_t*, const bf16_t*, int64_t, int, int, int, const int32_t*,
-                                             hipStream_t);
 
 }  // namespace fdh

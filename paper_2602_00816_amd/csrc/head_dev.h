@@ -2,7 +2,7 @@
 #pragma once
 #include <type_traits>
 
-#include "common.h"
+#include "kernels.h"
 
 namespace fdh {
 namespace {
@@ -37,8 +37,9 @@ __device__ inline void pair_exp_near(float lm, float ld, float c, float& a, floa
 template <bool FINE>
 __device__ inline void pair_exp(float lm, float ld, float c, float& a, float& s) {
   const float e = FINE ? exp_fine(lm - c) : __expf(lm - c), b2 = ld * ld;
-  a = e * (1.f + b2 * (0.5f + b2 * (1.f / 24 + b2 * (1.f / 720 + b2 * (1.f / 40320)))));
-  s = e * ld * (1.f + b2 * (1.f / 6 + b2 * (1.f / 120 + b2 * (1.f / 5040))));
+  const bool near = fabsf(ld) < HEAD_NEAR;   // (a logit's value goes by itself alone: the short series where it serves)
+  a = near ? fmaf(e, 0.5f * b2, e) : e * (1.f + b2 * (0.5f + b2 * (1.f / 24 + b2 * (1.f / 720 + b2 * (1.f / 40320)))));
+  s = e * ld * (near ? fmaf(b2, 1.f / 6, 1.f) : 1.f + b2 * (1.f / 6 + b2 * (1.f / 120 + b2 * (1.f / 5040))));
 }
 // p and q of one logit: fp32 (bf16 models) or fp64
 __device__ inline void pair_exp_far(float lm, float ld, float c, float& p, float& q) {
@@ -66,6 +67,21 @@ __device__ inline void logit_grad(float lm, float ld, float c, double f0, double
     pair_exp<FINE>(lm, ld, c, a, s);
     gm = a * (float)f0 - s * (float)f1;
     gd = s * (float)f0 - a * (float)f1;
+  }
+}
+
+// x as the gradients' products read it: contiguous, with zeros in the rows that have no target
+// (whatever stands there) and in those behind the last; workgroup `block` of `blocks`
+template <typename T>
+__device__ inline void copy_rows(const HeadCopy& c, int block, int blocks) {
+  constexpr int VEC = 16 / sizeof(T);
+  for (int64_t t = block; t < c.Tp; t += blocks) {
+    const bool live = t < c.T && c.tgt[t] != IGNORE_LABEL;
+    for (int j = VEC * threadIdx.x; j < c.d; j += VEC * blockDim.x) {
+      const uint4 none = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>((T*)c.om + t * c.d + j) = live ? *reinterpret_cast<const uint4*>((const T*)c.xm + t * c.ldx + j) : none;
+      *reinterpret_cast<uint4*>((T*)c.od + t * c.d + j) = live ? *reinterpret_cast<const uint4*>((const T*)c.xd + t * c.ldx + j) : none;
+    }
   }
 }
 

@@ -12,7 +12,6 @@
 #include <type_traits>
 
 #include "head_dev.h"
-#include "kernels.h"
 
 namespace fdh {
 

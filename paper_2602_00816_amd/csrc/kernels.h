@@ -344,9 +344,17 @@ hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_
 template <typename T>
 hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
                                const int32_t* tgt, hipStream_t s);
-// o [Tp][dm] = the rows of x that have a target, zeros elsewhere
+// om, od [Tp][d] = the rows of x that have a target, zeros elsewhere
+struct HeadCopy {
+  void *om, *od;           // null: no copy
+  const void *xm, *xd;     // [T][ldx]
+  int64_t ldx;
+  int T, Tp, d;
+  const int32_t* tgt;
+};
 template <typename T>
-hipError_t launch_head_copy(PairT<T> o, const T* xm, const T* xd, int64_t ldx, int T_, int Tp, int dm, const int32_t* tgt, hipStream_t s);
+hipError_t launch_head_copy(const HeadCopy& c, hipStream_t s);
+
 // head_gemm.hip: the product that forms columns n0 .. n0 + C - 1 of the logits, and what its epilogue
 // makes of them
 struct HeadTile {
@@ -363,6 +371,7 @@ struct HeadLogits {
   float *lm, *ld;          // statistics: the logits too, [T][C], or null
   void *gm, *gd;           // gradient: [Tp][C], operand type
   HeadTile tile;           // head_tile
+  HeadCopy copy;           // made beside the tiles
 };
 HeadTile head_tile(int T_, int C);
 // whether this product forms the logits of an fp32 model, or the GEMM
