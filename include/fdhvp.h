@@ -335,7 +335,7 @@ fdh_status fdh_set_embed_scale(fdh_ctx* ctx, double scale);
  * points), B*S rows ldx elements apart, row t = scale e[token t] + p[t % S].  Tables and x
  * 16-byte aligned, ldx a multiple of 4; directions and tokens of any element alignment.
  * x overlaps neither an input nor itself.  A token outside [0, vocab) has no row: its
- * row of x is NaN.  Any B*S from 0 to 2^31 - 64; S <= max_seq for the GPT-2 family.
+ * row of x is NaN.  Any B*S from 0 to 2^28; S <= max_seq for the GPT-2 family.
  * Outputs are rounded once.  Only enqueued on the context stream (no wait, no
  * allocation: may be captured in a graph); one token is the call with B = S = 1. */
 fdh_status fdh_embed_forward(fdh_ctx* ctx, const fdh_embed_tables* tables, const int32_t* tokens_dev, int32_t B, int32_t S,

@@ -36,23 +36,23 @@ __device__ inline float4 row4(const bf16_t* p, int64_t i) {
 template <typename T>
 __global__ __launch_bounds__(NT) void embed_fwd_kernel(PairF x, int64_t ldx, const int32_t* tok, int64_t T_, int S, int dm, int V,
                                                        EmbedTables w, int lanes, int* bad_tok) {
-  const int64_t t = (int64_t)blockIdx.x * (NT / lanes) + threadIdx.x / lanes;
-  if (t >= T_) return;
-  const int tk = tok[t];
-  const bool bad = tk < 0 || tk >= V;
-  const int l = threadIdx.x % lanes;
-  if (bad && bad_tok && l == 0) bad_tok[0] = 1;
-  const T* e = (const T*)w.e + (bad ? 0 : (int64_t)tk * dm);
-  const float* ve = w.ve ? w.ve + (bad ? 0 : (int64_t)tk * dm) : nullptr;
-  const int64_t pr = w.p ? t % S * dm : 0;
-  for (int c = 4 * l; c < dm; c += 4 * lanes) {
-    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 a = row4(e, c), va = ve ? row4(ve, c) : none;
-    const float4 b = w.p ? row4((const T*)w.p, pr + c) : none, vb = w.vp ? row4(w.vp, pr + c) : none;
-    auto mean = [&](float p, float q) { return bad ? __builtin_nanf("") : (float)(w.scale * (double)p + (double)q); };
-    auto half = [&](float p, float q) { return bad ? __builtin_nanf("") : (float)(w.eps * (w.scale * (double)p + (double)q)); };
-    put4(x.m, t * ldx + c, mean(a.x, b.x), mean(a.y, b.y), mean(a.z, b.z), mean(a.w, b.w));
-    put4(x.d, t * ldx + c, half(va.x, vb.x), half(va.y, vb.y), half(va.z, vb.z), half(va.w, vb.w));
+  const int per = NT / lanes, l = threadIdx.x % lanes;
+  for (int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / lanes; t < T_; t += (int64_t)gridDim.x * per) {
+    const int tk = tok[t];
+    const bool bad = tk < 0 || tk >= V;
+    if (bad && bad_tok && l == 0) bad_tok[0] = 1;
+    const T* e = (const T*)w.e + (bad ? 0 : (int64_t)tk * dm);
+    const float* ve = w.ve ? w.ve + (bad ? 0 : (int64_t)tk * dm) : nullptr;
+    const int64_t pr = w.p ? t % S * dm : 0;
+    for (int c = 4 * l; c < dm; c += 4 * lanes) {
+      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 a = row4(e, c), va = ve ? row4(ve, c) : none;
+      const float4 b = w.p ? row4((const T*)w.p, pr + c) : none, vb = w.vp ? row4(w.vp, pr + c) : none;
+      auto mean = [&](float p, float q) { return bad ? __builtin_nanf("") : (float)(w.scale * (double)p + (double)q); };
+      auto half = [&](float p, float q) { return bad ? __builtin_nanf("") : (float)(w.eps * (w.scale * (double)p + (double)q)); };
+      put4(x.m, t * ldx + c, mean(a.x, b.x), mean(a.y, b.y), mean(a.z, b.z), mean(a.w, b.w));
+      put4(x.d, t * ldx + c, half(va.x, vb.x), half(va.y, vb.y), half(va.z, vb.z), half(va.w, vb.w));
+    }
   }
 }
 
@@ -479,8 +479,9 @@ hipError_t launch_embed_fwd(PairF x, int64_t ldx, const int32_t* tok, int64_t T_
   if (T_ == 0) return hipSuccess;
   int lanes = 2;
   while (lanes < NT && 4 * lanes < dm) lanes *= 2;
-  hipLaunchKernelGGL((embed_fwd_kernel<T>), dim3(ceil_div(T_, NT / lanes)), dim3(NT), 0, s, x, ldx, tok, T_, S, dm, V, w, lanes,
-                     bad_tok);
+  // (a launch ends at 2^32 threads)
+  const dim3 grid((unsigned)std::min<int64_t>(1 << 22, ceil_div(T_, NT / lanes)));
+  hipLaunchKernelGGL((embed_fwd_kernel<T>), grid, dim3(NT), 0, s, x, ldx, tok, T_, S, dm, V, w, lanes, bad_tok);
   return hipGetLastError();
 }
 template hipError_t launch_embed_fwd<float>(PairF, int64_t, const int32_t*, int64_t, int, int, int, const EmbedTables&, int*, hipStream_t);

@@ -24,7 +24,7 @@ namespace fdh {
 int Engine::embed_check(const int32_t* tok, int B, int S) {
   if (quad) { err = "needs a language-model context"; return FDH_ERR_UNSUPPORTED; }
   if (B < 0 || S < 0) { err = "B and S must not be negative"; return FDH_ERR_INVALID_ARG; }
-  if ((int64_t)B * S > END_MAX_TOKENS) { err = "B*S must be <= 2^31 - 64"; return FDH_ERR_UNSUPPORTED; }
+  if ((int64_t)B * S > END_MAX_TOKENS) { err = "B*S must be <= 2^28"; return FDH_ERR_UNSUPPORTED; }
   if (gpt2 && S > Smax) { err = "S must be <= max_seq"; return FDH_ERR_INVALID_ARG; }
   if ((int64_t)B * S > 0 && (!tok || (uintptr_t)tok % 4)) { err = "tokens: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
   return FDH_OK;
@@ -96,6 +96,8 @@ constexpr int64_t HEAD_PIECE_ELEMS = (int64_t)64 << 20;
 // bytes of statistics of column groups that are aimed at where no gradient takes more
 constexpr size_t HEAD_PART = (size_t)64 << 20;
 constexpr int HEAD_PIECE_ROUND = 256, HEAD_PIECE_MIN = 1024;
+// most elements of a launch's logits (2^20 of the largest tiles, 2^29 threads)
+constexpr int64_t HEAD_LAUNCH_ELEMS = (int64_t)1 << 35;
 // scratch that the plan of a split contraction may take
 constexpr size_t HEAD_SPLIT = (size_t)512 << 20;
 
@@ -145,6 +147,7 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   };
   const size_t ob = bf16 ? 2 : 4, t = (size_t)T_;
   c.Tp = (int)((t + 7) / 8 * 8);
+  if (piece > 0) piece = (int)std::min<int64_t>(piece, HEAD_LAUNCH_ELEMS / std::max(1, T_));
   c.thin = grads && T_ <= HEAD_THIN;   // (no more logits than w has rows 8 wide)
   const bool whole = c.thin || (piece > 0 ? piece >= V : (int64_t)T_ * V <= HEAD_PIECE_ELEMS);
   int64_t C = piece > 0 ? piece : std::max<int64_t>(HEAD_PIECE_MIN, HEAD_PIECE_ELEMS / std::max(1, T_) / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND);
@@ -170,7 +173,8 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   size_t part = (size_t)ceil_div(c.C, HEAD_CHUNK) * pb * t;
   if (c.fused) {
     const size_t col = std::max<size_t>(1, t * pb / tile.group), room = std::max<size_t>(2 * gb, piece > 0 ? 0 : HEAD_PART);
-    c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, room / col / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
+    const size_t fit = std::min<size_t>(room / col, HEAD_LAUNCH_ELEMS / std::max<size_t>(1, t));
+    c.C1 = (int)std::min<size_t>(V, std::max<size_t>(c.C, fit / HEAD_PIECE_ROUND * HEAD_PIECE_ROUND));
     part = (size_t)ceil_div(c.C1, tile.group) * pb * t;
   }
   c.gm = take(gb);

@@ -284,7 +284,9 @@ hipError_t launch_count_targets(int64_t* out3, const int32_t* tok, const int32_t
 
 // ---- embed.hip: token embedding and the gradients of its tables -----------------------
 // (v, hv and dx of any element alignment; the tables' rows 16-byte aligned)
-constexpr int64_t END_MAX_TOKENS = ((int64_t)1 << 31) - 64;
+// (the sums' launch, 4 threads a token and 1024 columns, stays below 2^32 threads for all that fits
+// into 288 GB)
+constexpr int64_t END_MAX_TOKENS = (int64_t)1 << 28;
 struct EmbedTables {
   const void* e;        // [V][dm], operand type
   const float* ve;      // its direction or null

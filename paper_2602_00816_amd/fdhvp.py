@@ -717,7 +717,7 @@ class Model:
         import torch
         dev, T, inp = self._head_inputs(x, w, targets, piece)
         if out is None:
-            out = tuple(torch.empty(T, device=targets.device) for _ in range(2))
+            out = tuple(torch.empty(T, dtype=torch.float32, device=targets.device) for _ in range(2))
         lm, ld = self._head_loss_out(out, T, dev)
         if scratch is None:
             scratch = self.head_scratch(T, piece, grads=False)
@@ -743,7 +743,7 @@ class Model:
         if gt is not dt and gt is not f32:
             raise ValueError(f"gradients must have dtype {dt} or {f32}")
         if loss is None:
-            loss = tuple(torch.empty(T, device=targets.device) for _ in range(2))
+            loss = tuple(torch.empty(T, dtype=torch.float32, device=targets.device) for _ in range(2))
         if dx is None:
             dx = tuple(torch.empty((T, d), dtype=gt, device=targets.device) for _ in range(2))
         if dw is None:

@@ -238,3 +238,16 @@ def test_vocab_piece_plan():
     assert lib.fdh_set_vocab_piece(m._h, -1) == INVALID and total(m, 4, 2048) == small
     assert lib.fdh_set_vocab_piece(m._h, 0) == 0 and total(m, 4, 2048) == whole
     assert lib.fdh_set_vocab_piece(fd.Model("quad_diag", quad_n=10)._h, 256) == UNSUPPORTED
+
+
+def test_ends_stay_below_the_largest_launch():
+    """Sizes whose one launch would pass 2^32 threads: refused (tokens), or cut in pieces (logits)."""
+    lib, n = fd.lib(), C.c_size_t()
+    m = fd.Model("llama", 0, 8, 1, 1, 8, 262136, 2, "bf16")
+    assert lib.fdh_embed_scratch_bytes(m._h, 1 << 14, 1 << 14, C.byref(n)) == 0
+    assert lib.fdh_embed_scratch_bytes(m._h, 1, (1 << 28) + 1, C.byref(n)) == UNSUPPORTED
+    T = 1 << 20
+    assert lib.fdh_head_scratch_bytes(m._h, T, 262136, 0, C.byref(n)) == 0
+    pieces = n.value
+    assert lib.fdh_head_scratch_bytes(m._h, T, 1 << 15, 0, C.byref(n)) == 0 and n.value == pieces   # 2^35 logits
+    assert lib.fdh_head_scratch_bytes(m._h, T, 1 << 14, 0, C.byref(n)) == 0 and n.value < pieces

@@ -286,3 +286,20 @@ def test_scale_in_the_gpt2_hvp():
     m.set_workspace(3, 16)
     got = m.hvp(torch.from_numpy(th32).cuda(), torch.from_numpy(v.astype(np.float32)).cuda(), EPS, torch.from_numpy(tok).cuda())
     assert rel_l2(got.cpu().numpy(), want) < 1e-4
+
+
+def test_more_rows_than_one_launch_has_workgroups():
+    """Four million rows and some: rows around the end of the first sweep, and the last ones."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    V, d, T = 64, 520, (1 << 22) + 300
+    m = _model(fd, "llama", V, d, "bf16")
+    g = torch.Generator().manual_seed(6)
+    table, v = torch.randn(V, d, generator=g).to(torch.bfloat16).cuda(), torch.randn(V, d, generator=g).cuda()
+    tok = torch.randint(0, V, (2, T // 2), generator=g, dtype=torch.int32).cuda()
+    tok[0, 3] = V
+    y, yd = m.embed_forward(tok, (table, v))
+    flat = tok.view(-1).long()
+    for r in (slice(0, 3), slice((1 << 22) - 200, T)):
+        assert torch.equal(y[r], table[flat[r]].float()) and torch.equal(yd[r], v[flat[r]])
+    assert bool(y[3].isnan().all()) and int(y[:, 0].isnan().sum()) == 1
