@@ -98,9 +98,10 @@ struct WsLayout {
 struct HeadCarve {
   int C = 0, C1 = 0, Tp = 0;   // columns of a piece, and in the first pass; rows of the logits' gradient (multiple of 8)
   bool keep = false;           // one piece, whose logits are formed once
+  bool order = false;          // rows without a target after the others
   bool thin = false;           // both gradients in one pass over w
   bool fused = true;           // logits on head_gemm.hip, else on the GEMM (fp32 models, many rows)
-  size_t top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, runs, split, split_bytes, total;
+  size_t rows, top, z, ym, f, lm, ld, part, gm, gd, xm, xd, dm, dd, runs, split, split_bytes, total;
 };
 struct HeadCall {
   const void *x_m = nullptr, *x_d = nullptr;   // [T][ldx], operand type

@@ -32,6 +32,33 @@ __global__ void head_targets_kernel(int32_t* tgt, const int32_t* tok, const int3
   tgt[t] = y == IGNORE_LABEL ? y : min(max(y, 0), V - 1);
 }
 
+// One workgroup: a thread counts a run of rows, the runs' counts are added up over the threads.
+constexpr int RT = 1024;
+__global__ __launch_bounds__(RT) void head_rows_kernel(int32_t* rows, const int32_t* tgt, int T_) {
+  __shared__ int sh[RT / 64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int per = (T_ + RT - 1) / RT, from = min((int)threadIdx.x * per, T_), end = min(from + per, T_);
+  int n = 0;
+  for (int t = from; t < end; ++t) n += tgt[t] != IGNORE_LABEL;
+  int at = n;   // inclusive over the wavefront's lanes
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(at, o, 64);
+    if (lane >= o) at += y;
+  }
+  if (lane == 63) sh[w] = at;
+  __syncthreads();
+  int all = 0;
+  at -= n;
+  for (int q = 0; q < RT / 64; ++q) {
+    if (q < w) at += sh[q];
+    all += sh[q];
+  }
+  int none = all + from - at;   // (of the rows before, from - at have no target)
+  for (int t = from; t < end; ++t) rows[tgt[t] != IGNORE_LABEL ? at++ : none++] = t;
+  if (threadIdx.x == 0) rows[T_] = all;
+}
+
 // Statistics of one piece of the logits (fp32 models, many rows), part [chunks][5][T]: the maximum and the four
 // sums of a row's CHUNK columns, one workgroup each; every thread keeps its sums relative to its own
 // maximum.
@@ -246,6 +273,10 @@ __global__ __launch_bounds__(NT) void head_round_kernel(PairT<bf16_t> o, int64_t
 
 hipError_t launch_head_targets(int32_t* tgt, const int32_t* tok, const int32_t* lab, int T_, int S, int V, hipStream_t s) {
   hipLaunchKernelGGL(head_targets_kernel, dim3(ceil_div(T_, NT)), dim3(NT), 0, s, tgt, tok, lab, T_, S, V);
+  return hipGetLastError();
+}
+hipError_t launch_head_rows(int32_t* rows, const int32_t* tgt, int T_, hipStream_t s) {
+  hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(RT), 0, s, rows, tgt, T_);
   return hipGetLastError();
 }
 hipError_t launch_head_stats(const HeadRows& r, double* part, const float* lm, const float* ld, int T_, int C, int n0, const int32_t* tgt,

@@ -67,8 +67,24 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   __shared__ __attribute__((aligned(1024))) char st1[STAGE];
   __shared__ __attribute__((aligned(1024))) char st2[STAGE];
 
-  const int gx = (a.C + BN - 1) / BN, gy = (a.T + BM - 1) / BM;
-  if ((int)blockIdx.x >= gx * gy) return copy_rows<T>(a.copy, blockIdx.x - gx * gy, gridDim.x - gx * gy);
+  const int gx = (a.C + BN - 1) / BN, tiles = gx * ((a.T + BM - 1) / BM);
+  if ((int)blockIdx.x >= tiles) return copy_rows<T>(a.copy, blockIdx.x - tiles, gridDim.x - tiles);
+  // rows without a target come last, and tiles that hold no other are not formed
+  const int live_rows = a.rows ? a.rows[a.T] : a.T, gy = (live_rows + BM - 1) / BM;
+  auto at = [&](int row) { return a.rows && row < a.T ? a.rows[row] : row; };
+  if ((int)blockIdx.x >= gx * gy) {
+    if constexpr (GRAD) {
+      const int q = blockIdx.x - gx * gy, c = q % gx * BN, n = min(BN, a.C - c) / CE, end = min((gy + q / gx + 1) * BM, a.Tp);
+      for (int row = (gy + q / gx) * BM + (int)threadIdx.x / (BN / CE); row < end; row += 64 * NW / (BN / CE)) {
+        const int i = threadIdx.x % (BN / CE);
+        if (i >= n) continue;
+        const int64_t o = (int64_t)at(row) * a.C + c + CE * i;
+        *reinterpret_cast<uint4*>((T*)a.gm + o) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>((T*)a.gd + o) = make_uint4(0, 0, 0, 0);
+      }
+    }
+    return;
+  }
   const int lin = xcd_order(blockIdx.x, gx * gy);
   // tiles run down 4 tile rows before the next column (an XCD's tiles share 4 row and 8 column blocks)
   constexpr int GM = 4;
@@ -97,8 +113,10 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
     const int64_t ld = isx ? a.ldx : a.d;
     const int first = isx ? m0 : n0, end = isx ? a.T : a.C;
     const T* p = (const T*)(isx ? (half ? a.xd : a.xm) : (half ? a.wd : a.wm));
-    base[u] = p + first * ld;
-    vo[u] = (uint32_t)sizeof(T) * (uint32_t)((min(first + row, end - 1) - first) * ld + CE * ck);
+    const bool moved = isx && a.rows;   // (all of x within 31 bits)
+    const int src = min(first + row, end - 1);
+    base[u] = moved ? p : p + first * ld;
+    vo[u] = (uint32_t)sizeof(T) * (uint32_t)((moved ? at(src) : src - first) * ld + CE * ck);
   }
   auto stage = [&](auto s) -> char* {
     constexpr int S = decltype(s)::value % 3;
@@ -217,7 +235,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
     }
 #pragma clang loop unroll(full)
     for (int i = 0; i < IM; ++i) {
-      const int row = m0 + wm * WTM + i * 32 + (lane & 31);
+      const int place = m0 + wm * WTM + i * 32 + (lane & 31), row = at(place);
       float mx = -INFINITY, far = 0.f;
 #pragma clang loop unroll(full)
       for (int j = 0; j < JN; ++j)
@@ -262,7 +280,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       P z[4] = {za, zs, zp, zq};
 #pragma clang loop unroll(full)
       for (int k = 0; k < 4; ++k) z[k] += __shfl_xor(z[k], 32, 64);
-      if (row >= a.T) continue;
+      if (place >= a.T) continue;
       if (a.lm) {   // (one piece: kept for its gradient)
         const int64_t o = (int64_t)row * a.C + c0 + 4 * h;
 #pragma clang loop unroll(full)
@@ -308,7 +326,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
 #pragma clang loop unroll(full)
     for (int i = 0; i < IM; ++i) {
       const int rb = m0 + wm * WTM + i * 32;
-      const int row = rb + (lane & 31);
+      const int row = at(rb + (lane & 31));
       const int t = min(row, a.T - 1);
       const int y = row < a.T ? a.tgt[t] : IGNORE_LABEL;
       const bool none = y == IGNORE_LABEL;
@@ -388,7 +406,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
           const uint2* p = reinterpret_cast<const uint2*>(stg + lr * LD + lc);
           const uint2 u = p[0], v = p[1];
           if (rb + lr < a.Tp && lc < live)   // (C is a multiple of 8)
-            *reinterpret_cast<uint4*>(o + (int64_t)(rb + lr) * a.C + c0 + lc) = make_uint4(u.x, u.y, v.x, v.y);
+            *reinterpret_cast<uint4*>(o + (int64_t)at(rb + lr) * a.C + c0 + lc) = make_uint4(u.x, u.y, v.x, v.y);
         }
         wave_lds_order();   // the next writes come after these reads
       }
@@ -416,8 +434,9 @@ void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t 
 //   256 x 4096 x 512                      29       23      19     18      20
 //   512 x 4096 x 512                      30       26      24     26      29
 //   1024 x 4096 x 512                     31       28      32     34      40
-// (256 x 128 on four wavefronts of 128 x 64, and 128 x 256, are 1 to 5% slower than eight of 64 x 64
-// at 8192 x 32000 x 2048.)
+// (1 x 32000 x 2048 on weights that no cache holds: 60; 62 and 64 with tiles of 32 x 64 and 32 x 32.
+// 256 x 128 on four wavefronts of 128 x 64, and 128 x 256, are 1 to 5% slower than eight of 64 x 64 at
+// 8192 x 32000 x 2048.)
 HeadTile head_tile(int T_, int C) {
   auto fills = [&](int bm, int bn) { return T_ > bm / 2 && (int64_t)ceil_div(T_, bm) * ceil_div(C, bn) >= 192; };
   if (fills(256, 128)) return {256, 128, 64};

@@ -346,6 +346,9 @@ hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_
 template <typename T>
 hipError_t launch_head_dlogits(PairT<T> o, const HeadRows& r, const float* lm, const float* ld, int T_, int Tp, int C, int n0,
                                const int32_t* tgt, hipStream_t s);
+// rows [T + 1] = the rows that have a target in their order, then those that have none; behind them how
+// many have one
+hipError_t launch_head_rows(int32_t* rows, const int32_t* tgt, int T_, hipStream_t s);
 // om, od [Tp][d] = the rows of x that have a target, zeros elsewhere
 struct HeadCopy {
   void *om, *od;           // null: no copy
@@ -374,6 +377,7 @@ struct HeadLogits {
   void *gm, *gd;           // gradient: [Tp][C], operand type
   HeadTile tile;           // head_tile
   HeadCopy copy;           // made beside the tiles
+  const int32_t* rows;     // launch_head_rows' order, or null: the batch's own
 };
 HeadTile head_tile(int T_, int C);
 // whether this product forms the logits of an fp32 model, or the GEMM

@@ -364,3 +364,50 @@ def test_from_tokens_to_losses_and_back():
     assert float(torch.linalg.norm(R.f64(hv) - diff) / torch.linalg.norm(diff)) < 2 * q + 3e-6
     assert abs(float(loss[0].double().sum() / n) - float(lp + ln) / 2) < 2 * q
     assert abs(float(loss[1].double().sum() / n) - float(lp - ln) / 2) < (4 * q + 1e-5) * abs(float(lp - ln))
+
+
+@pytest.mark.parametrize("T,V,d,pad,dtype,piece", [
+    (1100, 8192, 4096, 8, "bf16", 0), (1100, 8192, 4096, 0, "bf16", 1000), (1100, 8192, 4096, 0, "bf16", 8192),
+    (517, 12008, 4104, 0, "bf16", 4096), (60, 262136, 2048, 0, "f32", 65536)])
+def test_large_batches_skip_rows_without_a_target(T, V, d, pad, dtype, piece):
+    """Large enough that only the rows with a target are multiplied: the others may hold anything, and no row's
+    result depends on which of the others have a target."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    m = _model(fd, V, d, dtype)
+    x, w, full = _case(torch, T, V, d, dtype, 15, pad=pad, ignore=0.0)
+    dt = torch.float32
+
+    def run(x, tgt):
+        dx = tuple(torch.full((T, d), 5.0, dtype=dt, device="cuda") for _ in range(2))
+        got = m.head_grad(x, w, tgt, eps=EPS, piece=piece, dx=dx, dw=torch.full((V, d), 5.0, dtype=dt, device="cuda"))
+        alone = m.head_loss(x, w, tgt, piece=piece)
+        torch.cuda.synchronize()
+        for q in (0, 1):
+            R.check(alone[q], R.f64(got[0][q]), R.f64(got[0][q]).abs() * 1e-6 + 1e-6, "loss alone")
+        return got
+
+    whole = run(x, full)
+    g = torch.Generator().manual_seed(16)
+    t = torch.arange(T)
+    masks = {"scattered": torch.rand(T, generator=g) < 0.3, "most": torch.rand(T, generator=g) < 0.9, "the end": t >= T // 3,
+             "the start": t < T - 7, "all but one": t != T // 2, "all": t >= 0}
+    for name, none in masks.items():
+        say(f"T {T} V {V} d {d} {dtype} piece {piece} without a target: {name}")
+        none = none.cuda()
+        tgt = torch.where(none, torch.full_like(full, R.IGNORE), full)
+        dirty = tuple(torch.where(none[:, None], torch.full_like(a, float("nan")), a) for a in x)
+        loss, dx, dw = run(dirty, tgt)
+        for a, b in zip((*loss, *dx), (*whole[0], *whole[1])):
+            assert torch.equal(a[~none], b[~none]) and float(a[none].abs().sum()) == 0.0
+        assert bool(torch.isfinite(dw).all())
+        if name == "all":
+            assert float(dw.abs().max()) == 0.0
+        if name == "all but one":
+            # dw of one row: its gradient's outer products
+            r = T // 2
+            one = m.head_grad(tuple(a[r:r + 1] for a in x), w, full[r:r + 1].contiguous(), eps=EPS,
+                              dw=torch.empty(V, d, device="cuda"))[2]
+            assert float(torch.linalg.norm(dw - one) / torch.linalg.norm(one)) <= 2 * R.half_step(x[0].dtype) + 1e-5
+        if name == "scattered" and dtype == "bf16" and piece == 0:
+            R.check_head((loss, dx, dw), x, w, tgt, 1.0, EPS, "scattered")
