@@ -102,6 +102,8 @@ constexpr int64_t HEAD_LAUNCH_ELEMS = (int64_t)1 << 35;
 // of 5 us, of some 150 here), so that only the others are multiplied: 2500 x 32000 x 1024, of which 30%
 // have none: 462 -> 349 us.
 constexpr double HEAD_ORDER_OPS = 1.5e11;
+// rows up to which the target's logits are formed in fp64 and x_d w_d is never left out
+constexpr int HEAD_FINE_ROWS = 32;
 // scratch that the plan of a split contraction may take
 constexpr size_t HEAD_SPLIT = (size_t)512 << 20;
 
@@ -120,21 +122,24 @@ GemmOperand mnmaj(const void* p, int64_t ld) {
   return o;
 }
 
+// products of the mean's logits on the GEMM: x_d w_d too for few rows
+int logit_pairs(int T_) { return T_ <= HEAD_FINE_ROWS ? 2 : 1; }
+
 // scratch of the products of a piece of C columns: those that its gradient goes to and, unless fused, its logits'
 template <typename T>
 size_t piece_split(int T_, int Tp, int C, int d, bool grads, bool fused) {
   GemmArgs g[2];
-  auto need = [&](int M, int N, int K, int n) {
+  auto need = [&](int M, int N, int K, int n, int mean_pairs = 1) {
     for (int p = 0; p < 2; ++p) {
       g[p].M = M;
       g[p].N = N;
       g[p].K = K;
       g[p].ldc = N;
-      g[p].npairs = 2 - p;
+      g[p].npairs = p ? mean_pairs : 2;
     }
     return gemm_scratch<T>(g, n, HEAD_SPLIT);
   };
-  size_t mx = fused ? 0 : need(T_, C, d, 2);
+  size_t mx = fused ? 0 : need(T_, C, d, 2, logit_pairs(T_));
   if (grads) mx = std::max(mx, std::max(need(T_, d, C, 2), need(C, d, Tp, 1)));
   return mx;
 }
@@ -268,7 +273,9 @@ int Engine::head_run(const HeadCall& c) {
       a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(wm + (int64_t)n0 * d, d);
       a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(wd + (int64_t)n0 * d, d);
       a[0].C = ld;
+      a[1].npairs = logit_pairs(T_);
       a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(wm + (int64_t)n0 * d, d);
+      a[1].A[1] = kmaj(xd, ldx); a[1].B[1] = kmaj(wd + (int64_t)n0 * d, d);
       a[1].C = lm;
       return product(a, 2);
     }
@@ -293,7 +300,11 @@ int Engine::head_run(const HeadCall& c) {
   };
   if (rows) CK(launch_head_rows(rows, c.tgt, T_, st));
   if (copy && !k.fused) CK(launch_head_copy<T>(cp, st));
-  const HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss};
+  HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss, nullptr, nullptr, ldx, wm, wd, d};
+  if (T_ <= HEAD_FINE_ROWS) {
+    out.xm = xm;
+    out.xd = xd;
+  }
   for (int n0 = 0; n0 < V; n0 += k.C1) {
     const int C = std::min(k.C1, V - n0);
     const int rc = logits(n0, C, false);

@@ -14,6 +14,7 @@
 // second one forms the logits again and gives their gradient to the products: nothing of the
 // size of the logits stays.  Where one piece holds the vocabulary its logits are formed once.
 #include <algorithm>
+#include <type_traits>
 
 #include "head_dev.h"
 
@@ -118,16 +119,34 @@ __global__ __launch_bounds__(NT) void head_stats_kernel(HeadRows r, double* part
   }
 }
 
+__device__ inline void wide(const float* p, double (&v)[4]) {
+  const float4 u = *reinterpret_cast<const float4*>(p);
+  v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+}
+__device__ inline void wide(const bf16_t* p, double (&v)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = __uint_as_float(x[k] << 16);
+    v[2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
+  }
+}
+
 // Joins the groups' statistics of the rows to those of the pieces before: 256 / R threads per row
 // take every 256 / R-th group, each relative to its own maximum; then the row's maximum, and the sums
 // relative to it, across the wavefronts' lanes and the wavefronts (a fixed order).  After the last
 // piece the rows' losses and the factors of their gradients: a target outside the vocabulary makes
-// its row NaN, rows without a target have no loss and no gradient.
+// its row NaN, rows without a target have no loss and no gradient.  loss.d is the difference of a mean
+// over the vocabulary, whose errors average out, and the target's ld_y, whose error stands alone:
+// of a few rows it may be all that they hold, so there the target's logits are formed in fp64 (1 row of
+// 32000 x 2048 bf16 whose loss.d is a fifth of ld's spread: 2e-6 of it off before).
 template <int R, typename P>
 __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part, int groups, int T_, const int32_t* tgt, bool first,
                                                        bool last, HeadOut out) {
   constexpr int L = NT / R, W = NT / 64;
-  __shared__ double sh[W][R][5];
+  typedef std::conditional_t<sizeof(P) == 8, float, bf16_t> T;
+  __shared__ double sh[W][R][7];
   const int lr = threadIdx.x % R, l = threadIdx.x / R, w = threadIdx.x >> 6;
   const int64_t t = (int64_t)blockIdx.x * R + lr;
   const int y = t < T_ ? tgt[t] : IGNORE_LABEL;
@@ -158,6 +177,25 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
     }
     if (!first && l == 0) join(r.top[t], r.z[0][t], r.z[1][t], r.z[2][t], r.z[3][t]);
   }
+  double ym = 0.0, yd = 0.0;
+  const bool fine = R == 1 && last && out.xm;
+  if (fine && on && y >= 0 && y < out.V) {
+    constexpr int VEC = 16 / sizeof(T);
+    const T *xm = (const T*)out.xm + t * out.ldx, *xd = (const T*)out.xd + t * out.ldx;
+    const T *wm = (const T*)out.wm + (int64_t)y * out.d, *wd = (const T*)out.wd + (int64_t)y * out.d;
+    for (int j = VEC * l; j < out.d; j += VEC * NT) {
+      double a[VEC], b[VEC], p[VEC], q[VEC];
+      wide(xm + j, a);
+      wide(xd + j, b);
+      wide(wm + j, p);
+      wide(wd + j, q);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        ym += a[e] * p[e] + b[e] * q[e];
+        yd += b[e] * p[e] + a[e] * q[e];
+      }
+    }
+  }
   double mx = top;
 #pragma unroll
   for (int o = R; o < 64; o <<= 1) mx = fmax(mx, __shfl_xor(mx, o, 64));
@@ -172,6 +210,17 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
 #pragma unroll
     for (int o = R; o < 64; o <<= 1) z[k] += __shfl_xor(z[k], o, 64);
     if (l % (64 / R) == 0) sh[w][lr][k + 1] = z[k];
+  }
+  if (fine) {
+#pragma unroll
+    for (int o = R; o < 64; o <<= 1) {
+      ym += __shfl_xor(ym, o, 64);
+      yd += __shfl_xor(yd, o, 64);
+    }
+    if (l % (64 / R) == 0) {
+      sh[w][lr][5] = ym;
+      sh[w][lr][6] = yd;
+    }
   }
   __syncthreads();
   if (l != 0 || t >= T_) return;
@@ -196,8 +245,19 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
     const double sa = z[0], ss = z[1], sp = z[2], sq = z[3];
     const double zp = sa + ss + sp, zn = sa - ss + sq, zm = sa + 0.5 * (sp + sq), zd = ss + 0.5 * (sp - sq);
     const double lp = log(zp), ln = log(zn);
-    m = top - (double)r.ym[t] + 0.5 * (lp + ln);
-    d = (fabs(zd) < 0.5 * zm ? atanh(zd / zm) : 0.5 * (lp - ln)) - (double)r.yd[t];
+    if (fine) {
+      ym = yd = 0.0;
+#pragma unroll
+      for (int q = 0; q < W; ++q) {
+        ym += sh[q][lr][5];
+        yd += sh[q][lr][6];
+      }
+    } else {
+      ym = r.ym[t];
+      yd = r.yd[t];
+    }
+    m = top - ym + 0.5 * (lp + ln);
+    d = (fabs(zd) < 0.5 * zm ? atanh(zd / zm) : 0.5 * (lp - ln)) - yd;
     f[0] = zm / (zp * zn);
     f[1] = zd / (zp * zn);
     f[2] = 0.5 / zp;

@@ -57,10 +57,11 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   constexpr int STAGE = 2 * (BM + BN) * ROW;         // bytes: xm, xd, wm, wd
   constexpr int NU = 2 * (BM + BN) / 16 / NW;        // 1 KB loads per wavefront and slice
   constexpr int NF = 2 * (IM + JN);                  // fragments of a half slice
-  // few rows (the operands' bytes bound the tile): lm with xd wd^T too, and exponentials to the last
-  // bits, which fp32 models always take.  What is otherwise left out or rounded is 1e-6 of a loss's
-  // half difference, which shows where that is small by chance and no other rows stand beside it.
-  constexpr bool WHOLE = BM == 32, FINE = WHOLE || sizeof(T) == 4;
+  // fp32 models and few rows (the operands' bytes bound the tile): lm with xd wd^T too, and exponentials
+  // to the last bits.  What is otherwise left out or rounded is 1e-6 of a gradient or of a loss's half
+  // difference: more than fp32 products lose, and in bf16 seen where that half difference is small by
+  // chance and no other rows stand beside it.
+  constexpr bool WHOLE = BM == 32 || sizeof(T) == 4, FINE = WHOLE;
   constexpr int NM = (WHOLE ? 4 : 3) * IM * JN * Frag<T>::OPS;       // matrix operations of a half slice
   static_assert(2 * (BM + BN) / 16 % NW == 0 && BM % 16 == 0 && BN % 16 == 0, "whole loads per wavefront");
   __shared__ __attribute__((aligned(1024))) char st0[STAGE];
@@ -446,18 +447,18 @@ HeadTile head_tile(int T_, int C) {
   return {32, 128, 32};
 }
 
-// fp32 models: this kernel takes the fp32 matrix instructions, the GEMM (gemm_f32.hip) products of
-// split operands, a tenth faster, on whole tiles of 128 rows, contractions cut where tiles are few; with it
-// the statistics are a launch more and the logits go through memory.  Estimates of both in us: the slices
-// of 16 k of the busiest compute unit at 613 GFLOP/s and a quarter for the rest, 8 for the joining launch;
-// 170 TFLOP/s and 24 for three launches.  Loss alone, us, here and there:
-//   1 x 32000 x 2048    158  300      64 x 32000 x 2048   235  292      128 x 32000 x 2048   413  301
-//   128 x 8192 x 512     39   51     256 x 8192 x 512      62   70      512 x 8192 x 512     111   94
-//   512 x 256 x 64       15   23       1 x 1024 x 1024     70   26     1024 x 1024 x 1024    63   73
+// fp32 models: this kernel takes the fp32 matrix instructions and all four products, the GEMM (gemm_f32.hip)
+// three products of split operands, a tenth faster each, on whole tiles of 128 rows, contractions cut where
+// tiles are few; with it the statistics are a launch more and the logits go through memory.  Estimates of
+// both in us: the slices of 16 k of the busiest compute unit at 613 GFLOP/s and what the rest was
+// measured to add (a half; as much again in the smallest tile), 8 for the joining launch; 170 TFLOP/s and 24 for
+// three launches.  Loss alone, us, here and there:
+//   1 x 32000 x 2048    158  300      64 x 32000 x 2048   328  292      128 x 8192 x 512    64   51
+//   512 x 256 x 64       18   23       1 x 1024 x 1024     70   30
 bool head_f32_fused(int T_, int C, int d) {
   const HeadTile t = head_tile(T_, C);
-  const double wgs = (double)ceil_div(T_, t.BM) * ceil_div(C, t.BN), slice = (t.BM == 32 ? 4 : 3) * 2.0 * t.BM * t.BN * 16 / 613e3;
-  const double here = 1.25 * std::ceil(wgs / 256) * ceil_div(d, 16) * slice + 8;
+  const double wgs = (double)ceil_div(T_, t.BM) * ceil_div(C, t.BN), slice = 4 * 2.0 * t.BM * t.BN * 16 / 613e3;
+  const double here = (t.BM == 64 && t.BN == 64 ? 2.0 : 1.5) * std::ceil(wgs / 256) * ceil_div(d, 16) * slice + 8;
   const double there = 6.0 * ceil_div(T_, 128) * 128 * C * d / 170e6 + 24;
   return here < there;
 }

@@ -336,9 +336,13 @@ struct HeadOut {
   double scale;
   float *loss_m, *loss_d;
   double* rowloss;
+  const void *xm, *xd;     // not null (fewer than 1024 rows): the target's logits are formed in fp64 from
+  int64_t ldx;             // these, [T][ldx], and the vocabulary's rows
+  const void *wm, *wd;
+  int d;
 };
 // joins the groups' statistics (part [groups][5][T]) to the rows' (first: there are none; last: nothing
-// comes behind, out is formed)
+// comes behind, out is formed).  P: float (bf16 models) or double (fp32)
 template <typename P>
 hipError_t launch_head_join(const HeadRows& r, const P* part, int groups, int T_, const int32_t* tgt, bool first, bool last,
                             const HeadOut& out, hipStream_t s);

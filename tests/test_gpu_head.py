@@ -335,11 +335,11 @@ def test_from_tokens_to_losses_and_back():
     m.embed_backward(dx[1], tok, eps=EPS, out=hv, accumulate=True)
     torch.cuda.synchronize()
 
-    # the statement: the mean of the logits without the product of the two half differences
+    # the statement (fp32 models of this size leave nothing out)
     t, dv = R.f64(th), EPS * R.f64(v)
     tk, keep = tok.cpu().long(), tgt.cpu() != R.IGNORE
     xm, xd = (scale * a[tk].reshape(-1, d) for a in (t, dv))
-    lm, ld = xm @ t.T, xd @ t.T + xm @ dv.T
+    lm, ld = xm @ t.T + xd @ dv.T, xd @ t.T + xm @ dv.T
     y = tgt.cpu().long().clamp(0)
     at = [torch.softmax(l, -1) - torch.nn.functional.one_hot(y, V) for l in (lm + ld, lm - ld)]
     gm, gd = ((a * keep[:, None] / n) for a in ((at[0] + at[1]) / 2, (at[0] - at[1]) / 2))
@@ -353,17 +353,12 @@ def test_from_tokens_to_losses_and_back():
         l = torch.nn.functional.cross_entropy(lg, tk[:, 1:].reshape(-1))
         return l.detach(), torch.autograd.grad(l, w)[0]
 
-    # the derivative itself: here x is a row of w, so the product left out, scale eps^2 <v_i, v_j>, is not
-    # small against the logits' rounding.  A shift of the logits by at most q moves every
-    # probability by at most e^(2 q) - 1 of itself (and p - 1 of the target by as much of p), and
-    # with them each of the terms above; the losses' mean by at most 2 q
+    # the derivative itself, of losses in fp64 (their rounding, 2^-52 of 5, over 2 eps: 1e-12)
     (lp, gp), (ln, gn) = grad(t + dv), grad(t - dv)
-    q = scale * EPS ** 2 * float((R.f64(v) @ R.f64(v).T).abs().max())
-    assert q < 5e-4
     diff = (gp - gn) / (2 * EPS)
-    assert float(torch.linalg.norm(R.f64(hv) - diff) / torch.linalg.norm(diff)) < 2 * q + 3e-6
-    assert abs(float(loss[0].double().sum() / n) - float(lp + ln) / 2) < 2 * q
-    assert abs(float(loss[1].double().sum() / n) - float(lp - ln) / 2) < (4 * q + 1e-5) * abs(float(lp - ln))
+    assert float(torch.linalg.norm(R.f64(hv) - diff) / torch.linalg.norm(diff)) < 3e-6
+    assert abs(float(loss[0].double().sum() / n) - float(lp + ln) / 2) < 1e-6 * abs(float(lp + ln))
+    assert abs(float(loss[1].double().sum() / n) - float(lp - ln) / 2) < 1e-5 * abs(float(lp - ln))
 
 
 @pytest.mark.parametrize("T,V,d,pad,dtype,piece", [
