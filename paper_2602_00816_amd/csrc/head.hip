@@ -33,30 +33,33 @@ __global__ void head_targets_kernel(int32_t* tgt, const int32_t* tok, const int3
   tgt[t] = y == IGNORE_LABEL ? y : min(max(y, 0), V - 1);
 }
 
-// One workgroup: a thread counts a run of rows, the runs' counts are added up over the threads.
+// One workgroup: a wavefront counts a run of rows, the runs' counts are added up over the wavefronts.
 constexpr int RT = 1024;
 __global__ __launch_bounds__(RT) void head_rows_kernel(int32_t* rows, const int32_t* tgt, int T_) {
   __shared__ int sh[RT / 64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int per = (T_ + RT - 1) / RT, from = min((int)threadIdx.x * per, T_), end = min(from + per, T_);
+  const int per = (T_ + RT - 1) / RT * 64, from = min(w * per, T_), end = min(from + per, T_);
+  auto live = [&](int t) { return t + lane < end && tgt[min(t + lane, T_ - 1)] != IGNORE_LABEL; };
   int n = 0;
-  for (int t = from; t < end; ++t) n += tgt[t] != IGNORE_LABEL;
-  int at = n;   // inclusive over the wavefront's lanes
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(at, o, 64);
-    if (lane >= o) at += y;
-  }
-  if (lane == 63) sh[w] = at;
+#pragma unroll 8
+  for (int t = from; t < end; t += 64) n += __popcll(__ballot(live(t)));
+  if (lane == 0) sh[w] = n;
   __syncthreads();
-  int all = 0;
-  at -= n;
+  int at = 0, all = 0;
   for (int q = 0; q < RT / 64; ++q) {
     if (q < w) at += sh[q];
     all += sh[q];
   }
   int none = all + from - at;   // (of the rows before, from - at have no target)
-  for (int t = from; t < end; ++t) rows[tgt[t] != IGNORE_LABEL ? at++ : none++] = t;
+#pragma unroll 8
+  for (int t = from; t < end; t += 64) {
+    const bool y = live(t);
+    const uint64_t m = __ballot(y);
+    const int ahead = __popcll(m & (((uint64_t)1 << lane) - 1)), count = __popcll(m);
+    if (t + lane < end) rows[y ? at + ahead : none + lane - ahead] = t + lane;
+    at += count;
+    none += min(64, end - t) - count;
+  }
   if (threadIdx.x == 0) rows[T_] = all;
 }
 

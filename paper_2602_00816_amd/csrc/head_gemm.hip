@@ -72,7 +72,8 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   if ((int)blockIdx.x >= tiles) return copy_rows<T>(a.copy, blockIdx.x - tiles, gridDim.x - tiles);
   // rows without a target come last, and tiles that hold no other are not formed
   const int live_rows = a.rows ? a.rows[a.T] : a.T, gy = (live_rows + BM - 1) / BM;
-  auto at = [&](int row) { return a.rows && row < a.T ? a.rows[row] : row; };
+  const int32_t* rows = live_rows < a.T ? a.rows : nullptr;
+  auto at = [&](int row) { return rows && row < a.T ? rows[row] : row; };
   if ((int)blockIdx.x >= gx * gy) {
     if constexpr (GRAD) {
       const int q = blockIdx.x - gx * gy, c = q % gx * BN, n = min(BN, a.C - c) / CE, end = min((gy + q / gx + 1) * BM, a.Tp);
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
     const int64_t ld = isx ? a.ldx : a.d;
     const int first = isx ? m0 : n0, end = isx ? a.T : a.C;
     const T* p = (const T*)(isx ? (half ? a.xd : a.xm) : (half ? a.wd : a.wm));
-    const bool moved = isx && a.rows;   // (all of x within 31 bits)
+    const bool moved = isx && rows;   // (all of x within 31 bits)
     const int src = min(first + row, end - 1);
     base[u] = moved ? p : p + first * ld;
     vo[u] = (uint32_t)sizeof(T) * (uint32_t)((moved ? at(src) : src - first) * ld + CE * ck);
@@ -406,8 +407,9 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
           const int lr = k * RPS + lane / LPR, lc = 8 * (lane % LPR);
           const uint2* p = reinterpret_cast<const uint2*>(stg + lr * LD + lc);
           const uint2 u = p[0], v = p[1];
+          const int to = __shfl(row, lr, 64);
           if (rb + lr < a.Tp && lc < live)   // (C is a multiple of 8)
-            *reinterpret_cast<uint4*>(o + (int64_t)at(rb + lr) * a.C + c0 + lc) = make_uint4(u.x, u.y, v.x, v.y);
+            *reinterpret_cast<uint4*>(o + (int64_t)to * a.C + c0 + lc) = make_uint4(u.x, u.y, v.x, v.y);
         }
         wave_lds_order();   // the next writes come after these reads
       }
