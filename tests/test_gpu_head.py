@@ -406,3 +406,49 @@ def test_large_batches_skip_rows_without_a_target(T, V, d, pad, dtype, piece):
             assert float(torch.linalg.norm(dw - one) / torch.linalg.norm(one)) <= 2 * R.half_step(x[0].dtype) + 1e-5
         if name == "scattered" and dtype == "bf16" and piece == 0:
             R.check_head((loss, dx, dw), x, w, tgt, 1.0, EPS, "scattered")
+
+
+def test_large_batch_in_rows_far_apart():
+    """Rows of x spread over more than 2^31 bytes: the same bits as from contiguous ones."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    T, V, d = 1100, 8192, 4096
+    m = _model(fd, V, d, "bf16")
+    x, w, tgt = _case(torch, T, V, d, "bf16", 17, ignore=0.4)
+    wide = tuple(torch.empty(T, 1 << 20, dtype=torch.bfloat16, device="cuda")[:, :d].copy_(a) for a in x)
+    for piece in (0, 1024):
+        got, want = m.head_grad(wide, w, tgt, eps=EPS, piece=piece), m.head_grad(x, w, tgt, eps=EPS, piece=piece)
+        torch.cuda.synchronize()
+        for a, b in zip((*got[0], *got[1], got[2]), (*want[0], *want[1], want[2])):
+            assert torch.equal(a, b)
+
+
+def test_graph_of_a_large_batch_whose_targets_change():
+    """Captured once; the rows that have a target are those of each replay."""
+    torch = need_gpu()
+    from paper_2602_00816_amd import fdhvp as fd
+    T, V, d = 1100, 8192, 4096
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        m = _model(fd, V, d, "bf16", stream=st.cuda_stream)
+        x, w, full = _case(torch, T, V, d, "bf16", 18, ignore=0.0)
+        tgt, scratch = full.clone(), m.head_scratch(T)
+        dx, dw = tuple(torch.empty_like(a) for a in x), torch.empty_like(w[0])
+        loss = tuple(torch.empty(T, device="cuda") for _ in range(2))
+        call = lambda: m.head_grad(x, w, tgt, eps=EPS, loss=loss, dx=dx, dw=dw, scratch=scratch)
+        call()
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            call()
+        g = torch.Generator().manual_seed(19)
+        for share in (0.3, 0.0, 0.95, 1.0, 0.5):
+            tgt.copy_(torch.where(torch.rand(T, generator=g).cuda() < share, torch.full_like(full, R.IGNORE), full))
+            graph.replay()
+            st.synchronize()
+            got = [a.clone() for a in (*loss, *dx, dw)]
+            for a in (*loss, *dx, dw):
+                a.fill_(7.0)
+            call()
+            st.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, (*loss, *dx, dw)))
