@@ -364,8 +364,8 @@ fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, siz
  * NULL).  It forms the logits twice (once where one piece holds the vocabulary, which is chosen for
  * up to 2^26 logits, and for up to 8 rows) and rounds their gradient to the context's dtype, as the
  * HVP's products do (not for up to 8 rows); sums and statistics are fp32 or wider, the order of the
- * additions is fixed (the same bits in every call).  The logits' mean may leave out x_d w_d^T, of second
- * order in the step, as the HVP does (not for up to 32 rows).
+ * additions is fixed (the same bits in every call).  Every product of the pairs is formed, x_d w_d^T in
+ * the logits' mean and the logits' gradient's half difference times w_d in dx_m among them, for any T.
  * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude.
  * Rows without a target may hold anything (NaN among it): their dx is 0 and they take no
  * part in dw.  A target outside [0, vocab) other than -100, or a NaN in its row, makes the row's

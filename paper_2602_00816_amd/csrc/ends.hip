@@ -103,7 +103,7 @@ constexpr int64_t HEAD_LAUNCH_ELEMS = (int64_t)1 << 35;
 // have none: 462 -> 349 us; gradients of 8192 x 32000 x 2048 with half of them 9.51 -> 7.14 ms, with none
 // 9.92 -> 9.94.
 constexpr double HEAD_ORDER_OPS = 1.5e11;
-// rows up to which the target's logits are formed in fp64 and x_d w_d is never left out
+// rows up to which the target's logits are formed in fp64
 constexpr int HEAD_FINE_ROWS = 32;
 // scratch that the plan of a split contraction may take
 constexpr size_t HEAD_SPLIT = (size_t)512 << 20;
@@ -123,14 +123,14 @@ GemmOperand mnmaj(const void* p, int64_t ld) {
   return o;
 }
 
-// products of the mean's logits on the GEMM: x_d w_d too for few rows
-int logit_pairs(int T_) { return T_ <= HEAD_FINE_ROWS ? 2 : 1; }
+// products of the mean's logits on the GEMM (few rows: x_d w_d in the HVP too, as the tiles of 32 rows have it)
+int logit_pairs(int T_, bool second) { return second || T_ <= HEAD_FINE_ROWS ? 2 : 1; }
 
 // scratch of the products of a piece of C columns: those that its gradient goes to and, unless fused, its logits'
 template <typename T>
-size_t piece_split(int T_, int Tp, int C, int d, bool grads, bool fused) {
+size_t piece_split(int T_, int Tp, int C, int d, bool grads, bool fused, bool second) {
   GemmArgs g[2];
-  auto need = [&](int M, int N, int K, int n, int mean_pairs = 1) {
+  auto need = [&](int M, int N, int K, int n, int mean_pairs) {
     for (int p = 0; p < 2; ++p) {
       g[p].M = M;
       g[p].N = N;
@@ -140,14 +140,14 @@ size_t piece_split(int T_, int Tp, int C, int d, bool grads, bool fused) {
     }
     return gemm_scratch<T>(g, n, HEAD_SPLIT);
   };
-  size_t mx = fused ? 0 : need(T_, C, d, 2, logit_pairs(T_));
-  if (grads) mx = std::max(mx, std::max(need(T_, d, C, 2), need(C, d, Tp, 1)));
+  size_t mx = fused ? 0 : need(T_, C, d, 2, logit_pairs(T_, second));
+  if (grads) mx = std::max(mx, std::max(need(T_, d, C, 2, second ? 2 : 1), need(C, d, Tp, 1, 1)));
   return mx;
 }
 
 }  // namespace
 
-HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
+HeadCarve Engine::head_carve(int T_, int piece, bool grads, bool second) const {
   HeadCarve c;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -165,7 +165,7 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   c.C = (int)(whole ? V : std::min<int64_t>(C, V));
   c.keep = grads && c.C == V;   // the logits of the one piece are formed once
   const size_t tp = (size_t)c.Tp, pc = tp * c.C, td = tp * d;
-  c.fused = bf16 || head_f32_fused(T_, c.C, d);
+  c.fused = bf16 || head_f32_fused(T_, c.C, d, second);
   c.order = c.fused && 6.0 * (double)T_ * V * d >= HEAD_ORDER_OPS;
   c.rows = take(c.order ? (t + 1) * 4 : 0);
   c.top = take(t * 4);
@@ -203,8 +203,11 @@ HeadCarve Engine::head_carve(int T_, int piece, bool grads) const {
   c.dm = take(products && bf16 ? t * d * 4 : 0);
   c.dd = take(products && bf16 ? t * d * 4 : 0);
   c.runs = take(c.thin ? head_thin_part(T_, V, d) : 0);
-  size_t sp = bf16 ? piece_split<bf16_t>(T_, c.Tp, c.C, d, products, c.fused) : piece_split<float>(T_, c.Tp, c.C, d, products, c.fused);
-  if (V % c.C) sp = std::max(sp, bf16 ? piece_split<bf16_t>(T_, c.Tp, V % c.C, d, products, c.fused) : piece_split<float>(T_, c.Tp, V % c.C, d, products, c.fused));
+  auto split = [&](int cols) {
+    return bf16 ? piece_split<bf16_t>(T_, c.Tp, cols, d, products, c.fused, second) : piece_split<float>(T_, c.Tp, cols, d, products, c.fused, second);
+  };
+  size_t sp = split(c.C);
+  if (V % c.C) sp = std::max(sp, split(V % c.C));
   c.split_bytes = sp;
   c.split = take(sp);
   c.total = T_ > 0 ? at : 0;
@@ -219,8 +222,8 @@ size_t Engine::head_scratch_most(size_t tokens, int piece) const {
   if (T_ == most_tokens && piece == most_piece) return most_bytes;
   most_tokens = T_;
   most_piece = piece;
-  most_bytes = head_carve(T_, piece, true).total;
-  for (int t = 8; t < T_; t += 8) most_bytes = std::max(most_bytes, head_carve(t, piece, true).total);
+  most_bytes = head_carve(T_, piece, true, false).total;
+  for (int t = 8; t < T_; t += 8) most_bytes = std::max(most_bytes, head_carve(t, piece, true, false).total);
   return most_bytes;
 }
 
@@ -274,7 +277,7 @@ int Engine::head_run(const HeadCall& c) {
       a[0].A[0] = kmaj(xd, ldx); a[0].B[0] = kmaj(wm + (int64_t)n0 * d, d);
       a[0].A[1] = kmaj(xm, ldx); a[0].B[1] = kmaj(wd + (int64_t)n0 * d, d);
       a[0].C = ld;
-      a[1].npairs = logit_pairs(T_);
+      a[1].npairs = logit_pairs(T_, c.second);
       a[1].A[0] = kmaj(xm, ldx); a[1].B[0] = kmaj(wm + (int64_t)n0 * d, d);
       a[1].A[1] = kmaj(xd, ldx); a[1].B[1] = kmaj(wd + (int64_t)n0 * d, d);
       a[1].C = lm;
@@ -291,6 +294,7 @@ int Engine::head_run(const HeadCall& c) {
       h.lm = lm; h.ld = ld;
     }
     h.tile = tile;
+    h.second = c.second;
     h.rows = rows;
     if (n0 == 0 && !grad) h.copy = cp;
     int e0 = 0;
@@ -361,7 +365,9 @@ int Engine::head_run(const HeadCall& c) {
     a[0].A[0] = kmaj(g.d, C); a[0].B[0] = mnmaj(wm + (int64_t)n0 * d, d);
     a[0].A[1] = kmaj(g.m, C); a[0].B[1] = mnmaj(wd + (int64_t)n0 * d, d);
     a[0].C = dxd;
+    a[1].npairs = c.second ? 2 : 1;
     a[1].A[0] = kmaj(g.m, C); a[1].B[0] = mnmaj(wm + (int64_t)n0 * d, d);
+    a[1].A[1] = kmaj(g.d, C); a[1].B[1] = mnmaj(wd + (int64_t)n0 * d, d);
     a[1].C = dxm;
     rc = product(a, 2);
     if (rc != FDH_OK) return rc;

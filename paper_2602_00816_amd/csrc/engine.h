@@ -109,7 +109,7 @@ struct HeadCall {
   const void *w_m = nullptr, *w_d = nullptr;   // [V][d], operand type
   const int32_t* tgt = nullptr;                // [T]
   int T = 0;
-  HeadCarve carve;                             // head_carve of T, the piece and grads
+  HeadCarve carve;                             // head_carve of T, the piece, grads and second
   float *loss_m = nullptr, *loss_d = nullptr;  // [T] or null
   double* rowloss = nullptr;                   // scale times the losses at the two points, [2][T], or null
   double scale = 1.0;
@@ -120,6 +120,10 @@ struct HeadCall {
   void* dw = nullptr;                          // [V][d]
   bool out_f32 = true, acc = false;            // outputs fp32 (acc: added to dw), else the operand type
   bool copy_x = true;                          // rows without a target may hold anything
+  // Products of two half differences in the means, x_d w_d^T of the logits' and g_d w_d of dx's: the calls on
+  // caller-owned memory form them always, the HVP leaves them out (of second order in the step, as in
+  // every linear layer) where a kernel without them is there.
+  bool second = true;
   char* scratch = nullptr;
 };
 double gemm_flops(const GemmArgs& g);   // executed by a product, causal tails clipped
@@ -202,8 +206,8 @@ class Engine : public WsLayout {
   // the loss over the vocabulary in pieces (fdh_head_loss, fdh_head_grad; the HVP's head with
   // vocab_piece > 0)
   int vocab_piece = 0;   // plan (and run) the head in pieces of so many columns; 0: whole logits
-  HeadCarve head_carve(int T_, int piece, bool grads) const;
-  size_t head_scratch_most(size_t tokens, int piece) const;   // of batches of up to so many tokens, with gradients
+  HeadCarve head_carve(int T_, int piece, bool grads, bool second = true) const;
+  size_t head_scratch_most(size_t tokens, int piece) const;   // of an HVP's batches of up to so many tokens
   template <typename T> int head_run(const HeadCall& c);
   int head_check(const fdh_head_inputs* in, bool grads, size_t scratch_bytes, const void* scratch, HeadCall* c);
   int head_loss(const fdh_head_inputs* in, float* loss_m, float* loss_d, void* scratch, size_t scratch_bytes);

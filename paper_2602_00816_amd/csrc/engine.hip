@@ -877,7 +877,8 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
     c.w_m = th + head.off; c.w_d = lo + head.off;
     c.tgt = (const int32_t*)(ws + tgt.off);
     c.T = T_;
-    c.carve = head_carve(T_, vp, true);
+    c.second = false;
+    c.carve = head_carve(T_, vp, true, c.second);
     c.rowloss = (double*)(ws + rowloss.off);
     c.scale = inv_n;
     c.grads = true;

@@ -2,9 +2,9 @@
 // vocabulary, both channels at once, whose epilogue leaves either the rows' statistics over the
 // tile's columns or the logits' gradient in the operand type.
 //
-// lm = xm wm^T (+ xd wd^T) and ld = xd wm^T + xm wd^T share their operands: a K slice of the four
-// tiles (x and w, mean and half difference) feeds three matrix operations per output block, as many
-// bytes per operation as a 256 x 256 tile of one product takes from two.  Slices of 64 bytes a row
+// lm = xm wm^T + xd wd^T and ld = xd wm^T + xm wd^T share their operands: a K slice of the four
+// tiles (x and w, mean and half difference) feeds four matrix operations per output block (three in the
+// HVP, which leaves xd wd^T out), fewer bytes per operation than a 256 x 256 tile of one product takes.  Slices of 64 bytes a row
 // (32 k in bf16, 16 in fp32) come by direct loads to LDS into a ring of three stages, two slices
 // ahead; a wavefront keeps two fragment sets (half slices) and reads one while the matrix operations
 // run on the other.  A stage is free as soon as every wavefront has the second half of its slice in
@@ -48,7 +48,8 @@ __device__ inline typename Frag<T>::type fragment(const char* t, int r0, int hal
   return *reinterpret_cast<const typename Frag<T>::type*>(t + tile_at(r0 + (lane & 31), 2 * half + (lane >> 5)));
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool GRAD>
+// ALL: with xd wd^T
+template <typename T, int BM, int BN, int WM, int WN, bool GRAD, bool ALL>
 __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a, HeadRows r) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, IM = WTM / 32, JN = WTN / 32;
   typedef typename Frag<T>::type F;
@@ -57,12 +58,11 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
   constexpr int STAGE = 2 * (BM + BN) * ROW;         // bytes: xm, xd, wm, wd
   constexpr int NU = 2 * (BM + BN) / 16 / NW;        // 1 KB loads per wavefront and slice
   constexpr int NF = 2 * (IM + JN);                  // fragments of a half slice
-  // fp32 models and few rows (the operands' bytes bound the tile): lm with xd wd^T too, and exponentials
-  // to the last bits.  What is otherwise left out or rounded is 1e-6 of a gradient or of a loss's half
-  // difference: more than fp32 products lose, and in bf16 seen where that half difference is small by
-  // chance and no other rows stand beside it.
-  constexpr bool WHOLE = BM == 32 || sizeof(T) == 4, FINE = WHOLE;
-  constexpr int NM = (WHOLE ? 4 : 3) * IM * JN * Frag<T>::OPS;       // matrix operations of a half slice
+  // fp32 models and few rows (the operands' bytes bound the tile): exponentials to the last bits.  What
+  // __expf rounds is 1e-6 of a gradient or of a loss's half difference: more than fp32 products lose, and in
+  // bf16 seen where that half difference is small by chance and no other rows stand beside it.
+  constexpr bool FINE = BM == 32 || sizeof(T) == 4;
+  constexpr int NM = (ALL ? 4 : 3) * IM * JN * Frag<T>::OPS;       // matrix operations of a half slice
   static_assert(2 * (BM + BN) / 16 % NW == 0 && BM % 16 == 0 && BN % 16 == 0, "whole loads per wavefront");
   __shared__ __attribute__((aligned(1024))) char st0[STAGE];
   __shared__ __attribute__((aligned(1024))) char st1[STAGE];
@@ -422,8 +422,17 @@ void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t 
   // (the copy of x on compute units that the tiles leave idle: 4 us less than a launch of its own)
   const int copies = a.copy.om ? std::min(256, a.copy.Tp) : 0;
   const dim3 grid(ceil_div(a.C, BN) * ceil_div(a.T, BM) + copies), block(64 * WM * WN);
-  if (grad) hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, true>), grid, block, 0, s, a, r);
-  else hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, false>), grid, block, 0, s, a, r);
+  auto launch = [&](auto all) {
+    constexpr bool ALL = decltype(all)::value;
+    if (grad) hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, true, ALL>), grid, block, 0, s, a, r);
+    else hipLaunchKernelGGL((head_logits_kernel<T, BM, BN, WM, WN, false, ALL>), grid, block, 0, s, a, r);
+  };
+  // (fp32 models and few rows have it in the HVP too: 1e-6 of a gradient or of a loss's half difference at its
+  // steps, more than is lost otherwise there)
+  if constexpr (BM > 32 && sizeof(T) == 2) {
+    if (!a.second) return launch(std::false_type{});
+  }
+  launch(std::true_type{});
 }
 
 }  // namespace
@@ -457,11 +466,11 @@ HeadTile head_tile(int T_, int C) {
 // three launches.  Loss alone, us, here and there:
 //   1 x 32000 x 2048    158  300      64 x 32000 x 2048   328  292      128 x 8192 x 512    64   51
 //   512 x 256 x 64       18   23       1 x 1024 x 1024     70   30
-bool head_f32_fused(int T_, int C, int d) {
+bool head_f32_fused(int T_, int C, int d, bool second) {
   const HeadTile t = head_tile(T_, C);
   const double wgs = (double)ceil_div(T_, t.BM) * ceil_div(C, t.BN), slice = 4 * 2.0 * t.BM * t.BN * 16 / 613e3;
   const double here = (t.BM == 64 && t.BN == 64 ? 2.0 : 1.5) * std::ceil(wgs / 256) * ceil_div(d, 16) * slice + 8;
-  const double there = 6.0 * ceil_div(T_, 128) * 128 * C * d / 170e6 + 24;
+  const double there = (second ? 8.0 : 6.0) * ceil_div(T_, 128) * 128 * C * d / 170e6 + 24;
   return here < there;
 }
 

@@ -380,12 +380,13 @@ struct HeadLogits {
   float *lm, *ld;          // statistics: the logits too, [T][C], or null
   void *gm, *gd;           // gradient: [Tp][C], operand type
   HeadTile tile;           // head_tile
+  bool second;             // xd wd^T in lm (fp32 models and tiles of 32 rows: always)
   HeadCopy copy;           // made beside the tiles
   const int32_t* rows;     // launch_head_rows' order, or null: the batch's own
 };
 HeadTile head_tile(int T_, int C);
-// whether this product forms the logits of an fp32 model, or the GEMM
-bool head_f32_fused(int T_, int C, int d);
+// whether this product forms the logits of an fp32 model, or the GEMM (with xd wd^T: second)
+bool head_f32_fused(int T_, int C, int d, bool second);
 // grad: the gradient of the losses, zeros in rows without a target and from T on; else
 // part, and the target logits of r
 template <typename T>
