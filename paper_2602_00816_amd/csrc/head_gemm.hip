@@ -458,19 +458,22 @@ HeadTile head_tile(int T_, int C) {
   return {32, 128, 32};
 }
 
-// fp32 models: this kernel takes the fp32 matrix instructions and all four products, the GEMM (gemm_f32.hip)
-// three products of split operands, a tenth faster each, on whole tiles of 128 rows, contractions cut where
-// tiles are few; with it the statistics are a launch more and the logits go through memory.  Estimates of
-// both in us: the slices of 16 k of the busiest compute unit at 613 GFLOP/s and what the rest was
-// measured to add (a half; as much again in the smallest tile), 8 for the joining launch; 170 TFLOP/s and 24 for
-// three launches.  Loss alone, us, here and there:
-//   1 x 32000 x 2048    158  300      64 x 32000 x 2048   328  292      128 x 8192 x 512    64   51
-//   512 x 256 x 64       18   23       1 x 1024 x 1024     70   30
+// fp32 models: this kernel takes the fp32 matrix instructions, the GEMM (gemm_f32.hip) split operands on the
+// bf16 ones, a quarter faster, on whole tiles of 128 rows, contractions cut where tiles are few; with it
+// the statistics are a launch more and the logits go through memory, 16 bytes written and read each.  Estimates
+// of both in us: rounds of tiles over the compute units, each its slices of 16 k at 613 GFLOP/s and 5%, and 9
+// for its epilogue, and 10 for the joining launch; 200 TFLOP/s, 5.5 TB/s and 25 for three launches.  Loss
+// alone, us, here and there:
+//   1 x 32000 x 2048    157  368      33 x 32000 x 2048   253  360      128 x 32000 x 2048  486  395
+//   128 x 8192 x 512     44   56      512 x 8192 x 512    136  118      2047 x 8192 x 512   483  400
+//   1000 x 32000 x 64   179  206      1000 x 32000 x 128  292  282      1000 x 32000 x 256  519  443
+//   4096 x 8192 x 64    160  219      2000 x 4096 x 16     26   59      8192 x 1024 x 256   132  138
+//   512 x 256 x 64       16   25      1 x 1024 x 1024      70   29      200 x 2048 x 512     41   40
 bool head_f32_fused(int T_, int C, int d, bool second) {
   const HeadTile t = head_tile(T_, C);
   const double wgs = (double)ceil_div(T_, t.BM) * ceil_div(C, t.BN), slice = 4 * 2.0 * t.BM * t.BN * 16 / 613e3;
-  const double here = (t.BM == 64 && t.BN == 64 ? 2.0 : 1.5) * std::ceil(wgs / 256) * ceil_div(d, 16) * slice + 8;
-  const double there = (second ? 8.0 : 6.0) * ceil_div(T_, 128) * 128 * C * d / 170e6 + 24;
+  const double here = std::ceil(wgs / 256) * (1.05 * ceil_div(d, 16) * slice + 9) + 10;
+  const double there = (second ? 8.0 : 6.0) * ceil_div(T_, 128) * 128 * C * d / 200e6 + 16.0 * T_ * C / 5.5e6 + 25;
   return here < there;
 }
 
