@@ -88,6 +88,13 @@ fdh_status fdh_testing_gemm_plan(int32_t dtype, int32_t M, int32_t N, int32_t K,
 fdh_status fdh_testing_qk_split(int32_t dtype, int64_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                 int32_t norm, int32_t backward, int32_t in_place, int64_t* out12);
 
+/* How fdh_head_grad (grads != 0) or fdh_head_loss would run T rows with that piece (host arithmetic
+ * only): out8 = 1 where both gradients come from one pass over w, 1 where the product's epilogue
+ * takes the logits (0: they go through memory from the GEMM), 1 where rows without a target are put
+ * last, 1 where the logits of the one piece are formed once, rows and columns of a tile, columns of a
+ * piece, columns of a launch of the first pass. */
+fdh_status fdh_testing_head_route(const fdh_ctx* ctx, int32_t T, int32_t piece, int32_t grads, int32_t* out8);
+
 /* on != 0 makes the next fdh_set_workspace plan the unfused attention path
  * (score, probability and score-gradient matrices in the workspace, MFMA
  * GEMMs and row kernels) even where the fused kernels apply (bf16 operands;

@@ -614,6 +614,21 @@ extern "C" fdh_status fdh_testing_gemm_plan(int32_t dtype, int32_t M, int32_t N,
   return FDH_OK;
 }
 
+extern "C" fdh_status fdh_testing_head_route(const fdh_ctx* ctx, int32_t T, int32_t piece, int32_t grads, int32_t* out8) {
+  if (!ctx || !ctx->eng || !out8 || T < 1 || piece < 0) return FDH_ERR_INVALID_ARG;
+  const fdh::Engine& e = *ctx->eng;
+  if (e.quad || T > fdh::HEAD_MAX_ROWS || e.d > fdh::HEAD_MAX_WIDTH) return FDH_ERR_UNSUPPORTED;
+  try {
+    const fdh::HeadCarve c = e.head_carve(T, piece, grads != 0);
+    const fdh::HeadTile t = fdh::head_tile(T, c.C);
+    const int32_t out[8] = {c.thin, c.fused, c.order, c.keep, t.BM, t.BN, c.C, c.C1};
+    std::copy(out, out + 8, out8);
+  } catch (...) {
+    return FDH_ERR_INVALID_ARG;
+  }
+  return FDH_OK;
+}
+
 extern "C" fdh_status fdh_testing_qk_split(int32_t dtype, int64_t T, int32_t n_heads, int32_t n_kv_heads,
                                            int32_t head_dim, int32_t norm, int32_t backward, int32_t in_place,
                                            int64_t* out12) {

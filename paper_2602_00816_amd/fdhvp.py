@@ -144,6 +144,7 @@ def lib():
         "fdh_testing_qk_split": (i32, [i32, i64, i32, i32, i32, i32, i32, i32, C.POINTER(i64)]),
         "fdh_testing_unfused_attention": (i32, [vp, i32]),
         "fdh_testing_unsplit_wgrad": (i32, [vp, i32]),
+        "fdh_testing_head_route": (i32, [vp, i32, i32, i32, pi]),
         "fdh_testing_timing": (i32, [vp, i32]),
         "fdh_testing_timing_read": (i32, [vp, pd]),
         "fdh_testing_copy": (i32, [vp, vp, C.c_size_t, vp]),
