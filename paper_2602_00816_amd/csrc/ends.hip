@@ -264,6 +264,7 @@ int Engine::head_run(const HeadCall& c) {
   const bool copy = c.grads && !k.thin && (c.copy_x || T_ != k.Tp);
   HeadCopy cp{};
   if (copy) cp = HeadCopy{ws + k.xm, ws + k.xd, xm, xd, ldx, T_, k.Tp, d, c.tgt};
+  int formed = T_;   // rows of the tiles that are formed (for the timing alone)
   // the product that forms columns n0 .. n0 + C - 1 of the logits, for their statistics (keeping them, if
   // they are kept) or for their gradient
   auto logits = [&](int n0, int C, bool grad) -> int {
@@ -300,10 +301,18 @@ int Engine::head_run(const HeadCall& c) {
     int e0 = 0;
     if (timing.on) CK(timing.begin(st, &e0));
     CK(launch_head_logits<T>(h, r, grad, st));
-    if (timing.on) CK(timing.end(st, 0, e0, 6.0 * T_ * C * d, 0.0));
+    if (timing.on) CK(timing.end(st, 0, e0, 2.0 * head_products<T>(tile, c.second) * formed * C * d, 0.0));
     return FDH_OK;
   };
-  if (rows) CK(launch_head_rows(rows, c.tgt, T_, st));
+  if (rows) {
+    CK(launch_head_rows(rows, c.tgt, T_, st));
+    if (timing.on) {
+      int32_t live = 0;
+      CK(hipMemcpyAsync(&live, rows + T_, sizeof live, hipMemcpyDeviceToHost, st));
+      CK(hipStreamSynchronize(st));
+      formed = std::min(T_, (int)ceil_div(live, tile.BM) * tile.BM);
+    }
+  }
   if (copy && !k.fused) CK(launch_head_copy<T>(cp, st));
   HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss, nullptr, nullptr, ldx, wm, wd, d};
   if (T_ <= HEAD_FINE_ROWS) {

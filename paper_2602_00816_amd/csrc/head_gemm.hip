@@ -430,7 +430,7 @@ void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t 
   // (fp32 models and few rows have it in the HVP too: 1e-6 of a gradient or of a loss's half difference at its
   // steps, more than is lost otherwise there)
   if constexpr (BM > 32 && sizeof(T) == 2) {
-    if (!a.second) return launch(std::false_type{});
+    if (head_products<T>(a.tile, a.second) == 3) return launch(std::false_type{});
   }
   launch(std::true_type{});
 }

@@ -385,6 +385,9 @@ struct HeadLogits {
   const int32_t* rows;     // launch_head_rows' order, or null: the batch's own
 };
 HeadTile head_tile(int T_, int C);
+// products that a tile of the logits' pair takes
+template <typename T>
+constexpr int head_products(const HeadTile& t, bool second) { return second || t.BM == 32 || sizeof(T) == 4 ? 4 : 3; }
 // whether this product forms the logits of an fp32 model, or the GEMM (with xd wd^T: second)
 bool head_f32_fused(int T_, int C, int d, bool second);
 // grad: the gradient of the losses, zeros in rows without a target and from T on; else
