@@ -222,8 +222,12 @@ fdh_status fdh_set_recompute(fdh_ctx* ctx, int32_t on);
  * workspace holds 4 bytes (bf16) or 8 (fp32) per token and column of one piece in place of 12 or
  * 16 per token and word of the vocabulary; the logits are formed twice (3 more products of the
  * head's size, where it has 8), unless one piece holds the vocabulary (bf16: 12 bytes then).  0 keeps
- * whole logits (the default).  Results agree to the rounding
- * of the context's dtype.  Takes effect for the following fdh_workspace_bytes / fdh_set_workspace;
+ * whole logits (the default).  Results agree to the rounding of the context's dtype: in bf16 the sums of
+ * exponentials are fp32 (fp64 with whole logits), and the rows' weight is outside the rounding of the logits'
+ * gradient.  As with whole logits, products of two half differences (of second order in the step) are left
+ * out of the means, but for batches of up to 32 tokens and where the fp32 kernels have them.  The half differences of the
+ * logits may reach 30 (bf16) or 300 (fp32): beyond, where whole logits hold longer steps, the product may be
+ * FDH_ERR_NONFINITE.  Takes effect for the following fdh_workspace_bytes / fdh_set_workspace;
  * the carve in use keeps its mode until then. */
 fdh_status fdh_set_vocab_piece(fdh_ctx* ctx, int32_t columns);
 
@@ -366,7 +370,8 @@ fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, siz
  * HVP's products do (not for up to 8 rows); sums and statistics are fp32 or wider, the order of the
  * additions is fixed (the same bits in every call).  Every product of the pairs is formed, x_d w_d^T in
  * the logits' mean and the logits' gradient's half difference times w_d in dx_m among them, for any T.
- * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude.
+ * The half differences of the logits may reach 30 (bf16) or 300 (fp32) in magnitude; where a row's reach
+ * so far beyond that a sum of exponentials may be cut, its loss and gradient, and dw, are NaN.
  * Rows without a target may hold anything (NaN among it): their dx is 0 and they take no
  * part in dw.  A target outside [0, vocab) other than -100, or a NaN in its row, makes the row's
  * loss and gradient, and with it dw, NaN.  Pointers 16-byte aligned (targets and losses

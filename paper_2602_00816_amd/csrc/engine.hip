@@ -1159,7 +1159,11 @@ int Engine::finish_checked(const float* hv) {
   CK(hipStreamSynchronize(stream));
   if (h[2]) { err = "a token lies outside [0, vocab)"; return FDH_ERR_INVALID_ARG; }
   if (h[0]) { err = "the direction v holds NaN or Inf"; return FDH_ERR_NONFINITE; }
-  if (h[1]) { err = "the product Hv holds NaN or Inf"; return FDH_ERR_NONFINITE; }
+  if (h[1]) {
+    err = "the product Hv holds NaN or Inf";
+    if (vp) err += bf16 ? " (the head in pieces holds half differences of the logits up to 30)" : " (the head in pieces holds half differences of the logits up to 300)";
+    return FDH_ERR_NONFINITE;
+  }
   return FDH_OK;
 }
 

@@ -246,7 +246,13 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
     m = d = f[0] = f[1] = f[2] = f[3] = __builtin_nan("");
   } else if (on) {
     const double sa = z[0], ss = z[1], sp = z[2], sq = z[3];
-    const double zp = sa + ss + sp, zn = sa - ss + sq, zm = sa + 0.5 * (sp + sq), zd = ss + 0.5 * (sp - sq);
+    double zp = sa + ss + sp, zn = sa - ss + sq;
+    const double zm = sa + 0.5 * (sp + sq), zd = ss + 0.5 * (sp - sq);
+    // Half differences to H leave both sums at e^(-2 H) or more.  Below LEAST, which 30 (bf16) and 300 (fp32) do
+    // not reach, the range of the exponentials may have cut terms (2^-126 in fp32: of 2^18 words 2^-18 of a
+    // sum of 2^-90 at the most; 2^-1022 in fp64), so the row is NaN.
+    constexpr double LEAST = sizeof(P) == 8 ? 0x1p-900 : 0x1p-90;
+    if (!(zp >= LEAST && zn >= LEAST)) zp = zn = __builtin_nan("");
     const double lp = log(zp), ln = log(zn);
     if (fine) {
       ym = yd = 0.0;
