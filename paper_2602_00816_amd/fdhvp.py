@@ -521,10 +521,13 @@ class Model:
         return pm, pd, lm
 
     @staticmethod
-    def _whole(t, what, dtype, n, dev):
-        """Pointer of a contiguous tensor of n elements."""
+    def _whole(t, what, dtype, n, dev, cols=0):
+        """Pointer of a contiguous tensor of n elements; with cols a table whose rows have so many (or
+        its elements in one dimension)."""
         if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} elements")
+        if cols and t.dim() > 1 and t.shape[-1] != cols:
+            raise ValueError(f"{what} must have rows of {cols} elements")
         if t.get_device() != dev:
             raise ValueError("tensors must lie on the current device")
         return t.data_ptr()
@@ -640,17 +643,17 @@ class Model:
         dev, B, S = self._embed_tokens(tokens)
         T, d, dt, f32 = B * S, self._d, self._qk_dtype, torch.float32
         e, ve = table
-        pe, pve = self._whole(e, "table", dt, self._vocab * d, dev), 0
+        pe, pve = self._whole(e, "table", dt, self._vocab * d, dev, d), 0
         if ve is not None:
-            pve = self._whole(ve, "the table's direction", f32, self._vocab * d, dev)
+            pve = self._whole(ve, "the table's direction", f32, self._vocab * d, dev, d)
         pp = pvp = 0
         if positions is not None:
             p, vp = positions
             if p.dim() != 2 or p.shape[0] < S:
                 raise ValueError(f"positions must have at least {S} rows")
-            pp = self._whole(p, "positions", dt, p.shape[0] * d, dev)
+            pp = self._whole(p, "positions", dt, p.shape[0] * d, dev, d)
             if vp is not None:
-                pvp = self._whole(vp, "the positions' direction", f32, p.shape[0] * d, dev)
+                pvp = self._whole(vp, "the positions' direction", f32, p.shape[0] * d, dev, d)
         if out is None:
             out = tuple(torch.empty((T, d), dtype=f32, device=tokens.device) for _ in range(2))
         xm, xd, ldx = self._row_pair(out, "out", f32, T, d, dev)
@@ -676,9 +679,9 @@ class Model:
             out = torch.empty((self._vocab, d), dtype=f32, device=tokens.device)
         if gpt2 and out_positions is None:
             out_positions = torch.empty((self._max_seq, d), dtype=f32, device=tokens.device)
-        po, pp = self._whole(out, "out", f32, self._vocab * d, dev), 0
+        po, pp = self._whole(out, "out", f32, self._vocab * d, dev, d), 0
         if out_positions is not None:
-            pp = self._whole(out_positions, "out_positions", f32, self._max_seq * d, dev)
+            pp = self._whole(out_positions, "out_positions", f32, self._max_seq * d, dev, d)
         if scratch is None:
             scratch = self.embed_scratch(B, S)
         ps, ns = self._scratch_arg(scratch, dev)
@@ -700,7 +703,7 @@ class Model:
         dev = self._call_device(targets)
         T, d, dt = targets.numel(), self._d, self._qk_dtype
         xm, xd, ldx = self._row_pair(x, "x", dt, T, d, dev)
-        wm, wd = (self._whole(t, "w", dt, self._vocab * d, dev) for t in w)
+        wm, wd = (self._whole(t, "w", dt, self._vocab * d, dev, d) for t in w)
         tg = self._whole(targets, "targets", torch.int32, T, dev)
         return dev, T, HeadInputs(xm, xd, ldx, wm, wd, tg, T, piece, 0)
 
@@ -751,7 +754,7 @@ class Model:
             dw = torch.empty((self._vocab, d), dtype=gt, device=targets.device)
         lm, ld = self._head_loss_out(loss, T, dev)
         dm, dd, lddx = self._row_pair(dx, "dx", gt, T, d, dev)
-        pw = self._whole(dw, "dw", gt, self._vocab * d, dev)
+        pw = self._whole(dw, "dw", gt, self._vocab * d, dev, d)
         if scratch is None:
             scratch = self.head_scratch(T, piece)
         ps, ns = self._scratch_arg(scratch, dev)
