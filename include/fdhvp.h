@@ -354,7 +354,8 @@ fdh_status fdh_embed_forward(fdh_ctx* ctx, const fdh_embed_tables* tables, const
  * set: the same bits in every call.  Positions of tokens outside [0, vocab) are left out.
  * scratch: device memory, 16-byte aligned, of at least fdh_embed_scratch_bytes, in use
  * until the call's work is done: calls that may overlap on the device need scratch of
- * their own.  No output overlaps an input.  Only enqueued, as fdh_embed_forward. */
+ * their own.  No output overlaps an input.  eps positive, finite, and so 1 / eps and scale / eps.  Only
+ * enqueued, as fdh_embed_forward. */
 fdh_status fdh_embed_backward(fdh_ctx* ctx, const int32_t* tokens_dev, int32_t B, int32_t S, const float* dx_d, int64_t lddx,
                               double eps, float* hv_e, float* hv_p, int32_t accumulate, void* scratch, size_t scratch_bytes);
 fdh_status fdh_embed_scratch_bytes(const fdh_ctx* ctx, int32_t B, int32_t S, size_t* bytes);

@@ -64,7 +64,10 @@ int Engine::embed_backward(const int32_t* tok, int B, int S, const float* dx_d, 
                            bool acc, void* scratch, size_t scratch_bytes) {
   const int rc = embed_check(tok, B, S);
   if (rc != FDH_OK) return rc;
-  if (!(eps > 0.0) || !std::isfinite(eps)) { err = "eps must be positive and finite"; return FDH_ERR_INVALID_ARG; }
+  if (!(eps > 0.0) || !std::isfinite(eps) || !std::isfinite(1.0 / eps) || !std::isfinite(embed_scale / eps)) {
+    err = "eps must be positive and finite, and so 1 / eps and the embedding's scale / eps";
+    return FDH_ERR_INVALID_ARG;
+  }
   if (!hv_e || (uintptr_t)hv_e % 4) { err = "hv_e: null or not 4-byte aligned"; return FDH_ERR_INVALID_ARG; }
   if (gpt2 ? (!hv_p || (uintptr_t)hv_p % 4) : hv_p != nullptr) {
     err = "the GPT-2 family has learned positions and the Llama family none: hv_p must be given or null";
@@ -342,7 +345,7 @@ int Engine::head_run(const HeadCall& c) {
     h.tgt = c.tgt;
     h.T = T_; h.V = V; h.d = d;
     h.scale = (float)c.scale;
-    h.alpha_w = (float)(c.scale * c.inv_eps);
+    h.alpha_w = (float)c.scale_w;
     h.dxm = c.dx_m; h.dxd = c.dx_d; h.lddx = c.lddx;
     h.dw = c.dw;
     h.acc = c.acc;
@@ -387,7 +390,7 @@ int Engine::head_run(const HeadCall& c) {
     w.C = (char*)c.dw + (size_t)n0 * d * ob;
     w.ldc = d;
     w.out_type = c.out_f32 ? OUT_F32 : OUT_OP;
-    w.alpha = (float)(c.scale * c.inv_eps);
+    w.alpha = (float)c.scale_w;
     w.beta = c.acc ? 1.f : 0.f;
     rc = product(&w, 1);
     if (rc != FDH_OK) return rc;
@@ -476,7 +479,7 @@ int Engine::head_grad(const fdh_head_inputs* in, float* loss_m, float* loss_d, c
   c.loss_m = loss_m; c.loss_d = loss_d;
   c.grads = true;
   c.scale = g->scale;
-  c.inv_eps = 1.0 / g->eps;
+  c.scale_w = g->scale / g->eps;
   c.dx_m = g->dx_m; c.dx_d = g->dx_d; c.lddx = g->lddx;
   c.dw = g->dw;
   c.out_f32 = g->dtype == FDH_F32;

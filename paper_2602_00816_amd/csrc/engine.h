@@ -114,7 +114,7 @@ struct HeadCall {
   double* rowloss = nullptr;                   // scale times the losses at the two points, [2][T], or null
   double scale = 1.0;
   bool grads = false;
-  double inv_eps = 1.0;
+  double scale_w = 1.0;                        // of dw: scale / eps
   void *dx_m = nullptr, *dx_d = nullptr;       // [T][lddx]
   int64_t lddx = 0;
   void* dw = nullptr;                          // [V][d]

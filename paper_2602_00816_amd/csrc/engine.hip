@@ -882,7 +882,7 @@ int Engine::hvp_t(const T* th, const float* v, double eps, const BatchRef& bt, d
     c.rowloss = (double*)(ws + rowloss.off);
     c.scale = inv_n;
     c.grads = true;
-    c.inv_eps = 1.0 / eps;
+    c.scale_w = inv_n * (1.0 / eps);
     c.dx_m = F32(db_m); c.dx_d = F32(db_d); c.lddx = d;
     c.dw = hv + head.off;
     c.acc = acc;
