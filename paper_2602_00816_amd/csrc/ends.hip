@@ -316,7 +316,7 @@ int Engine::head_run(const HeadCall& c) {
       formed = std::min(T_, (int)ceil_div(live, tile.BM) * tile.BM);
     }
   }
-  if (copy && !k.fused) CK(launch_head_copy<T>(cp, st));
+  if (copy && !k.fused) CK(launch_head_copy(cp, st));
   HeadOut out{V, c.scale, c.loss_m, c.loss_d, c.rowloss, nullptr, nullptr, ldx, wm, wd, d};
   if (T_ <= HEAD_FINE_ROWS) {
     out.xm = xm;

@@ -322,9 +322,8 @@ __global__ __launch_bounds__(NT) void head_dlogits_kernel(PairT<T> o, HeadRows r
   }
 }
 
-template <typename T>
 __global__ __launch_bounds__(NT) void head_copy_kernel(HeadCopy c) {
-  copy_rows<T>(c, blockIdx.x, gridDim.x);
+  copy_rows<float>(c, blockIdx.x, gridDim.x);
 }
 
 // bf16 copy of the fp32 pair [T][dm]
@@ -374,13 +373,10 @@ template hipError_t launch_head_dlogits<float>(PairT<float>, const HeadRows&, co
                                                const int32_t*, hipStream_t);
 template hipError_t launch_head_dlogits<bf16_t>(PairT<bf16_t>, const HeadRows&, const float*, const float*, int, int, int, int,
                                                 const int32_t*, hipStream_t);
-template <typename T>
 hipError_t launch_head_copy(const HeadCopy& c, hipStream_t s) {
-  hipLaunchKernelGGL(head_copy_kernel<T>, dim3(std::min(c.Tp, 2048)), dim3(NT), 0, s, c);
+  hipLaunchKernelGGL(head_copy_kernel, dim3(std::min(c.Tp, 2048)), dim3(NT), 0, s, c);
   return hipGetLastError();
 }
-template hipError_t launch_head_copy<float>(const HeadCopy&, hipStream_t);
-template hipError_t launch_head_copy<bf16_t>(const HeadCopy&, hipStream_t);
 hipError_t launch_head_round(PairT<bf16_t> o, int64_t ldo, const float* m, const float* d, int T_, int dm, hipStream_t s) {
   hipLaunchKernelGGL(head_round_kernel, dim3(T_), dim3(NT), 0, s, o, ldo, m, d, dm);
   return hipGetLastError();

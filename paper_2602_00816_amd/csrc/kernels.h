@@ -361,7 +361,7 @@ struct HeadCopy {
   int T, Tp, d;
   const int32_t* tgt;
 };
-template <typename T>
+// a launch of its own, where the logits come from the GEMM (fp32 models); else beside launch_head_logits' tiles
 hipError_t launch_head_copy(const HeadCopy& c, hipStream_t s);
 
 // head_gemm.hip: the product that forms columns n0 .. n0 + C - 1 of the logits, and what its epilogue
