@@ -218,7 +218,9 @@ __device__ inline void pos_part(const PosArgs& a, int block, int blocks) {
 // chunk before holds that token too, in 1 that of its last token when it begins here and
 // goes on.  embed_join_kernel adds the parts of such a token from the chunk in which it
 // begins.  However often a token occurs, no wavefront adds more than R rows and the join's
-// wavefronts a quarter of R-th as many parts.
+// wavefronts a quarter of R-th as many parts, one after the other: where one token is everywhere that
+// is most of the time (8192 tokens of 32000 x 2048: 83 us spread evenly, 108 with half of them
+// one token, 132 with all).
 struct SumArgs {
   const uint32_t *key, *pos;
   const float* dx;
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(NT) void embed_join_kernel(SumArgs a) {
 // ---- a few tokens: one launch, no sort -----------------------------------------------------
 // A workgroup per position and 1024 columns: the first position of a token adds the rows of all of
 // them in their order (eight in flight), the others have nothing to do.  The rows that no token has
-// and the positions come behind, as above.  2 tokens, 11784 x 112: 23 -> 8 us.
+// and the positions come behind, as above.  2 tokens, 11784 x 112: 23 -> 7 us.
 constexpr int FEW = 256;
 static_assert(FEW == NT, "a thread for every position");
 __global__ __launch_bounds__(NT) void embed_few_kernel(SumArgs a, const int32_t* tok) {

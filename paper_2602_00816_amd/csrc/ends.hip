@@ -103,8 +103,8 @@ constexpr int HEAD_PIECE_ROUND = 256, HEAD_PIECE_MIN = 1024;
 constexpr int64_t HEAD_LAUNCH_ELEMS = (int64_t)1 << 35;
 // Operations of the logits from which on the rows without a target are put behind the others (a launch
 // of 5 us, of some 150 here), so that only the others are multiplied: 2500 x 32000 x 1024, of which 30%
-// have none: 462 -> 349 us; gradients of 8192 x 32000 x 2048 with half of them 9.51 -> 7.14 ms, with none
-// 9.92 -> 9.94.
+// have none: 520 -> 385 us, with none 517 -> 523; gradients of 8192 x 32000 x 2048 with half of them
+// 10.85 -> 7.97 ms, with none 11.37 -> 11.38.
 constexpr double HEAD_ORDER_OPS = 1.5e11;
 // rows up to which the target's logits are formed in fp64
 constexpr int HEAD_FINE_ROWS = 32;

@@ -1,6 +1,6 @@
 // The loss over the vocabulary at both points, a piece of the vocabulary at a time.
 //
-// For the logits' pair (lm, ld) of a row and its reference c = max_j (lm_j + |ld_j|) let
+// For the logits' pair (lm, ld) of a row and its reference c, from max_j (lm_j + |ld_j|) to max lm + max |ld|, let
 //   a_j = e^(lm_j - c) cosh ld_j,  s_j = e^(lm_j - c) sinh ld_j,  so that  e^(l_j+- - c) = a_j +- s_j,
 // each with full relative precision however small ld is, and Zm = sum a, Zd = sum s.  Then
 //   loss.m = c + log(Z+ Z-) / 2 - lm_y,          loss.d = log(Z+ / Z-) / 2 - ld_y   (Z+- = Zm +- Zd),
@@ -285,8 +285,8 @@ __global__ __launch_bounds__(NT) void head_join_kernel(HeadRows r, const P* part
 }
 
 // Gradient of logits that are in memory (one piece holds the vocabulary, or an fp32 model's many rows)
-// in the operand type, [Tp][C]; rows without a target and rows behind the last are zeros.  o may be the
-// logits (fp32 models).
+// in the operand type (what its rounding costs stands at head_gemm.hip's), [Tp][C]; rows without a target
+// and rows behind the last are zeros.  o may be the logits (fp32 models).
 __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ inline void store4(bf16_t* p, float a, float b, float c, float d) {
   auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16); };

@@ -318,6 +318,10 @@ __global__ __launch_bounds__(64 * WM * WN) void head_logits_kernel(HeadLogits a,
       }
     }
   } else {
+    // The gradient is held in the operand type, which its products read: bf16's half step, 2^-9 to 2^-8 of an
+    // element, is independent from one to the next and leaves 1.0e-4 of dx.m and 2.1e-4 of dx.d and dw
+    // (1024 x 32000 x 2048, float32 outputs; rounded to bf16 they are off by 1.7e-3).  Two bf16 parts
+    // would double the products.
     // bf16: through LDS, so that a store covers 8 rows of 64 columns (JN = 2) or 16 of 32; a wavefront's
     // own area, 32 rows of WTN columns for each channel in turn
     constexpr int LD = WTN + 4;      // elements: 8-byte rows, lanes of 32 rows on distinct banks
@@ -439,16 +443,16 @@ void launch_tile(const HeadLogits& a, const HeadRows& r, bool grad, hipStream_t 
 
 // The largest tile that the rows fill and that gives most compute units a workgroup.  Loss alone, us,
 // by tile (rows x columns):          256x128  128x128  64x128  64x64  32x128
-//   32 x 32000 x 2048                     84       60      53     54      53
-//   64 x 32000 x 2048                     85       63      56     65      70
-//   128 x 32000 x 2048                    87       73      87    100     116
-//   512 x 32000 x 2048                   193      233     295    345     415
-//   256 x 4096 x 512                      29       23      19     18      20
-//   512 x 4096 x 512                      30       26      24     26      29
-//   1024 x 4096 x 512                     31       28      32     34      40
+//   32 x 32000 x 2048                     92       64      51     52      51
+//   64 x 32000 x 2048                     93       64      55     67      71
+//   128 x 32000 x 2048                    99       72      85     99     110
+//   512 x 32000 x 2048                   213      242     294    344     406
+//   256 x 4096 x 512                      29       21      17     16      17
+//   512 x 4096 x 512                      31       24      21     22      25
+//   1024 x 4096 x 512                     31       25      29     31      36
 // (1 x 32000 x 2048 on weights that no cache holds: 60; 62 and 64 with tiles of 32 x 64 and 32 x 32.
-// 256 x 128 on four wavefronts of 128 x 64, and 128 x 256, are 1 to 5% slower than eight of 64 x 64 at
-// 8192 x 32000 x 2048.)
+// With three products 256 x 128 on four wavefronts of 128 x 64, and 128 x 256, were 1 to 5% slower than eight of
+// 64 x 64 at 8192 x 32000 x 2048.  The matrix cores are busy for 78% of the cycles there, 66% with three.)
 HeadTile head_tile(int T_, int C) {
   auto fills = [&](int bm, int bn) { return T_ > bm / 2 && (int64_t)ceil_div(T_, bm) * ceil_div(C, bn) >= 192; };
   if (fills(256, 128)) return {256, 128, 64};

@@ -336,7 +336,7 @@ struct HeadOut {
   double scale;
   float *loss_m, *loss_d;
   double* rowloss;
-  const void *xm, *xd;     // not null (fewer than 1024 rows): the target's logits are formed in fp64 from
+  const void *xm, *xd;     // not null (up to 32 rows): the target's logits are formed in fp64 from
   int64_t ldx;             // these, [T][ldx], and the vocabulary's rows
   const void *wm, *wd;
   int d;
